@@ -1,6 +1,7 @@
 """Compile the HIP libraries in place for gfx950 (hipcc cross-compiles; no GPU needed).
 
-* paper_2506_20252_amd/libpat.so -- the PAT collectives (C-ABI of include/pat.h)
+* paper_2506_20252_amd/libpat.so -- the PAT collectives (C-ABI of include/pat.h) and the operators
+                                   on gathered and scattered tensors (include/pat_ops.h)
 * synth/libpatsynth.so           -- the seeded input filler used by tests and the benchmark
 * paper_2506_20252_amd/libpatceiling.so -- streaming-ceiling probes (a copy, a copy into two buffers,
                                           a 2-read/1-write add) that the benchmark reports beside
@@ -20,7 +21,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 
 TARGETS = [
     (os.path.join(PKG, "libpat.so"),
-     [os.path.join(CSRC, f) for f in ("plan.cpp", "api.cpp", "kernels.hip", "walk.hip", "noalloc.hip")]),
+     [os.path.join(CSRC, f) for f in ("plan.cpp", "api.cpp", "kernels.hip", "walk.hip", "noalloc.hip",
+                                      "ops.cpp", "mx.hip", "mx_grad.hip", "embedding.hip", "dropout.hip")]),
     (os.path.join(ROOT, "synth", "libpatsynth.so"), [os.path.join(ROOT, "synth", "synth.hip")]),
     (os.path.join(PKG, "libpatceiling.so"), [os.path.join(CSRC, "ceiling.hip")]),
 ]

@@ -16,6 +16,7 @@
 
 #include "../../include/pat.h"
 #include "kernels.hpp"
+#include "ops.hpp"
 #include "plan.hpp"
 #include "walk.hpp"
 
@@ -1229,6 +1230,8 @@ pat_status_t describe(int coll, int N, size_t count, pat_dtype_t dt, pat::PlanDe
 }
 
 }  // namespace
+
+void pat::record_hip_error(hipError_t e) { g_last_hip.store((int)e); }
 
 extern "C" {
 
