@@ -122,6 +122,7 @@ pat_status_t pat_embedding(const void* tokens, int token_bytes, size_t ntokens, 
  * tokens[t] == first + v, 0 where there is none.  g: ntokens x cols; out: rows x
  * cols, every element written.  Tokens are sorted (stable) first; a row's sum runs
  * over its tokens in rising t, in pieces whose partial sums are added in order.
+ * Fewer than 2^28 tokens and rows, 2^23 columns (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_embedding_grad(const void* tokens, int token_bytes, size_t ntokens, const void* g, int64_t g_stride,
                                 pat_dtype_t g_dtype, int64_t first, size_t rows, size_t cols, float scale, void* out,

@@ -1,4 +1,6 @@
 // Embedding lookup with scaling, and its dense gradient by sorted tokens.
+#include <algorithm>
+
 #include "ops_device.hpp"
 
 namespace pat {
@@ -15,15 +17,37 @@ __device__ __forceinline__ int64_t token_row(const char* tokens, int token_bytes
   return row < (uint64_t)rows ? (int64_t)row : -1;
 }
 
-// One workgroup per token (in turn).
+// A row is taken by `lanes` lanes, 8 columns each at a time; a workgroup holds 256 / lanes tokens side by side and
+// kLookupTokens of them in turn, whose table rows a lane reads before it writes any.
+constexpr int kLookupTokens = 4;
+
 template <typename TI, typename TO>
 __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int token_bytes, int64_t ntokens, Mat table,
-                                                     int64_t first, int64_t rows, int64_t cols, float scale, MatOut out) {
-  for (int64_t t = blockIdx.x; t < ntokens; t += gridDim.x) {
-    const int64_t row = token_row(tokens, token_bytes, t, first, rows);
-    for (int64_t c = threadIdx.x; c < cols; c += 256)
-      TO::store((char*)out.p, t * out.stride + c,
-                row < 0 ? 0.0f : TI::load((const char*)table.p, row * table.stride + c) * scale);
+                                                     int64_t first, int64_t rows, int64_t cols, float scale, MatOut out,
+                                                     int lanes) {
+  const int side = 256 / lanes, lane = threadIdx.x % lanes;
+  const int64_t step = (int64_t)side * kLookupTokens;
+  for (int64_t t0 = blockIdx.x * step + threadIdx.x / lanes; t0 < ntokens; t0 += gridDim.x * step) {
+    int64_t row[kLookupTokens];
+#pragma unroll
+    for (int u = 0; u < kLookupTokens; ++u) {
+      const int64_t t = t0 + u * side;
+      row[u] = t < ntokens ? token_row(tokens, token_bytes, t, first, rows) : -1;
+    }
+    for (int64_t c = 8 * lane; c < cols; c += 8 * lanes) {
+      float v[kLookupTokens][8];
+#pragma unroll
+      for (int u = 0; u < kLookupTokens; ++u)
+        TI::template load8<false>((const char*)table.p + (row[u] * table.stride + c) * TI::kBytes,
+                                  row[u] < 0 ? 0 : cols - c, v[u]);
+#pragma unroll
+      for (int u = 0; u < kLookupTokens; ++u) {
+        const int64_t t = t0 + u * side;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = v[u][i] * scale;
+        TO::template store8<true>((char*)out.p + (t * out.stride + c) * TO::kBytes, t < ntokens ? cols - c : 0, v[u]);
+      }
+    }
   }
 }
 
@@ -185,41 +209,187 @@ __device__ __forceinline__ int32_t lower_bound(const int32_t* keys, int32_t n, i
   return lo;
 }
 
-// One workgroup per row (in turn): the row's tokens are keys' run of its number.
-template <typename TI, typename TO>
-__global__ __launch_bounds__(256) void sum_kernel(const int32_t* keys, const int32_t* pos, const int32_t* nvalid, Mat g,
-                                                  int64_t rows, int64_t cols, float scale, MatOut out) {
-  const int32_t n = nvalid ? *nvalid : 0;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const int32_t lo = lower_bound(keys, n, (int32_t)r), hi = lower_bound(keys, n, (int32_t)r + 1);
-    for (int64_t c = threadIdx.x; c < cols; c += 256) {
-      float s = 0.0f;
-      for (int32_t i = lo; i < hi; ++i) s += TI::load((const char*)g.p, (int64_t)pos[i] * g.stride + c);
-      TO::store((char*)out.p, r * out.stride + c, s * scale);
+// ---- sums over the sorted entries -------------------------------------------------------------------------
+//
+// The sorted entries are cut into pieces of equal length, whatever rows they belong to, so that a frequent token is
+// as much work as rare ones.  A row's entries inside one piece are summed in registers and written out at once;
+// what a row has in several pieces goes to the workspace, a row of float32 per piece, and join_kernel adds these in
+// order.  A piece has two such rows at most: slot 0 for the row of its first entry, slot 1 for that of its last.
+// Rows without an entry are zeroed by workgroups of their own in the same launch.
+
+struct SumArgs {
+  const int32_t *keys, *pos, *nvalid;  // nvalid == nullptr: there are no entries
+  Mat g;
+  MatOut out;
+  float* partial;  // [pieces][2][pitch]
+  int64_t rows, cols, pitch;
+  float scale;
+  int32_t piece;  // entries, a multiple of 8
+  int lanes, sum_wgs, zero_wgs;
+};
+
+constexpr int kZeroRows = 64;  // rows that one workgroup looks through for ones without an entry
+
+template <typename TO>
+__device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
+  __shared__ uint64_t absent;
+  const int64_t r0 = (int64_t)wg * kZeroRows;
+  if (threadIdx.x < 64) {
+    const int64_t r = r0 + threadIdx.x;
+    bool none = r < a.rows;
+    if (none && n) {
+      const int32_t at = lower_bound(a.keys, n, (int32_t)r);
+      none = at == n || a.keys[at] != (int32_t)r;
     }
+    const uint64_t m = __ballot(none);
+    if (threadIdx.x == 0) absent = m;
+  }
+  __syncthreads();
+  const int side = 256 / a.lanes, lane = threadIdx.x % a.lanes;
+  const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  const uint64_t m = absent;
+  for (int i = threadIdx.x / a.lanes; i < kZeroRows; i += side) {
+    if (!(m >> i & 1)) continue;
+    for (int64_t c = 8 * lane; c < a.cols; c += 8 * a.lanes)
+      TO::template store8<true>((char*)a.out.p + ((r0 + i) * a.out.stride + c) * TO::kBytes, a.cols - c, zero);
   }
 }
 
-// Workspace: two (keys, positions) pairs, the tiles' histograms, the number of kept entries.
+template <typename TI, typename TO>
+__global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
+  const int32_t n = a.nvalid ? *a.nvalid : 0;
+  if ((int)blockIdx.x >= a.sum_wgs) {
+    if (blockIdx.y == 0) zero_rows<TO>(a, (int)blockIdx.x - a.sum_wgs, n);
+    return;
+  }
+  const int64_t piece = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
+  const int64_t i0 = piece * a.piece, c = 8 * ((int64_t)blockIdx.y * a.lanes + threadIdx.x % a.lanes);
+  if (i0 >= n || c >= a.cols) return;
+  const int64_t i1 = min(i0 + a.piece, (int64_t)n), left = a.cols - c;
+  const bool open_left = i0 > 0 && a.keys[i0 - 1] == a.keys[i0];
+  const bool open_right = i1 < n && a.keys[i1] == a.keys[i1 - 1];
+
+  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  int32_t row = a.keys[i0];
+  bool head = true;  // still in the row of the piece's first entry
+  auto flush = [&](bool last) {
+    if ((head && open_left) || (last && open_right)) {
+      float* p = a.partial + (2 * piece + (head ? 0 : 1)) * a.pitch + c;
+      F32::store8<false>((char*)p, left, sum);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
+      TO::template store8<true>((char*)a.out.p + ((int64_t)row * a.out.stride + c) * TO::kBytes, left, v);
+    }
+  };
+  constexpr int U = 8;
+  for (int64_t i = i0; i < i1; i += U) {
+    int32_t key[U];
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(i + u, i1 - 1);
+      key[u] = a.keys[at];
+      TI::template load8<false>((const char*)a.g.p + ((int64_t)a.pos[at] * a.g.stride + c) * TI::kBytes, left, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u >= i1) break;
+      if (key[u] != row) {
+        flush(false);
+        row = key[u];
+        head = false;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
+    }
+  }
+  flush(true);
+}
+
+// One workgroup per boundary of two pieces and 256 columns.  The first boundary inside a row adds up the row's
+// partial sums: each wave a section of the pieces, then the waves' sums in order.
+constexpr int kJoinWaves = 8;
+
+template <typename TO>
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(SumArgs a) {
+  __shared__ v4f part[kJoinWaves][64];
+  const int32_t n = *a.nvalid;
+  const int64_t b = (int64_t)blockIdx.x + 1, at = b * a.piece;
+  if (at >= n) return;
+  const int32_t row = a.keys[at];
+  if (a.keys[at - 1] != row || (b > 1 && a.keys[at - a.piece - 1] == row)) return;
+  const int64_t p0 = b - 1, p1 = ((int64_t)lower_bound(a.keys, n, row + 1) - 1) / a.piece + 1;
+  const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+  const int64_t c = 256 * (int64_t)blockIdx.y + 4 * lane, per = (p1 - p0 + kJoinWaves - 1) / kJoinWaves;
+  v4f sum = {0, 0, 0, 0};
+  if (c < a.cols) {
+    // only the first piece may begin with another row
+    const int64_t lo = p0 + wave * per, hi = min(lo + per, p1);
+    const bool first_slot = a.keys[p0 * a.piece] == row;
+#pragma unroll 4
+    for (int64_t p = lo; p < hi; ++p) {
+      const int64_t slot = 2 * p + (p == p0 && !first_slot ? 1 : 0);
+      sum += ldg<v4f, false>((const char*)(a.partial + slot * a.pitch + c));
+    }
+  }
+  part[wave][lane] = sum;
+  __syncthreads();
+  if (wave || c >= a.cols) return;
+#pragma unroll
+  for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (c + j < a.cols) TO::store((char*)a.out.p, (int64_t)row * a.out.stride + c + j, sum[j] * a.scale);
+}
+
+// How the sums are cut: lanes for the columns, entries per piece.  Longer pieces write and join fewer partial sums,
+// shorter ones give more workgroups; 2048 of them keep the chip's loads in flight.
+struct SumPlan {
+  int lanes;
+  int32_t piece;
+  int64_t pieces, pitch, sum_wgs, zero_wgs, col_wgs;
+};
+
+SumPlan sum_plan(int64_t ntokens, int64_t rows, int64_t cols) {
+  SumPlan s;
+  s.lanes = row_lanes((cols + 7) / 8, 256);
+  s.col_wgs = (int64_t)ceil_div(cols, 8 * s.lanes);
+  s.piece = 64;
+  while (s.piece > 16 && (int64_t)ceil_div(ntokens, s.piece) * s.lanes * s.col_wgs < 2048 * 256) s.piece /= 2;
+  while ((int64_t)ceil_div(ntokens, s.piece) > 1 << 20) s.piece *= 2;  // bounds the launches and the workspace
+  s.pieces = (int64_t)ceil_div(ntokens, s.piece);
+  s.pitch = (cols + 7) / 8 * 8;
+  s.sum_wgs = (int64_t)ceil_div(s.pieces, 256 / s.lanes);
+  s.zero_wgs = (int64_t)ceil_div(rows, kZeroRows);
+  return s;
+}
+
+// Workspace: the number of kept entries, two (keys, positions) pairs, the tiles' histograms, the partial sums.
 struct GradSpace {
   int32_t *keys[2], *pos[2], *counts, *nvalid;
+  float* partial;
   size_t bytes;
 };
 
-GradSpace grad_space(char* base, int64_t ntokens, const SortPlan& s) {
+GradSpace grad_space(char* base, int64_t ntokens, const SortPlan& s, const SumPlan& u) {
   GradSpace w;
   size_t at = 0;
   auto take = [&](size_t words) {
-    int32_t* p = reinterpret_cast<int32_t*>(base + at);
+    char* p = base + at;
     at += ceil_div(words * 4, 16) * 16;
     return p;
   };
-  w.nvalid = take(1);
+  w.nvalid = (int32_t*)take(1);
   for (int i = 0; i < 2; ++i) {
-    w.keys[i] = take((size_t)ntokens);
-    w.pos[i] = take((size_t)ntokens);
+    w.keys[i] = (int32_t*)take((size_t)ntokens);
+    w.pos[i] = (int32_t*)take((size_t)ntokens);
   }
-  w.counts = take((size_t)s.tiles << s.bits);
+  w.counts = (int32_t*)take((size_t)s.tiles << s.bits);
+  w.partial = (float*)take(u.pieces > 1 ? (size_t)(2 * u.pieces * u.pitch) : 0);
   w.bytes = at;
   return w;
 }
@@ -240,20 +410,22 @@ hipError_t launch_embedding(const void* tokens, int token_bytes, int64_t ntokens
                             int64_t first, int64_t rows, int64_t cols, float scale, MatOut out, Elem dtype,
                             hipStream_t stream) {
   const auto kernel = table_dtype == Elem::f32 ? lookup_of<F32>(dtype) : lookup_of<B16>(dtype);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ntokens < (1 << 20) ? ntokens : 1 << 20)), dim3(256), 0, stream,
-                     (const char*)tokens, token_bytes, ntokens, table, first, rows, cols, scale, out);
+  const int lanes = row_lanes((cols + 7) / 8, 256);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<size_t>(ceil_div(ntokens, kLookupTokens * (256 / lanes)), 1 << 20)), dim3(256), 0, stream,
+                     (const char*)tokens, token_bytes, ntokens, table, first, rows, cols, scale, out, lanes);
   return hipGetLastError();
 }
 
-size_t embedding_grad_workspace(int64_t ntokens, int64_t rows, int64_t) {
-  return ntokens ? grad_space(nullptr, ntokens, sort_plan(ntokens, rows)).bytes : 0;
+size_t embedding_grad_workspace(int64_t ntokens, int64_t rows, int64_t cols) {
+  return ntokens ? grad_space(nullptr, ntokens, sort_plan(ntokens, rows), sum_plan(ntokens, rows, cols)).bytes : 0;
 }
 
 hipError_t launch_embedding_grad(const void* tokens, int token_bytes, int64_t ntokens, Mat g, Elem g_dtype, int64_t first,
                                  int64_t rows, int64_t cols, float scale, MatOut out, Elem dtype, void* workspace,
                                  hipStream_t stream) {
   const SortPlan plan = sort_plan(ntokens, rows);
-  const GradSpace w = grad_space((char*)workspace, ntokens, plan);
+  const SumPlan cut = sum_plan(ntokens, rows, cols);
+  const GradSpace w = grad_space((char*)workspace, ntokens, plan, cut);
   int at = 0;
   if (ntokens) {
     SortArgs a{};
@@ -284,9 +456,28 @@ hipError_t launch_embedding_grad(const void* tokens, int token_bytes, int64_t nt
       }
     }
   }
+  SumArgs u{};
+  u.keys = w.keys[at];
+  u.pos = w.pos[at];
+  u.nvalid = ntokens ? w.nvalid : nullptr;
+  u.g = g;
+  u.out = out;
+  u.partial = w.partial;
+  u.rows = rows;
+  u.cols = cols;
+  u.pitch = cut.pitch;
+  u.scale = scale;
+  u.piece = cut.piece;
+  u.lanes = cut.lanes;
+  u.sum_wgs = (int)cut.sum_wgs;
+  u.zero_wgs = (int)cut.zero_wgs;
   const auto kernel = g_dtype == Elem::f32 ? sum_of<F32>(dtype) : sum_of<B16>(dtype);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(rows < (1 << 20) ? rows : 1 << 20)), dim3(256), 0, stream, w.keys[at],
-                     w.pos[at], ntokens ? w.nvalid : nullptr, g, rows, cols, scale, out);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(cut.sum_wgs + cut.zero_wgs), (unsigned)cut.col_wgs), dim3(256), 0, stream, u);
+  if (cut.pieces > 1) {
+    const auto join = dtype == Elem::f32 ? join_kernel<F32> : join_kernel<B16>;
+    hipLaunchKernelGGL(join, dim3((unsigned)(cut.pieces - 1), (unsigned)ceil_div(cols, 256)), dim3(64 * kJoinWaves), 0,
+                       stream, u);
+  }
   return hipGetLastError();
 }
 

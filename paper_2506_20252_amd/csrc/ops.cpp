@@ -82,6 +82,11 @@ pat_status_t workspace_span(const void* p, size_t bytes, size_t need, Span* s) {
 bool dims_ok(size_t a, size_t b, size_t c = 0) { return a < kMaxDim && b < kMaxDim && c < kMaxDim; }
 bool groups_ok(size_t rows, size_t cols) { return rows * ((cols + 127) / 128) < kMaxDim; }
 
+// Embedding gradients: what a launch's grid holds.
+bool grad_dims_ok(size_t ntokens, size_t rows, size_t cols) {
+  return ntokens < size_t(1) << 28 && rows < size_t(1) << 28 && cols < size_t(1) << 23;
+}
+
 // Output tiles of 16 x 16: below 2^31 for one launch.
 bool tiles_ok(size_t rows, size_t cols) { return ((rows + 15) / 16) * ((cols + 15) / 16) < kMaxDim; }
 
@@ -207,7 +212,7 @@ pat_status_t pat_embedding(const void* tokens, int token_bytes, size_t ntokens, 
 }
 
 size_t pat_embedding_grad_workspace(size_t ntokens, size_t rows, size_t cols) {
-  if (!dims_ok(ntokens, rows, cols) || !rows || !cols) return 0;
+  if (!grad_dims_ok(ntokens, rows, cols) || !rows || !cols) return 0;
   return pat::embedding_grad_workspace(int64_t(ntokens), int64_t(rows), int64_t(cols));
 }
 
@@ -218,7 +223,7 @@ pat_status_t pat_embedding_grad(const void* tokens, int token_bytes, size_t ntok
   Elem ge, e;
   if (!elem_of(g_dtype, &ge) || !elem_of(dtype, &e)) return PAT_ERR_UNSUPPORTED;
   if (token_bytes != 4 && token_bytes != 8) return PAT_ERR_UNSUPPORTED;
-  if (!dims_ok(ntokens, rows, cols)) return PAT_ERR_UNSUPPORTED;
+  if (!grad_dims_ok(ntokens, rows, cols)) return PAT_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0) return PAT_OK;
   Span tk, in, o, w;
   if (!span_of(tokens, ntokens * size_t(token_bytes), size_t(token_bytes), &tk) ||
