@@ -25,8 +25,9 @@ template <typename TI, typename TO>
 __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int token_bytes, int64_t ntokens, Mat table,
                                                      int64_t first, int64_t rows, int64_t cols, float scale, MatOut out,
                                                      int lanes) {
+  constexpr bool SPLIT = Split<TI, TO>::value;
   const int side = 256 / lanes, lane = threadIdx.x % lanes;
-  const int64_t step = (int64_t)side * kLookupTokens;
+  const int64_t step = (int64_t)side * kLookupTokens, gap = lane_gap<SPLIT>(lanes);
   for (int64_t t0 = blockIdx.x * step + threadIdx.x / lanes; t0 < ntokens; t0 += gridDim.x * step) {
     int64_t row[kLookupTokens];
 #pragma unroll
@@ -34,19 +35,25 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
       const int64_t t = t0 + u * side;
       row[u] = t < ntokens ? token_row(tokens, token_bytes, t, first, rows) : -1;
     }
-    for (int64_t c = 8 * lane; c < cols; c += 8 * lanes) {
+    auto columns = [&](int64_t c, auto full) {
+      constexpr bool FULL = decltype(full)::value;
       float v[kLookupTokens][8];
 #pragma unroll
-      for (int u = 0; u < kLookupTokens; ++u)
-        TI::template load8<false>((const char*)table.p + (row[u] * table.stride + c) * TI::kBytes,
-                                  row[u] < 0 ? 0 : cols - c, v[u]);
+      for (int u = 0; u < kLookupTokens; ++u)  // a token that the table does not hold reads row 0 and is zeroed below
+        load8<TI, SPLIT, false, FULL>((const char*)table.p + (max(row[u], (int64_t)0) * table.stride + c) * TI::kBytes,
+                                      rows ? cols - c : 0, gap, v[u]);
 #pragma unroll
       for (int u = 0; u < kLookupTokens; ++u) {
         const int64_t t = t0 + u * side;
+        if (t >= ntokens) break;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[u][i] = v[u][i] * scale;
-        TO::template store8<true>((char*)out.p + (t * out.stride + c) * TO::kBytes, t < ntokens ? cols - c : 0, v[u]);
+        for (int i = 0; i < 8; ++i) v[u][i] = row[u] < 0 ? 0.0f : v[u][i] * scale;
+        store8<TO, SPLIT, true, FULL>((char*)out.p + (t * out.stride + c) * TO::kBytes, cols - c, gap, v[u]);
       }
+    };
+    for (int64_t c = lane_column<SPLIT>(lane); c < cols; c += 8 * lanes) {
+      if (rows && cols - c >= gap + 4) columns(c, Bool<true>{});
+      else columns(c, Bool<false>{});
     }
   }
 }
@@ -146,9 +153,10 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
     before[j] = 0;
     if (j >= per || b >= bins) continue;
     int32_t total = 0;
+#pragma unroll 16
     for (int32_t w = 0; w < a.tiles; ++w) {
       const int32_t c = a.counts[(int64_t)w * bins + b];
-      if (w < (int32_t)blockIdx.x) before[j] += c;
+      before[j] += w < (int32_t)blockIdx.x ? c : 0;
       total += c;
     }
     before[j] += all;
@@ -245,105 +253,155 @@ __device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
     if (threadIdx.x == 0) absent = m;
   }
   __syncthreads();
+  constexpr bool SPLIT = Split<TO, TO>::value;
   const int side = 256 / a.lanes, lane = threadIdx.x % a.lanes;
+  const int64_t gap = lane_gap<SPLIT>(a.lanes);
   const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   const uint64_t m = absent;
   for (int i = threadIdx.x / a.lanes; i < kZeroRows; i += side) {
     if (!(m >> i & 1)) continue;
-    for (int64_t c = 8 * lane; c < a.cols; c += 8 * a.lanes)
-      TO::template store8<true>((char*)a.out.p + ((r0 + i) * a.out.stride + c) * TO::kBytes, a.cols - c, zero);
+    for (int64_t c = lane_column<SPLIT>(lane); c < a.cols; c += 8 * a.lanes) {
+      char* p = (char*)a.out.p + ((r0 + i) * a.out.stride + c) * TO::kBytes;
+      if (a.cols - c >= gap + 4) store8<TO, SPLIT, true, true>(p, a.cols - c, gap, zero);
+      else store8<TO, SPLIT, true, false>(p, a.cols - c, gap, zero);
+    }
   }
 }
 
-template <typename TI, typename TO>
+// UNIFORM: a piece's lanes are whole waves (rows of 505 columns and more).  A wave then holds 64 entries at a time, one
+// per lane, and takes each from its lane into scalar registers: no load of a row waits for a load of its entry.
+template <bool UNIFORM, typename TI, typename TO>
 __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
   const int32_t n = a.nvalid ? *a.nvalid : 0;
-  if ((int)blockIdx.x >= a.sum_wgs) {
-    if (blockIdx.y == 0) zero_rows<TO>(a, (int)blockIdx.x - a.sum_wgs, n);
+  // both kinds of workgroups in turn, as long as there are both
+  const int both = 2 * min(a.sum_wgs, a.zero_wgs), rest = (int)blockIdx.x - both;
+  const bool zeroes = rest < 0 ? blockIdx.x & 1 : a.zero_wgs > a.sum_wgs;
+  const int wg = rest < 0 ? blockIdx.x / 2 : both / 2 + rest;
+  if (zeroes) {
+    if (blockIdx.y == 0) zero_rows<TO>(a, wg, n);
     return;
   }
-  const int64_t piece = (int64_t)blockIdx.x * (256 / a.lanes) + threadIdx.x / a.lanes;
-  const int64_t i0 = piece * a.piece, c = 8 * ((int64_t)blockIdx.y * a.lanes + threadIdx.x % a.lanes);
-  if (i0 >= n || c >= a.cols) return;
+  int side = threadIdx.x / a.lanes;
+  if constexpr (UNIFORM) side = __builtin_amdgcn_readfirstlane(side);
+  const int64_t piece = (int64_t)wg * (256 / a.lanes) + side;
+  constexpr bool SPLIT = Split<TI, TO>::value;
+  const int64_t i0 = piece * a.piece, gap = lane_gap<SPLIT>(a.lanes);
+  const int64_t c = 8 * (int64_t)blockIdx.y * a.lanes + lane_column<SPLIT>(threadIdx.x % a.lanes);
+  if (i0 >= n) return;
   const int64_t i1 = min(i0 + a.piece, (int64_t)n), left = a.cols - c;
   const bool open_left = i0 > 0 && a.keys[i0 - 1] == a.keys[i0];
   const bool open_right = i1 < n && a.keys[i1] == a.keys[i1 - 1];
 
-  float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  int32_t row = a.keys[i0];
-  bool head = true;  // still in the row of the piece's first entry
-  auto flush = [&](bool last) {
-    if ((head && open_left) || (last && open_right)) {
-      float* p = a.partial + (2 * piece + (head ? 0 : 1)) * a.pitch + c;
-      F32::store8<false>((char*)p, left, sum);
-    } else {
-      float v[8];
+  auto columns = [&](auto full) {
+    constexpr bool FULL = decltype(full)::value;
+    float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int32_t row = a.keys[i0];
+    bool head = true;  // still in the row of the piece's first entry
+    auto flush = [&](bool last) {
+      if ((head && open_left) || (last && open_right)) {
+        float* p = a.partial + (2 * piece + (head ? 0 : 1)) * a.pitch + c;
+        store8<F32, SPLIT, false, FULL>((char*)p, left, gap, sum);
+      } else {
+        float v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
-      TO::template store8<true>((char*)a.out.p + ((int64_t)row * a.out.stride + c) * TO::kBytes, left, v);
-    }
-  };
-  constexpr int U = 8;
-  for (int64_t i = i0; i < i1; i += U) {
-    int32_t key[U];
-    float v[U][8];
+        for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
+        store8<TO, SPLIT, true, FULL>((char*)a.out.p + ((int64_t)row * a.out.stride + c) * TO::kBytes, left, gap, v);
+      }
+    };
+    constexpr int U = 8;
+    int32_t key64 = 0, pos64 = 0;
+    for (int64_t i = i0; i < i1; i += U) {
+      if (UNIFORM && (i - i0) % 64 == 0) {
+        const int64_t at = min(i + threadIdx.x % 64, i1 - 1);
+        key64 = a.keys[at];
+        pos64 = a.pos[at];
+      }
+      int32_t key[U];
+      float v[U][8];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = min(i + u, i1 - 1);
-      key[u] = a.keys[at];
-      TI::template load8<false>((const char*)a.g.p + ((int64_t)a.pos[at] * a.g.stride + c) * TI::kBytes, left, v[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= i1) break;
-      if (key[u] != row) {
-        flush(false);
-        row = key[u];
-        head = false;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+      for (int u = 0; u < U; ++u) {
+        int64_t pos;
+        if constexpr (UNIFORM) {
+          const int src = (int)min(i + u, i1 - 1) - (int)(i - (i - i0) % 64);
+          key[u] = __builtin_amdgcn_readlane(key64, src);
+          pos = __builtin_amdgcn_readlane(pos64, src);
+        } else {
+          const int64_t at = min(i + u, i1 - 1);
+          key[u] = a.keys[at];
+          pos = a.pos[at];
+        }
+        load8<TI, SPLIT, true, FULL>((const char*)a.g.p + (pos * a.g.stride + c) * TI::kBytes, left, gap, v[u]);
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
+      for (int u = 0; u < U; ++u) {
+        if (i + u >= i1) break;
+        if (key[u] != row) {
+          flush(false);
+          row = key[u];
+          head = false;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) sum[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
+      }
     }
-  }
-  flush(true);
+    flush(true);
+  };
+  // one way for the whole wave: entries are taken from every lane, so every lane has to be there
+  if (__all(left >= gap + 4)) columns(Bool<true>{});
+  else columns(Bool<false>{});
 }
 
-// One workgroup per boundary of two pieces and 256 columns.  The first boundary inside a row adds up the row's
-// partial sums: each wave a section of the pieces, then the waves' sums in order.
-constexpr int kJoinWaves = 8;
+// A workgroup looks at kJoinPieces boundaries between pieces, for 256 columns.  Where a row goes over a boundary and
+// over none before it, the workgroup adds up the row's partial sums: each wave takes a section of the pieces, then
+// the waves' sums are added in order.
+constexpr int kJoinWaves = 4, kJoinPieces = 4;
 
 template <typename TO>
 __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(SumArgs a) {
   __shared__ v4f part[kJoinWaves][64];
   const int32_t n = *a.nvalid;
-  const int64_t b = (int64_t)blockIdx.x + 1, at = b * a.piece;
-  if (at >= n) return;
-  const int32_t row = a.keys[at];
-  if (a.keys[at - 1] != row || (b > 1 && a.keys[at - a.piece - 1] == row)) return;
-  const int64_t p0 = b - 1, p1 = ((int64_t)lower_bound(a.keys, n, row + 1) - 1) / a.piece + 1;
   const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
-  const int64_t c = 256 * (int64_t)blockIdx.y + 4 * lane, per = (p1 - p0 + kJoinWaves - 1) / kJoinWaves;
-  v4f sum = {0, 0, 0, 0};
-  if (c < a.cols) {
-    // only the first piece may begin with another row
-    const int64_t lo = p0 + wave * per, hi = min(lo + per, p1);
-    const bool first_slot = a.keys[p0 * a.piece] == row;
-#pragma unroll 4
-    for (int64_t p = lo; p < hi; ++p) {
-      const int64_t slot = 2 * p + (p == p0 && !first_slot ? 1 : 0);
-      sum += ldg<v4f, false>((const char*)(a.partial + slot * a.pitch + c));
-    }
+  const int64_t b0 = (int64_t)blockIdx.x * kJoinPieces + 1, at = (b0 + lane) * a.piece;
+  bool starts = false;
+  if (lane < kJoinPieces && at < n) {
+    const int32_t row = a.keys[at];
+    starts = a.keys[at - 1] == row && !(b0 + lane > 1 && a.keys[at - a.piece - 1] == row);
   }
-  part[wave][lane] = sum;
-  __syncthreads();
-  if (wave || c >= a.cols) return;
+  const int64_t c = 256 * (int64_t)blockIdx.y + 4 * lane;
+  for (uint64_t todo = __ballot(starts); todo; todo &= todo - 1) {  // the same in every wave
+    const int64_t b = b0 + __builtin_ctzll(todo), p0 = b - 1;
+    const int32_t row = a.keys[b * a.piece];
+    // pieces after p0 that begin with the row, 64 looked at together
+    int64_t p1 = b + 1;
+    for (;;) {
+      const int64_t p = p1 + lane;
+      const uint64_t other = __ballot(p * a.piece >= n || a.keys[p * a.piece] != row);
+      p1 += other ? __builtin_ctzll(other) : 64;
+      if (other) break;
+    }
+    const int64_t per = (p1 - p0 + kJoinWaves - 1) / kJoinWaves, lo = p0 + wave * per, hi = min(lo + per, p1);
+    const bool first_slot = a.keys[p0 * a.piece] == row;  // only the first piece may begin with another row
+    v4f sum = {0, 0, 0, 0};
+    if (c < a.cols) {
+#pragma unroll 4
+      for (int64_t p = lo; p < hi; ++p) {
+        const int64_t slot = 2 * p + (p == p0 && !first_slot ? 1 : 0);
+        sum += ldg<v4f, false>((const char*)(a.partial + slot * a.pitch + c));
+      }
+    }
+    part[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && c < a.cols) {
 #pragma unroll
-  for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
+      for (int w = 1; w < kJoinWaves; ++w) sum += part[w][lane];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (c + j < a.cols) TO::store((char*)a.out.p, (int64_t)row * a.out.stride + c + j, sum[j] * a.scale);
+      for (int j = 0; j < 4; ++j)
+        if (c + j < a.cols) TO::store((char*)a.out.p, (int64_t)row * a.out.stride + c + j, sum[j] * a.scale);
+    }
+    __syncthreads();
+  }
 }
 
 // How the sums are cut: lanes for the columns, entries per piece.  Longer pieces write and join fewer partial sums,
@@ -399,9 +457,9 @@ auto lookup_of(Elem dtype) {
   return dtype == Elem::f32 ? lookup_kernel<TI, F32> : lookup_kernel<TI, B16>;
 }
 
-template <typename TI>
+template <bool UNIFORM, typename TI>
 auto sum_of(Elem dtype) {
-  return dtype == Elem::f32 ? sum_kernel<TI, F32> : sum_kernel<TI, B16>;
+  return dtype == Elem::f32 ? sum_kernel<UNIFORM, TI, F32> : sum_kernel<UNIFORM, TI, B16>;
 }
 
 }  // namespace
@@ -411,8 +469,9 @@ hipError_t launch_embedding(const void* tokens, int token_bytes, int64_t ntokens
                             hipStream_t stream) {
   const auto kernel = table_dtype == Elem::f32 ? lookup_of<F32>(dtype) : lookup_of<B16>(dtype);
   const int lanes = row_lanes((cols + 7) / 8, 256);
-  hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<size_t>(ceil_div(ntokens, kLookupTokens * (256 / lanes)), 1 << 20)), dim3(256), 0, stream,
-                     (const char*)tokens, token_bytes, ntokens, table, first, rows, cols, scale, out, lanes);
+  const size_t wgs = std::min<size_t>(ceil_div(ntokens, kLookupTokens * (256 / lanes)), 1 << 20);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, stream, (const char*)tokens, token_bytes, ntokens, table,
+                     first, rows, cols, scale, out, lanes);
   return hipGetLastError();
 }
 
@@ -471,11 +530,13 @@ hipError_t launch_embedding_grad(const void* tokens, int token_bytes, int64_t nt
   u.lanes = cut.lanes;
   u.sum_wgs = (int)cut.sum_wgs;
   u.zero_wgs = (int)cut.zero_wgs;
-  const auto kernel = g_dtype == Elem::f32 ? sum_of<F32>(dtype) : sum_of<B16>(dtype);
+  const bool uniform = cut.lanes >= 64, f32 = g_dtype == Elem::f32;
+  const auto kernel = uniform ? (f32 ? sum_of<true, F32>(dtype) : sum_of<true, B16>(dtype))
+                              : (f32 ? sum_of<false, F32>(dtype) : sum_of<false, B16>(dtype));
   hipLaunchKernelGGL(kernel, dim3((unsigned)(cut.sum_wgs + cut.zero_wgs), (unsigned)cut.col_wgs), dim3(256), 0, stream, u);
   if (cut.pieces > 1) {
     const auto join = dtype == Elem::f32 ? join_kernel<F32> : join_kernel<B16>;
-    hipLaunchKernelGGL(join, dim3((unsigned)(cut.pieces - 1), (unsigned)ceil_div(cols, 256)), dim3(64 * kJoinWaves), 0,
+    hipLaunchKernelGGL(join, dim3((unsigned)ceil_div(cut.pieces - 1, kJoinPieces), (unsigned)ceil_div(cols, 256)), dim3(64 * kJoinWaves), 0,
                        stream, u);
   }
   return hipGetLastError();

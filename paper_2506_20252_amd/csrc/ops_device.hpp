@@ -23,64 +23,103 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// An element type in memory: single elements, and 8 consecutive ones as vectors at element-aligned addresses, of
-// which the first n count (the others read as 0 and are not written).  NT: nontemporal.
+// A compile-time truth value as an argument.
+template <bool B>
+struct Bool {
+  static constexpr bool value = B;
+};
+
+// Element types in memory: single elements, and a lane's 8 columns as vectors at element-aligned addresses.
 struct F32 {
   static constexpr int kBytes = 4;
+  typedef v4f vec4;
   __device__ static float load(const char* p, int64_t i) { return ldg<float, false>(p + i * 4); }
   __device__ static void store(char* p, int64_t i, float v) { stg<false>(p + i * 4, v); }
-  template <bool NT>
-  __device__ static void load8(const char* p, int64_t n, float (&v)[8]) {
-    if (n >= 8) {
-      const v4f a = ldg<v4f, NT, 4>(p), b = ldg<v4f, NT, 4>(p + 16);
+  __device__ static void widen(const vec4& a, float* v) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < n ? ldg<float, false>(p + 4 * i) : 0.0f;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = a[i];
   }
-  template <bool NT>
-  __device__ static void store8(char* p, int64_t n, const float (&v)[8]) {
-    if (n >= 8) {
-      stg<NT, 4>(p, v4f{v[0], v[1], v[2], v[3]});
-      stg<NT, 4>(p + 16, v4f{v[4], v[5], v[6], v[7]});
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) stg<false>(p + 4 * i, v[i]);
-    }
-  }
+  __device__ static vec4 narrow(const float* v) { return vec4{v[0], v[1], v[2], v[3]}; }
 };
 struct B16 {
   static constexpr int kBytes = 2;
+  typedef v2u vec4;
   __device__ static float load(const char* p, int64_t i) { return bf16_lo(ldg<uint16_t, false>(p + i * 2)); }
   __device__ static void store(char* p, int64_t i, float v) { stg<false>(p + i * 2, (uint16_t)bf16_rne(v)); }
-  template <bool NT>
-  __device__ static void load8(const char* p, int64_t n, float (&v)[8]) {
-    if (n >= 8) {
-      const v4u a = ldg<v4u, NT, 2>(p);
+  __device__ static void widen(const vec4& a, float* v) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < n ? bf16_lo(ldg<uint16_t, false>(p + 2 * i)) : 0.0f;
-    }
+    for (int i = 0; i < 2; ++i) v[2 * i] = bf16_lo(a[i]), v[2 * i + 1] = bf16_hi(a[i]);
   }
-  template <bool NT>
-  __device__ static void store8(char* p, int64_t n, const float (&v)[8]) {
-    if (n >= 8) {
-      v4u a;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) a[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-      stg<NT, 2>(p, a);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < n) stg<false>(p + 2 * i, (uint16_t)bf16_rne(v[i]));
-    }
-  }
+  __device__ static vec4 narrow(const float* v) { return vec4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])}; }
 };
+
+// The 8 columns that a lane takes at a time out of `lanes` lanes' 8 * lanes: one vector of 16 bytes where every type
+// is bfloat16, else two vectors of 4 columns, `lanes` vectors apart.  Either way the lanes of a wave read and write
+// consecutive bytes with each instruction; float32 columns taken 8 in a row would be written in alternate
+// 16-byte pieces.
+template <typename A, typename B>
+struct Split {
+  static constexpr bool value = A::kBytes == 4 || B::kBytes == 4;
+};
+// First of a lane's columns, and from there to the first of its second four.
+template <bool SPLIT>
+__device__ __forceinline__ int64_t lane_column(int lane) {
+  return SPLIT ? 4 * lane : 8 * lane;
+}
+template <bool SPLIT>
+__device__ __forceinline__ int64_t lane_gap(int lanes) {
+  return SPLIT ? 4 * lanes : 4;
+}
+
+// Loads and stores of such columns at p, of which those below n (counted from p) exist: others read as 0 and are not
+// written.  FULL: all exist; without the branch, the loads of several rows are in flight together.  NT: nontemporal.
+template <typename T, bool SPLIT, bool NT, bool FULL>
+__device__ __forceinline__ void load8(const char* p, int64_t n, int64_t gap, float (&v)[8]) {
+  if constexpr (FULL && !SPLIT && T::kBytes == 2) {
+    const v4u a = ldg<v4u, NT, 2>(p);
+    T::widen({a[0], a[1]}, v);
+    T::widen({a[2], a[3]}, v + 4);
+  } else if constexpr (FULL) {
+    typedef typename T::vec4 V;
+    const V a = ldg<V, NT, T::kBytes>(p), b = ldg<V, NT, T::kBytes>(p + gap * T::kBytes);
+    T::widen(a, v);
+    T::widen(b, v + 4);
+  } else {
+    typedef typename T::vec4 V;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = h * gap;
+      if (n - at >= 4) {
+        T::widen(ldg<V, NT, T::kBytes>(p + at * T::kBytes), v + 4 * h);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * h + i] = at + i < n ? T::load(p, at + i) : 0.0f;
+      }
+    }
+  }
+}
+template <typename T, bool SPLIT, bool NT, bool FULL>
+__device__ __forceinline__ void store8(char* p, int64_t n, int64_t gap, const float (&v)[8]) {
+  if constexpr (FULL && !SPLIT && T::kBytes == 2) {
+    const v2u a = T::narrow(v), b = T::narrow(v + 4);
+    stg<NT, 2>(p, v4u{a[0], a[1], b[0], b[1]});
+  } else if constexpr (FULL) {
+    stg<NT, T::kBytes>(p, T::narrow(v));
+    stg<NT, T::kBytes>(p + gap * T::kBytes, T::narrow(v + 4));
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = h * gap;
+      if (n - at >= 4) {
+        stg<NT, T::kBytes>(p + at * T::kBytes, T::narrow(v + 4 * h));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at + i < n) T::store(p, at + i, v[4 * h + i]);
+      }
+    }
+  }
+}
 
 // Lanes of a power of two that take a row of `vectors` vectors, at most a workgroup of `threads`.
 inline int row_lanes(int64_t vectors, int threads) {

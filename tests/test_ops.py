@@ -418,6 +418,13 @@ def test_embedding(ntokens, rows, cols, first, dtype, out_dtype, wide):
         within(out, want, 0.0, 0, out_dtype)
 
 
+@gpu
+def test_embedding_in_a_table_without_rows():
+    out = torch.full((9, 40), 5.0, device="cuda")
+    ops.embedding(torch.arange(9, device="cuda"), torch.empty((0, 40), device="cuda"), dtype=F32, out=out)
+    assert bool((out == 0).all())
+
+
 def token_sets():
     g = np.random.default_rng(9)
     yield "one", np.array([3]), 10, 0
