@@ -73,7 +73,9 @@ pat_status_t pat_mx_dequantize(const void* codes, const void* scales, size_t row
 
 /*
  * out[i][j] = sum over x < k of a[i][x] * b[j][x]: a (m rows) and b (n rows) in
- * the stored form, both of k columns; out PAT_FLOAT32 or PAT_BFLOAT16.
+ * the stored form, both of k columns; out PAT_FLOAT32 or PAT_BFLOAT16.  All
+ * products here: fewer than 2^26 rows and columns of the output, 2^24 terms of a
+ * sum (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, size_t m,
                            size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, void* workspace,

@@ -87,8 +87,11 @@ bool grad_dims_ok(size_t ntokens, size_t rows, size_t cols) {
   return ntokens < size_t(1) << 28 && rows < size_t(1) << 28 && cols < size_t(1) << 23;
 }
 
-// Output tiles of 16 x 16: below 2^31 for one launch.
-bool tiles_ok(size_t rows, size_t cols) { return ((rows + 15) / 16) * ((cols + 15) / 16) < kMaxDim; }
+// Products: what a launch's grid and its kernels' 32-bit offsets inside a tile's rows hold.
+bool product_ok(size_t rows, size_t cols, size_t inner) {
+  return rows < size_t(1) << 26 && cols < size_t(1) << 26 && inner < size_t(1) << 24 &&
+         ((rows + 15) / 16) * ((cols + 15) / 16) < kMaxDim;
+}
 
 }  // namespace
 
@@ -123,7 +126,7 @@ pat_status_t pat_mx_dequantize(const void* codes, const void* scales, size_t row
 }
 
 size_t pat_mx_matmul_workspace(size_t m, size_t n, size_t k) {
-  if (!dims_ok(m, n, k) || !m || !n) return 0;
+  if (!product_ok(m, n, k) || !m || !n) return 0;
   return pat::mx_matmul_workspace(int64_t(m), int64_t(n), int64_t(k));
 }
 
@@ -132,7 +135,7 @@ pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void
                            size_t workspace_bytes, hipStream_t stream) {
   Elem e;
   if (!elem_of(dtype, &e)) return PAT_ERR_UNSUPPORTED;
-  if (!dims_ok(m, n, k) || !groups_ok(m, k) || !groups_ok(n, k) || !tiles_ok(m, n)) return PAT_ERR_UNSUPPORTED;
+  if (!product_ok(m, n, k) || !groups_ok(m, k) || !groups_ok(n, k)) return PAT_ERR_UNSUPPORTED;
   if (m == 0 || n == 0) return PAT_OK;
   Span ac, as, bc, bs, o, w;
   if (!mx_spans(a_codes, a_scales, m, k, &ac, &as) || !mx_spans(b_codes, b_scales, n, k, &bc, &bs) ||
@@ -146,7 +149,7 @@ pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void
 }
 
 size_t pat_mx_linear_workspace(size_t m, size_t n, size_t k) {
-  if (!dims_ok(m, n, k) || !m || !n || !groups_ok(m, k)) return 0;
+  if (!product_ok(m, n, k) || !m || !n || !groups_ok(m, k)) return 0;
   return pat::mx_linear_workspace(int64_t(m), int64_t(n), int64_t(k));
 }
 
@@ -155,7 +158,7 @@ pat_status_t pat_mx_linear(const void* x, int64_t x_stride, pat_dtype_t x_dtype,
                            size_t workspace_bytes, hipStream_t stream) {
   Elem xe, e;
   if (!elem_of(x_dtype, &xe) || !elem_of(dtype, &e)) return PAT_ERR_UNSUPPORTED;
-  if (!dims_ok(m, n, k) || !groups_ok(m, k) || !groups_ok(n, k) || !tiles_ok(m, n)) return PAT_ERR_UNSUPPORTED;
+  if (!product_ok(m, n, k) || !groups_ok(m, k) || !groups_ok(n, k)) return PAT_ERR_UNSUPPORTED;
   if (m == 0 || n == 0) return PAT_OK;
   Span in, wc, ws, o, w;
   if (!matrix_span(x, x_stride, m, k, elem_bytes(xe), &in) || !mx_spans(w_codes, w_scales, n, k, &wc, &ws) ||
@@ -169,7 +172,7 @@ pat_status_t pat_mx_linear(const void* x, int64_t x_stride, pat_dtype_t x_dtype,
 }
 
 size_t pat_mx_matmul_grad_workspace(size_t rows, size_t inner, size_t cols) {
-  if (!dims_ok(rows, inner, cols) || !rows || !cols) return 0;
+  if (!product_ok(rows, cols, inner) || !rows || !cols) return 0;
   return pat::mx_grad_workspace(int64_t(rows), int64_t(inner), int64_t(cols));
 }
 
@@ -178,7 +181,7 @@ pat_status_t pat_mx_matmul_grad(const void* g, int64_t g_stride, int transposed,
                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
   Elem e;
   if (!elem_of(dtype, &e)) return PAT_ERR_UNSUPPORTED;
-  if (!dims_ok(rows, inner, cols) || !groups_ok(inner, cols) || !tiles_ok(rows, cols)) return PAT_ERR_UNSUPPORTED;
+  if (!product_ok(rows, cols, inner) || !groups_ok(inner, cols)) return PAT_ERR_UNSUPPORTED;
   if (rows == 0 || cols == 0) return PAT_OK;
   Span in, qc, qs, o, w;
   if (!matrix_span(g, g_stride, transposed ? inner : rows, transposed ? rows : inner, 2, &in) ||

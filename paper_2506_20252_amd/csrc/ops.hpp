@@ -33,6 +33,8 @@ struct MxMat {
   const uint8_t* scales;
 };
 
+inline int64_t groups_of(int64_t cols) { return (cols + 127) / 128; }
+
 hipError_t launch_mx_quantize(Mat x, Elem dtype, int64_t rows, int64_t cols, uint8_t* codes, uint8_t* scales,
                               hipStream_t stream);
 hipError_t launch_mx_dequantize(MxMat q, int64_t rows, int64_t cols, MatOut out, Elem dtype, hipStream_t stream);

@@ -138,5 +138,22 @@ __device__ __forceinline__ float mx_scale_value(uint32_t s) {
   return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
 }
 
+// 32 values as 32 codes under one scale: the four words of a block's codes.
+__device__ __forceinline__ v4u mx_codes(const float (&v)[32], uint32_t s) {
+  v4u q = {0, 0, 0, 0};
+  if (s == 255u) return q;
+  const float scale = mx_scale_value(s);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t word = 0;
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w], v[8 * w + 1], scale, 0);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 2], v[8 * w + 3], scale, 1);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 4], v[8 * w + 5], scale, 2);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 6], v[8 * w + 7], scale, 3);
+    q[w] = word;
+  }
+  return q;
+}
+
 }  // namespace
 }  // namespace pat
