@@ -138,6 +138,97 @@ __device__ __forceinline__ float mx_scale_value(uint32_t s) {
   return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
 }
 
+// Eight consecutive elements as they are in memory, those from n on zero; nothing is done with what is loaded, so
+// that several are in flight together.
+template <typename T>
+struct Raw8 {
+  v4u w[T::kBytes / 2];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8(const char* p, int64_t n) {
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = v4u{0, 0, 0, 0};
+  if (n >= 8) {
+#pragma unroll
+    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(p + 16 * i);
+  } else if (n > 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i >= n) break;
+      if constexpr (T::kBytes == 4) r.w[i / 4][i % 4] = ldg<uint32_t, false>(p + 4 * i);
+      else r.w[0][i / 2] |= (uint32_t)ldg<uint16_t, false>(p + 2 * i) << (16 * (i & 1));
+    }
+  }
+  return r;
+}
+
+// Largest magnitude of 8 elements, as float32 bits.
+__device__ __forceinline__ uint32_t high_bits(const Raw8<F32>& r) {
+  uint32_t h = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) h = max(h, r.w[i / 4][i % 4] & 0x7FFFFFFFu);
+  return h;
+}
+__device__ __forceinline__ uint32_t high_bits(const Raw8<B16>& r) {
+  typedef unsigned short v2h __attribute__((ext_vector_type(2)));
+  v2h h = {0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h = __builtin_elementwise_max(h, __builtin_bit_cast(v2h, r.w[0][i] & 0x7FFF7FFFu));
+  return (uint32_t)(h[0] > h[1] ? h[0] : h[1]) << 16;
+}
+
+// The codes of 8 elements under scale byte s, one word.
+__device__ __forceinline__ uint32_t mx_codes(const Raw8<F32>& r, uint32_t s) {
+  const float scale = mx_scale_value(s);
+  auto f = [&](int i) { return __uint_as_float(r.w[i / 4][i % 4]); };
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f(0), f(1), scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f(2), f(3), scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f(4), f(5), scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f(6), f(7), scale, 3);
+  return s == 255u ? 0u : c;
+}
+__device__ __forceinline__ uint32_t mx_codes(const Raw8<B16>& r, uint32_t s) {
+  const float scale = mx_scale_value(s);
+  auto f = [&](int i) {
+    const uint32_t w = r.w[0][i];  // __builtin_bit_cast of a vector's element itself takes its first one
+    return __builtin_bit_cast(v2bf, w);
+  };
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, f(0), scale, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, f(1), scale, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, f(2), scale, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, f(3), scale, 3);
+  return s == 255u ? 0u : c;
+}
+
+// Division of numbers below 2^31 by a launch constant d < 2^31: with 2^(s - 1) < d <= 2^s and
+// m = ceil(2^(31 + s) / d) < 2^32, n / d = n * m >> (31 + s), since n * (m * d - 2^(31 + s)) < 2^(31 + s).
+struct Divisor {
+  uint32_t d, m;
+  int shift;
+  explicit Divisor(uint32_t divisor) : d(divisor), m(0), shift(31) {
+    while (((uint64_t)1 << (shift - 31)) < d) ++shift;
+    m = (uint32_t)((((__uint128_t)1 << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ uint32_t divide(uint32_t n) const { return (uint32_t)((uint64_t)n * m >> shift); }
+};
+
+// Lane exchange inside groups of 4 and 16 lanes; every lane of the wave has to be active.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+__device__ __forceinline__ uint32_t max_of_4(uint32_t v) {
+  v = max(v, dpp<0xB1>(v));         // quad_perm 1, 0, 3, 2
+  return max(v, dpp<0x4E>(v));      // quad_perm 2, 3, 0, 1
+}
+__device__ __forceinline__ uint32_t or_of_16_by_4(uint32_t v) {
+  v |= dpp<0x124>(v);               // row_ror 4
+  return v | dpp<0x128>(v);         // row_ror 8
+}
+
 // 32 values as 32 codes under one scale: the four words of a block's codes.
 __device__ __forceinline__ v4u mx_codes(const float (&v)[32], uint32_t s) {
   v4u q = {0, 0, 0, 0};
