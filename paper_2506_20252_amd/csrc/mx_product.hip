@@ -43,22 +43,6 @@ struct TileLds {
   uint8_t scales[2][kRows * 8];
 };
 
-// Where a tile of the output is; neighbours in `t` share rows of a or b.
-struct TilePlace {
-  int64_t i, j;
-};
-// Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles, in bands of 8 tile rows, so that what its
-// workgroups read together stays in its L2.
-__device__ __forceinline__ bool tile_place(int64_t tiles_m, int64_t tiles_n, TilePlace* p) {
-  const int64_t total = tiles_m * tiles_n, per = (total + 7) / 8;
-  const int64_t t = blockIdx.x % 8 * per + blockIdx.x / 8;
-  if (blockIdx.x / 8 >= per || t >= total) return false;
-  const int64_t band = t / (8 * tiles_n), in_band = t % (8 * tiles_n), high = min((int64_t)8, tiles_m - band * 8);
-  p->i = band * 8 + in_band % high;
-  p->j = in_band / high;
-  return true;
-}
-
 template <int F, typename T>
 __global__ __launch_bounds__(kTileThreads, F == 4 ? 1 : 2) void tile_kernel(MxMat a, MxMat b, int64_t m, int64_t n,
                                                                              int groups, MatOut out) {

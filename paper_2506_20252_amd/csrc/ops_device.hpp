@@ -246,5 +246,21 @@ __device__ __forceinline__ v4u mx_codes(const float (&v)[32], uint32_t s) {
   return q;
 }
 
+// Where a tile of the output is; neighbours in `t` share rows of a or b.
+struct TilePlace {
+  int64_t i, j;
+};
+// Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles, in bands of 8 tile rows, so that what its
+// workgroups read together stays in its L2.
+__device__ __forceinline__ bool tile_place(int64_t tiles_m, int64_t tiles_n, TilePlace* p) {
+  const int64_t total = tiles_m * tiles_n, per = (total + 7) / 8;
+  const int64_t t = blockIdx.x % 8 * per + blockIdx.x / 8;
+  if (blockIdx.x / 8 >= per || t >= total) return false;
+  const int64_t band = t / (8 * tiles_n), in_band = t % (8 * tiles_n), high = min((int64_t)8, tiles_m - band * 8);
+  p->i = band * 8 + in_band % high;
+  p->j = in_band / high;
+  return true;
+}
+
 }  // namespace
 }  // namespace pat
