@@ -8,7 +8,8 @@ allocate outputs and workspaces, and raise.  Marshalling only: all work is done
 by the HIP kernels of ``libpat.so``, and there is no fallback.
 
 Tensors are 2-D with unit stride along rows; rows may be strided.  Calls run on
-`stream`, by default torch's current stream of the tensors' device.
+`stream`, by default torch's current stream of the tensors' device; what they
+allocate belongs to that stream.
 """
 
 import ctypes
@@ -44,16 +45,19 @@ _SIGNATURES = {
                      ctypes.c_uint64, _P], _I),
 }
 
-_fns = {}
+class _Calls:
+    """The library's functions, each looked up and given its signature at its first use."""
 
-
-def _fn(name):
-    fn = _fns.get(name)
-    if fn is None:
+    def __getattr__(self, name):
+        if name not in _SIGNATURES:
+            raise AttributeError(name)
         fn = getattr(pat.lib(), name)
         fn.argtypes, fn.restype = _SIGNATURES[name]
-        _fns[name] = fn
-    return fn
+        setattr(self, name, fn)
+        return fn
+
+
+_c = _Calls()
 
 
 def _address(b):
@@ -68,69 +72,69 @@ def _address(b):
 
 
 def pat_mx_quantize(x, x_stride, rows, cols, dtype, codes, scales, stream=None):
-    return _fn("pat_mx_quantize")(_address(x), x_stride, rows, cols, pat._dtype(dtype), _address(codes),
+    return _c.pat_mx_quantize(_address(x), x_stride, rows, cols, pat._dtype(dtype), _address(codes),
                                   _address(scales), pat._stream(stream))
 
 
 def pat_mx_dequantize(codes, scales, rows, cols, out, out_stride, dtype, stream=None):
-    return _fn("pat_mx_dequantize")(_address(codes), _address(scales), rows, cols, _address(out), out_stride,
+    return _c.pat_mx_dequantize(_address(codes), _address(scales), rows, cols, _address(out), out_stride,
                                     pat._dtype(dtype), pat._stream(stream))
 
 
 def pat_mx_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, out_stride, dtype, workspace, workspace_bytes,
                   stream=None):
-    return _fn("pat_mx_matmul")(_address(a_codes), _address(a_scales), _address(b_codes), _address(b_scales), m, n, k,
+    return _c.pat_mx_matmul(_address(a_codes), _address(a_scales), _address(b_codes), _address(b_scales), m, n, k,
                                 _address(out), out_stride, pat._dtype(dtype), _address(workspace), workspace_bytes,
                                 pat._stream(stream))
 
 
 def pat_mx_matmul_workspace(m, n, k):
-    return _fn("pat_mx_matmul_workspace")(m, n, k)
+    return _c.pat_mx_matmul_workspace(m, n, k)
 
 
 def pat_mx_linear(x, x_stride, x_dtype, w_codes, w_scales, m, n, k, out, out_stride, dtype, workspace, workspace_bytes,
                   stream=None):
-    return _fn("pat_mx_linear")(_address(x), x_stride, pat._dtype(x_dtype), _address(w_codes), _address(w_scales), m, n, k,
+    return _c.pat_mx_linear(_address(x), x_stride, pat._dtype(x_dtype), _address(w_codes), _address(w_scales), m, n, k,
                                 _address(out), out_stride, pat._dtype(dtype), _address(workspace), workspace_bytes,
                                 pat._stream(stream))
 
 
 def pat_mx_linear_workspace(m, n, k):
-    return _fn("pat_mx_linear_workspace")(m, n, k)
+    return _c.pat_mx_linear_workspace(m, n, k)
 
 
 def pat_mx_matmul_grad(g, g_stride, transposed, q_codes, q_scales, rows, inner, cols, out, out_stride, dtype, workspace,
                        workspace_bytes, stream=None):
-    return _fn("pat_mx_matmul_grad")(_address(g), g_stride, int(transposed), _address(q_codes), _address(q_scales), rows,
+    return _c.pat_mx_matmul_grad(_address(g), g_stride, int(transposed), _address(q_codes), _address(q_scales), rows,
                                      inner, cols, _address(out), out_stride, pat._dtype(dtype), _address(workspace),
                                      workspace_bytes, pat._stream(stream))
 
 
 def pat_mx_matmul_grad_workspace(rows, inner, cols):
-    return _fn("pat_mx_matmul_grad_workspace")(rows, inner, cols)
+    return _c.pat_mx_matmul_grad_workspace(rows, inner, cols)
 
 
 def pat_embedding(tokens, token_bytes, ntokens, table, table_stride, table_dtype, first, rows, cols, scale, out,
                   out_stride, dtype, stream=None):
-    return _fn("pat_embedding")(_address(tokens), token_bytes, ntokens, _address(table), table_stride,
+    return _c.pat_embedding(_address(tokens), token_bytes, ntokens, _address(table), table_stride,
                                 pat._dtype(table_dtype), first, rows, cols, scale, _address(out), out_stride,
                                 pat._dtype(dtype), pat._stream(stream))
 
 
 def pat_embedding_grad(tokens, token_bytes, ntokens, g, g_stride, g_dtype, first, rows, cols, scale, out, out_stride,
                        dtype, workspace, workspace_bytes, stream=None):
-    return _fn("pat_embedding_grad")(_address(tokens), token_bytes, ntokens, _address(g), g_stride, pat._dtype(g_dtype),
+    return _c.pat_embedding_grad(_address(tokens), token_bytes, ntokens, _address(g), g_stride, pat._dtype(g_dtype),
                                      first, rows, cols, scale, _address(out), out_stride, pat._dtype(dtype),
                                      _address(workspace), workspace_bytes, pat._stream(stream))
 
 
 def pat_embedding_grad_workspace(ntokens, rows, cols):
-    return _fn("pat_embedding_grad_workspace")(ntokens, rows, cols)
+    return _c.pat_embedding_grad_workspace(ntokens, rows, cols)
 
 
 def pat_dropout(x, x_stride, residual, residual_stride, out, out_stride, rows, cols, dtype, p, seed, index, index_stride,
                 stream=None):
-    return _fn("pat_dropout")(_address(x), x_stride, _address(residual), residual_stride, _address(out), out_stride, rows,
+    return _c.pat_dropout(_address(x), x_stride, _address(residual), residual_stride, _address(out), out_stride, rows,
                               cols, pat._dtype(dtype), p, seed, index, index_stride, pat._stream(stream))
 
 
@@ -167,11 +171,15 @@ def _matrix(t, what, shape=None):
     """Checks a float matrix and returns its row stride."""
     if t.dim() != 2 or not t.is_cuda:
         raise ValueError(f"{what}: a 2-D GPU tensor")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{what}: shape {tuple(shape)} is needed, got {tuple(t.shape)}")
-    _float(t.dtype, what)
-    rows, cols = t.shape
+    size = t.shape
+    if shape is not None and size != shape:
+        raise ValueError(f"{what}: shape {tuple(shape)} is needed, got {tuple(size)}")
+    if t.dtype not in _CODE:
+        _float(t.dtype, what)
+    rows, cols = size
     stride, unit = t.stride()
+    if stride == cols and unit == 1:
+        return stride
     if rows and cols > 1 and unit != 1:
         raise ValueError(f"{what}: the elements of a row must be consecutive in memory")
     if rows > 1 and cols and stride < cols:
@@ -185,7 +193,7 @@ def _stored(q, what):
     groups = -(-cols // PAT_MX_GROUP)
     rows = codes.shape[0] if codes.dim() == 2 else -1
     for t, width, name in ((codes, 64 * groups, "codes"), (scales, 4 * groups, "scales")):
-        if not t.is_cuda or t.dtype != torch.uint8 or not t.is_contiguous() or tuple(t.shape) != (rows, width):
+        if not t.is_cuda or t.dtype != torch.uint8 or t.shape != (rows, width) or not t.is_contiguous():
             raise ValueError(f"{what}: {name} must be a contiguous uint8 GPU tensor of shape (rows, {width})")
     return rows
 
@@ -197,53 +205,70 @@ def _indices(t, what):
 
 
 def _on(stream, *tensors):
-    """The stream of a call whose tensors must all be on the current device."""
-    device = tensors[0].device
-    for t in tensors[1:]:
-        if t.device != device:
-            raise ValueError(f"all tensors must be on one device, got {device} and {t.device}")
-    return pat._tensor_call_stream(device, stream)
+    """The stream of a call, as an integer; all tensors must be on the current device."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError(f"all tensors must be on the current device, cuda:{device}, got {t.device}")
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
+    return pat._stream(stream)
 
 
-def _output(out, shape, dtype, device, what):
+# The current stream's handle without a Stream object, where this torch has it (a microsecond less per call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _empty(shape, dtype, like, stream):
+    """New memory for a call on `stream`: that stream's own (torch hands memory out again in the order of the stream
+    that it was allocated on), so that neither earlier nor later work on the current stream meets it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(pat._stream(stream), device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _output(out, rows, cols, dtype, like, stream, what):
+    """The output tensor and its row stride; a new one is on the device of `like`."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _empty((rows, cols), dtype, like, stream), cols
     if out.dtype != dtype:
         raise ValueError(f"{what}: out is {out.dtype}, not {dtype}")
-    return out
+    return out, _matrix(out, "out", (rows, cols))
 
 
-def _work(nbytes, device, stream):
-    """A workspace, or None.  On another stream than torch's current one, the caching allocator is told, so that
-    the memory is not handed out again before the call has run."""
+def _work(nbytes, like, stream):
+    """Address of a workspace and the tensor that holds it."""
     if not nbytes:
-        return None
-    w = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if isinstance(stream, torch.cuda.Stream) and stream != torch.cuda.current_stream(device):
-        w.record_stream(stream)
-    return w
+        return None, None
+    w = _empty(nbytes, torch.uint8, like, stream)
+    return w.data_ptr(), w
 
 
 def mx_quantize(x, out=None, stream=None):
     """4-bit blocks of a float32 or bfloat16 matrix, as an Mx."""
     stride = _matrix(x, "x")
     rows, cols = x.shape
-    q = mx_empty(rows, cols, x.device) if out is None else out
-    if _stored(q, "out") != rows or q.cols != cols:
+    if out is None:
+        groups = -(-cols // PAT_MX_GROUP)
+        out = Mx(_empty((rows, 64 * groups), torch.uint8, x, stream), _empty((rows, 4 * groups), torch.uint8, x, stream), cols)
+    elif _stored(out, "out") != rows or out.cols != cols:
         raise ValueError(f"out: an Mx of {rows} x {cols} is needed")
-    stream = _on(stream, x, q.codes, q.scales)
-    pat.check(pat_mx_quantize(x, stride, rows, cols, _CODE[x.dtype], q.codes, q.scales, stream), "pat_mx_quantize")
-    return q
+    codes, scales, _ = out
+    pat.check(_c.pat_mx_quantize(x.data_ptr(), stride, rows, cols, _CODE[x.dtype], codes.data_ptr(), scales.data_ptr(),
+                                 _on(stream, x, codes, scales)), "pat_mx_quantize")
+    return out
 
 
 def mx_dequantize(q, dtype=torch.bfloat16, out=None, stream=None):
     """The matrix that an Mx stands for, in `dtype` (exact)."""
-    rows = _stored(q, "q")
-    _float(dtype, "dtype")
-    out = _output(out, (rows, q.cols), dtype, q.codes.device, "mx_dequantize")
-    stride = _matrix(out, "out", (rows, q.cols))
-    stream = _on(stream, q.codes, q.scales, out)
-    pat.check(pat_mx_dequantize(q.codes, q.scales, rows, q.cols, out, stride, _CODE[dtype], stream), "pat_mx_dequantize")
+    rows, code = _stored(q, "q"), _float(dtype, "dtype")
+    codes, scales, cols = q
+    out, stride = _output(out, rows, cols, dtype, codes, stream, "mx_dequantize")
+    pat.check(_c.pat_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, code,
+                                   _on(stream, codes, scales, out)), "pat_mx_dequantize")
     return out
 
 
@@ -252,13 +277,13 @@ def mx_matmul(a, b, dtype=torch.bfloat16, out=None, stream=None):
     m, n, k = _stored(a, "a"), _stored(b, "b"), a.cols
     if b.cols != k:
         raise ValueError(f"a has {k} columns, b has {b.cols}")
-    _float(dtype, "dtype")
-    out = _output(out, (m, n), dtype, a.codes.device, "mx_matmul")
-    stride = _matrix(out, "out", (m, n))
-    stream = _on(stream, a.codes, a.scales, b.codes, b.scales, out)
-    need = pat_mx_matmul_workspace(m, n, k)
-    pat.check(pat_mx_matmul(a.codes, a.scales, b.codes, b.scales, m, n, k, out, stride, _CODE[dtype],
-                            _work(need, out.device, stream), need, stream), "pat_mx_matmul")
+    code = _float(dtype, "dtype")
+    out, stride = _output(out, m, n, dtype, a.codes, stream, "mx_matmul")
+    on = _on(stream, a.codes, a.scales, b.codes, b.scales, out)
+    need = _c.pat_mx_matmul_workspace(m, n, k)
+    work, hold = _work(need, out, stream)
+    pat.check(_c.pat_mx_matmul(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, k,
+                               out.data_ptr(), stride, code, work, need, on), "pat_mx_matmul")
     return out
 
 
@@ -266,16 +291,17 @@ def mx_linear(x, w, dtype=None, out=None, stream=None):
     """Q(x) w^T: the rows of x, quantised on the way, times an Mx; `dtype` is x's by default."""
     stride, n = _matrix(x, "x"), _stored(w, "w")
     m, k = x.shape
-    if w.cols != k:
-        raise ValueError(f"x has {k} columns, w has {w.cols}")
+    codes, scales, cols = w
+    if cols != k:
+        raise ValueError(f"x has {k} columns, w has {cols}")
     dtype = x.dtype if dtype is None else dtype
-    _float(dtype, "dtype")
-    out = _output(out, (m, n), dtype, x.device, "mx_linear")
-    out_stride = _matrix(out, "out", (m, n))
-    stream = _on(stream, x, w.codes, w.scales, out)
-    need = pat_mx_linear_workspace(m, n, k)
-    pat.check(pat_mx_linear(x, stride, _CODE[x.dtype], w.codes, w.scales, m, n, k, out, out_stride, _CODE[dtype],
-                            _work(need, out.device, stream), need, stream), "pat_mx_linear")
+    code = _float(dtype, "dtype")
+    out, out_stride = _output(out, m, n, dtype, x, stream, "mx_linear")
+    on = _on(stream, x, codes, scales, out)
+    need = _c.pat_mx_linear_workspace(m, n, k)
+    work, hold = _work(need, out, stream)
+    pat.check(_c.pat_mx_linear(x.data_ptr(), stride, _CODE[x.dtype], codes.data_ptr(), scales.data_ptr(), m, n, k,
+                               out.data_ptr(), out_stride, code, work, need, on), "pat_mx_linear")
     return out
 
 
@@ -285,16 +311,17 @@ def mx_matmul_grad(g, q, dtype=torch.bfloat16, transposed=False, out=None, strea
     stride, inner = _matrix(g, "g"), _stored(q, "q")
     if g.dtype != torch.bfloat16:
         raise ValueError(f"g: bfloat16, got {g.dtype}")
+    codes, scales, cols = q
     rows = g.shape[1 if transposed else 0]
     if g.shape[0 if transposed else 1] != inner:
         raise ValueError(f"g: {tuple(g.shape)} does not match q's {inner} rows")
-    _float(dtype, "dtype")
-    out = _output(out, (rows, q.cols), dtype, g.device, "mx_matmul_grad")
-    out_stride = _matrix(out, "out", (rows, q.cols))
-    stream = _on(stream, g, q.codes, q.scales, out)
-    need = pat_mx_matmul_grad_workspace(rows, inner, q.cols)
-    pat.check(pat_mx_matmul_grad(g, stride, transposed, q.codes, q.scales, rows, inner, q.cols, out, out_stride,
-                                 _CODE[dtype], _work(need, out.device, stream), need, stream), "pat_mx_matmul_grad")
+    code = _float(dtype, "dtype")
+    out, out_stride = _output(out, rows, cols, dtype, g, stream, "mx_matmul_grad")
+    on = _on(stream, g, codes, scales, out)
+    need = _c.pat_mx_matmul_grad_workspace(rows, inner, cols)
+    work, hold = _work(need, out, stream)
+    pat.check(_c.pat_mx_matmul_grad(g.data_ptr(), stride, transposed, codes.data_ptr(), scales.data_ptr(), rows, inner,
+                                    cols, out.data_ptr(), out_stride, code, work, need, on), "pat_mx_matmul_grad")
     return out
 
 
@@ -304,13 +331,10 @@ def embedding(tokens, table, scale=1.0, first=0, dtype=None, out=None, stream=No
     size, stride = _indices(tokens, "tokens"), _matrix(table, "table")
     rows, cols = table.shape
     dtype = table.dtype if dtype is None else dtype
-    _float(dtype, "dtype")
-    n = tokens.numel()
-    out = _output(out, (n, cols), dtype, table.device, "embedding")
-    out_stride = _matrix(out, "out", (n, cols))
-    stream = _on(stream, tokens, table, out)
-    pat.check(pat_embedding(tokens, size, n, table, stride, _CODE[table.dtype], first, rows, cols, scale, out, out_stride,
-                            _CODE[dtype], stream), "pat_embedding")
+    code, n = _float(dtype, "dtype"), tokens.shape[0]
+    out, out_stride = _output(out, n, cols, dtype, table, stream, "embedding")
+    pat.check(_c.pat_embedding(tokens.data_ptr(), size, n, table.data_ptr(), stride, _CODE[table.dtype], first, rows, cols,
+                               scale, out.data_ptr(), out_stride, code, _on(stream, tokens, table, out)), "pat_embedding")
     return out
 
 
@@ -318,16 +342,16 @@ def embedding_grad(tokens, g, rows, scale=1.0, first=0, dtype=None, out=None, st
     """The gradient of ``embedding`` with respect to a table of `rows` rows, dense; `dtype` is g's by default."""
     size, stride = _indices(tokens, "tokens"), _matrix(g, "g")
     n, cols = g.shape
-    if tokens.numel() != n:
-        raise ValueError(f"g has {n} rows for {tokens.numel()} tokens")
+    if tokens.shape[0] != n:
+        raise ValueError(f"g has {n} rows for {tokens.shape[0]} tokens")
     dtype = g.dtype if dtype is None else dtype
-    _float(dtype, "dtype")
-    out = _output(out, (rows, cols), dtype, g.device, "embedding_grad")
-    out_stride = _matrix(out, "out", (rows, cols))
-    stream = _on(stream, tokens, g, out)
-    need = pat_embedding_grad_workspace(n, rows, cols)
-    pat.check(pat_embedding_grad(tokens, size, n, g, stride, _CODE[g.dtype], first, rows, cols, scale, out, out_stride,
-                                 _CODE[dtype], _work(need, out.device, stream), need, stream), "pat_embedding_grad")
+    code = _float(dtype, "dtype")
+    out, out_stride = _output(out, rows, cols, dtype, g, stream, "embedding_grad")
+    on = _on(stream, tokens, g, out)
+    need = _c.pat_embedding_grad_workspace(n, rows, cols)
+    work, hold = _work(need, out, stream)
+    pat.check(_c.pat_embedding_grad(tokens.data_ptr(), size, n, g.data_ptr(), stride, _CODE[g.dtype], first, rows, cols,
+                                    scale, out.data_ptr(), out_stride, code, work, need, on), "pat_embedding_grad")
     return out
 
 
@@ -338,15 +362,15 @@ def dropout(x, p, seed, index=0, index_stride=None, residual=None, out=None, str
     call on the output's gradient.  `out` may be x or the residual."""
     stride = _matrix(x, "x")
     rows, cols = x.shape
-    out = _output(out, x.shape, x.dtype, x.device, "dropout")
-    out_stride = _matrix(out, "out", x.shape)
-    tensors, residual_stride = [x, out], 0
+    out, out_stride = _output(out, rows, cols, x.dtype, x, stream, "dropout")
+    address, residual_stride = None, 0
     if residual is not None:
         residual_stride = _matrix(residual, "residual", x.shape)
         if residual.dtype != x.dtype:
             raise ValueError(f"residual is {residual.dtype}, x is {x.dtype}")
-        tensors.append(residual)
-    stream = _on(stream, *tensors)
-    pat.check(pat_dropout(x, stride, residual, residual_stride, out, out_stride, rows, cols, _CODE[x.dtype], p, seed, index,
-                          cols if index_stride is None else index_stride, stream), "pat_dropout")
+        address = residual.data_ptr()
+    on = _on(stream, x, out) if residual is None else _on(stream, x, out, residual)
+    pat.check(_c.pat_dropout(x.data_ptr(), stride, address, residual_stride, out.data_ptr(), out_stride, rows, cols,
+                             _CODE[x.dtype], p, seed, index, cols if index_stride is None else index_stride, on),
+              "pat_dropout")
     return out

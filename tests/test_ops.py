@@ -606,6 +606,31 @@ def test_graph_replays_and_other_streams(name):
 
 
 @gpu
+@pytest.mark.parametrize("name", ["quantize", "dequantize", "linear", "grad", "embedding_grad", "dropout"])
+def test_memory_of_a_call_on_another_stream(name):
+    """Outputs and workspaces of a call on a given stream are not memory that work queued on the current stream still
+    writes: a tensor that a delayed fill goes to is freed before the call."""
+    x, w = values((20, 300), 1, B16), values((70, 300), 2)
+    g, tokens, q = values((20, 70), 3, B16), torch.arange(20, device="cuda") * 7 % 13, ops.mx_quantize(w)
+    call = {"quantize": lambda s: ops.mx_quantize(w, stream=s).codes, "dequantize": lambda s: ops.mx_dequantize(q, F32, stream=s),
+            "linear": lambda s: ops.mx_linear(x, q, F32, stream=s),
+            "grad": lambda s: ops.mx_matmul_grad(g, q, F32, stream=s),
+            "embedding_grad": lambda s: ops.embedding_grad(tokens, x, 13, dtype=F32, stream=s),
+            "dropout": lambda s: ops.dropout(w, 0.2, 3, stream=s)}[name]
+    want, side = call(None), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for handle in (side, side.cuda_stream):
+        torch.cuda._sleep(20_000_000)
+        late = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (512, 4480, 6000, 15600, 24000, 84000, 200000)]
+        for t in late:
+            t.fill_(0x77)
+        del late, t
+        got = call(handle)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+@gpu
 def test_offsets_beyond_32_bits():
     """Tables, gradients and outputs whose byte and element offsets pass 2^32: rows spread over 10 GiB."""
     pitch, rows, cols = 1 << 30, 5, 40
