@@ -24,31 +24,38 @@ __device__ __forceinline__ v8i frag(v4i c) { return v8i{c[0], c[1], c[2], c[3], 
 
 // ---- tiles through LDS ---------------------------------------------------------------------------------------
 //
-// A workgroup of 2 x 2 waves computes a tile of 2 * 32 * F rows and columns, a wave F x F blocks of 32 x 32.  It goes
+// A workgroup of WA x WB waves computes a tile of R x R of the output, a wave FA x FB blocks of 32 x 32.  It goes
 // through the columns 256 at a time (two groups, 128 bytes of codes a row).  The next 256 columns of both sides are
 // on their way into the other half of LDS, written there by the loads themselves, while these are multiplied.
 //
-// LDS holds a row's eight 16-byte blocks of codes at place block ^ (row mod 8), so that lanes reading one block of
-// consecutive rows hit different banks; the loads write lane after lane, so each lane fetches the block that
-// belongs at its place.  An instruction of 32 x 32 x 64 takes two blocks of 32 rows: lane l has row l mod 32 and one
-// block, and any two blocks will do as long as both sides take the same.  Lane half h takes blocks 2h and 2h + 1 of a
-// group in turn, whose scales are two neighbouring bytes: the instruction picks the byte.
+// LDS holds a row's eight 16-byte blocks of codes at place block ^ (row / 2 mod 8): a row is half of the 64 banks, so
+// 16 lanes that read one block of consecutive rows hit all banks once.  The loads write lane after lane, so each lane
+// fetches the block that belongs at its place.  An instruction of 32 x 32 x 64 takes two blocks of 32 rows: lane l has
+// row l mod 32 and one block, and any two blocks will do as long as both sides take the same.  Lane half h takes blocks
+// 2h and 2h + 1 of a group in turn, whose scales are two neighbouring bytes: the instruction picks the byte.
+//
+// 256 x 256 takes eight waves, two a SIMD: the loads issue in order with the multiplications, 64 cycles apiece when
+// all waves issue them after a barrier, and a second wave multiplies meanwhile (with four waves of 128 x 128 the loads
+// added 75 us to an 8192^3 product whose multiplications take 154).
 
-constexpr int kTileThreads = 256;
-
-template <int F>
-struct TileLds {
-  static constexpr int kRows = 64 * F;
-  uint8_t codes[2][kRows * 128];  // [a, b]
-  uint8_t scales[2][kRows * 8];
+template <int FA, int FB, int WA, int WB>
+struct Tile {
+  static constexpr int kWaves = WA * WB, R = 32 * FA * WA;
+  static_assert(R == 32 * FB * WB, "square");
+  struct Lds {
+    uint8_t codes[2][R * 128];  // [a, b]
+    uint8_t scales[2][R * 8];
+  };
 };
 
-template <int F, typename T>
-__global__ __launch_bounds__(kTileThreads, F == 4 ? 1 : 2) void tile_kernel(MxMat a, MxMat b, int64_t m, int64_t n,
-                                                                             int groups, MatOut out) {
-  constexpr int R = 64 * F;
-  __shared__ __attribute__((aligned(16))) TileLds<F> lds0;
-  __shared__ __attribute__((aligned(16))) TileLds<F> lds1;
+template <int FA, int FB, int WA, int WB, typename T>
+__global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b, int64_t m, int64_t n, int groups,
+                                                               MatOut out) {
+  typedef Tile<FA, FB, WA, WB> S;
+  typedef typename S::Lds Lds;
+  constexpr int R = S::R, W = S::kWaves;
+  __shared__ __attribute__((aligned(16))) Lds lds0;
+  __shared__ __attribute__((aligned(16))) Lds lds1;
   TilePlace place;
   if (!tile_place((m + R - 1) / R, (n + R - 1) / R, &place)) return;
   const int64_t i0 = place.i * R, j0 = place.j * R;
@@ -57,113 +64,163 @@ __global__ __launch_bounds__(kTileThreads, F == 4 ? 1 : 2) void tile_kernel(MxMa
 
   // Rows beyond a matrix are its last row again; what they give is not stored.
   const int rows_a = (int)min((int64_t)R, m - i0), rows_b = (int)min((int64_t)R, n - j0);
-  uint32_t at_a[F * 2], at_b[F * 2];  // of this lane's block, in the rows' codes
-  const int block = lane % 8 ^ lane / 8;
+  constexpr int LOADS = R / 8 / W;  // of codes, 8 rows each, a wave
+  uint32_t at_a[LOADS], at_b[LOADS];  // of this lane's block, in the rows' codes
+  const int block = (lane ^ (wave * 8 + lane / 8) / 2) % 8;
 #pragma unroll
-  for (int u = 0; u < F * 2; ++u) {
-    const int row = (u * 4 + wave) * 8 + lane / 8;
+  for (int u = 0; u < LOADS; ++u) {
+    const int row = (u * W + wave) * 8 + lane / 8;
     at_a[u] = (uint32_t)min(row, rows_a - 1) * pitch + block * 16;
     at_b[u] = (uint32_t)min(row, rows_b - 1) * pitch + block * 16;
   }
-  constexpr int SU = (F + 1) / 2;  // loads of scales: 32 rows of 8 bytes a wave
-  uint32_t sat_a[SU], sat_b[SU];
-#pragma unroll
-  for (int u = 0; u < SU; ++u) {
-    const int row = (u * 4 + wave) * 32 + lane / 2;
-    sat_a[u] = (uint32_t)min(row, rows_a - 1) * spitch + lane % 2 * 4;
-    sat_b[u] = (uint32_t)min(row, rows_b - 1) * spitch + lane % 2 * 4;
-  }
+  constexpr bool SCALES_OF_ALL = R / 32 >= W;  // a wave loads the scales of 32 rows; small tiles have fewer than waves
+  static_assert(R / 32 <= W, "");
+  const int srow = wave * 32 + lane / 2;
+  const uint32_t sat_a = (uint32_t)min(srow, rows_a - 1) * spitch + lane % 2 * 4;
+  const uint32_t sat_b = (uint32_t)min(srow, rows_b - 1) * spitch + lane % 2 * 4;
   const uint8_t *codes_a = a.codes + i0 * pitch, *codes_b = b.codes + j0 * pitch;
   const uint8_t *scales_a = a.scales + i0 * spitch, *scales_b = b.scales + j0 * spitch;
 
-  auto fetch = [&](TileLds<F>& l, int g) {
+  auto fetch = [&](Lds& l, int g) {
     // the second group of the last 256 columns may not exist: the first again, not multiplied
     const uint32_t back = g + 1 < groups ? 0 : (block >= 4 ? 64 : 0), sback = g + 1 < groups ? 0 : lane % 2 * 4;
     const uint8_t *pa = codes_a + (int64_t)g * 64, *pb = codes_b + (int64_t)g * 64;
 #pragma unroll
-    for (int u = 0; u < F * 2; ++u) {
-      __builtin_amdgcn_global_load_lds((GlobalWords)(pa + (at_a[u] - back)), (LdsWords)(l.codes[0] + (u * 4 + wave) * 1024),
+    for (int u = 0; u < LOADS; ++u) {
+      __builtin_amdgcn_global_load_lds((GlobalWords)(pa + (at_a[u] - back)), (LdsWords)(l.codes[0] + (u * W + wave) * 1024),
                                        16, 0, 0);
-      __builtin_amdgcn_global_load_lds((GlobalWords)(pb + (at_b[u] - back)), (LdsWords)(l.codes[1] + (u * 4 + wave) * 1024),
+      __builtin_amdgcn_global_load_lds((GlobalWords)(pb + (at_b[u] - back)), (LdsWords)(l.codes[1] + (u * W + wave) * 1024),
                                        16, 0, 0);
     }
-    const uint8_t *qa = scales_a + (int64_t)g * 4, *qb = scales_b + (int64_t)g * 4;
-#pragma unroll
-    for (int u = 0; u < SU; ++u) {
-      if ((u * 4 + wave) * 32 >= R) continue;
-      __builtin_amdgcn_global_load_lds((GlobalWords)(qa + (sat_a[u] - sback)), (LdsWords)(l.scales[0] + (u * 4 + wave) * 256),
-                                       4, 0, 0);
-      __builtin_amdgcn_global_load_lds((GlobalWords)(qb + (sat_b[u] - sback)), (LdsWords)(l.scales[1] + (u * 4 + wave) * 256),
-                                       4, 0, 0);
+    if (SCALES_OF_ALL || wave < R / 32) {
+      const uint8_t *qa = scales_a + (int64_t)g * 4, *qb = scales_b + (int64_t)g * 4;
+      __builtin_amdgcn_global_load_lds((GlobalWords)(qa + (sat_a - sback)), (LdsWords)(l.scales[0] + wave * 256), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((GlobalWords)(qb + (sat_b - sback)), (LdsWords)(l.scales[1] + wave * 256), 4, 0, 0);
     }
   };
 
-  const int row_a = wave / 2 * 32 * F + lane % 32, row_b = wave % 2 * 32 * F + lane % 32, half = lane / 32;
-  v16f acc[F][F];
+  const int half = lane / 32, wave_row = wave / WB * 32 * FA, wave_col = wave % WB * 32 * FB;
+  const int row_a = wave_row + lane % 32, row_b = wave_col + lane % 32;
+  v16f acc[FA][FB];
 #pragma unroll
-  for (int x = 0; x < F; ++x)
+  for (int x = 0; x < FA; ++x)
 #pragma unroll
-    for (int y = 0; y < F; ++y)
+    for (int y = 0; y < FB; ++y)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
 
-  auto multiply = [&](const TileLds<F>& l, int g) {
-    v2u sa[F], sb[F];
+  // A step is one block of every row: FA x FB instructions.  What the next step multiplies is read from LDS while these
+  // run, from one register set into the other.
+  struct Blocks {
+    v4i a[FA], b[FB];
+  };
+  struct Scales {
+    v2u a[FA], b[FB];
+  };
+  auto read_scales = [&](const Lds& l, Scales& s) {
 #pragma unroll
-    for (int x = 0; x < F; ++x) {
-      sa[x] = *(const v2u*)(l.scales[0] + (row_a + 32 * x) * 8);
-      sb[x] = *(const v2u*)(l.scales[1] + (row_b + 32 * x) * 8);
-    }
-    auto group = [&](int e) {
-      int fa[F], fb[F];
+    for (int x = 0; x < FA; ++x) s.a[x] = *(const v2u*)(l.scales[0] + (row_a + 32 * x) * 8);
 #pragma unroll
-      for (int x = 0; x < F; ++x) fa[x] = sa[x][e] >> (16 * half), fb[x] = sb[x][e] >> (16 * half);
-      auto step = [&](auto which) {
-        constexpr int J = decltype(which)::value;
-        const int at = ((e * 4 + half * 2 + J) ^ (lane & 7)) * 16;
-        v4i ca[F], cb[F];
+    for (int y = 0; y < FB; ++y) s.b[y] = *(const v2u*)(l.scales[1] + (row_b + 32 * y) * 8);
+  };
+  auto read = [&](const Lds& l, int step, Blocks& c) {  // step: 2 * group + which of the half's two blocks
+    const int at = ((step / 2 * 4 + half * 2 + step % 2) ^ (lane >> 1 & 7)) * 16;
 #pragma unroll
-        for (int x = 0; x < F; ++x) {
-          ca[x] = *(const v4i*)(l.codes[0] + (row_a + 32 * x) * 128 + at);
-          cb[x] = *(const v4i*)(l.codes[1] + (row_b + 32 * x) * 128 + at);
-        }
+    for (int x = 0; x < FA; ++x) c.a[x] = *(const v4i*)(l.codes[0] + (row_a + 32 * x) * 128 + at);
 #pragma unroll
-        for (int x = 0; x < F; ++x)
+    for (int y = 0; y < FB; ++y) c.b[y] = *(const v4i*)(l.codes[1] + (row_b + 32 * y) * 128 + at);
+  };
+  auto multiply = [&](const Blocks& c, const Scales& s, auto which) {
+    constexpr int STEP = decltype(which)::value, J = STEP % 2;
+    int fa[FA], fb[FB];
 #pragma unroll
-          for (int y = 0; y < F; ++y)
-            acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(ca[x]), frag(cb[y]), acc[x][y], 4, 4, J, fa[x], J,
-                                                                       fb[y]);
-      };
-      step(Int<0>{});
-      step(Int<1>{});
-    };
-    group(0);
-    if (g + 1 < groups) group(1);
+    for (int x = 0; x < FA; ++x) fa[x] = s.a[x][STEP / 2] >> (16 * half);
+#pragma unroll
+    for (int y = 0; y < FB; ++y) fb[y] = s.b[y][STEP / 2] >> (16 * half);
+#pragma unroll
+    for (int x = 0; x < FA; ++x)
+#pragma unroll
+      for (int y = 0; y < FB; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(c.a[x]), frag(c.b[y]), acc[x][y], 4, 4, J, fa[x], J,
+                                                                   fb[y]);
+    // a step's instructions stay together: moved over each other, all steps' blocks would be in registers at once
+    __builtin_amdgcn_sched_barrier(0);
   };
 
-  fetch(lds0, 0);
-  for (int g = 0; g < groups; g += 4) {
-    __syncthreads();  // these columns have arrived, and nobody reads the other half any more
-    if (g + 2 < groups) fetch(lds1, g + 2);
-    multiply(lds0, g);
-    if (g + 2 >= groups) break;
+  const int tiles = (groups + 1) / 2, pairs = groups / 4;  // 256 columns each; whole ones, two by two
+  Blocks c0, c1;
+  Scales s0, s1;
+  // Tile t out of `l`; the first step's blocks are in c0 and the scales in `s`.  Before the last step's
+  // multiplications the next tile has arrived and this half of LDS has been read by all, so both the next first
+  // step and the tile after the next come in under them.  No branch: beyond the last tile it is fetched again.
+  auto columns = [&](Lds& l, Lds& next, const Scales& s, Scales& s_next, int t) {
+    read(l, 1, c1);
+    multiply(c0, s, Int<0>{});
+    read(l, 2, c0);
+    multiply(c1, s, Int<1>{});
+    read(l, 3, c1);
+    multiply(c0, s, Int<2>{});
     __syncthreads();
-    if (g + 4 < groups) fetch(lds0, g + 4);
-    multiply(lds1, g + 2);
+    read_scales(next, s_next);
+    read(next, 0, c0);
+    fetch(l, 2 * min(t + 2, tiles - 1));
+    multiply(c1, s, Int<3>{});
+  };
+  fetch(lds0, 0);
+  __syncthreads();
+  fetch(lds1, 2 * min(1, tiles - 1));
+  read_scales(lds0, s0);
+  read(lds0, 0, c0);
+  for (int p = 0; p < pairs; ++p) {
+    columns(lds0, lds1, s0, s1, 2 * p);
+    columns(lds1, lds0, s1, s0, 2 * p + 1);
+  }
+  // up to three groups are left, in both halves
+  if (groups % 4) {
+    read(lds0, 1, c1);
+    multiply(c0, s0, Int<0>{});
+    multiply(c1, s0, Int<1>{});
+    if (groups % 4 >= 2) {
+      read(lds0, 2, c0);
+      read(lds0, 3, c1);
+      multiply(c0, s0, Int<2>{});
+      multiply(c1, s0, Int<3>{});
+    }
+    if (groups % 4 == 3) {
+      __syncthreads();
+      read_scales(lds1, s1);
+      read(lds1, 0, c0);
+      read(lds1, 1, c1);
+      multiply(c0, s1, Int<0>{});
+      multiply(c1, s1, Int<1>{});
+    }
   }
 
-  // Lane l has column l mod 32 of a block and rows 8 * (e / 4) + 4 * (l / 32) + e mod 4.
+  // Lane l has column l mod 32 of a block and rows 8 * (e / 4) + 4 * (l / 32) + e mod 4.  A wave turns 32 rows at a
+  // time round in its own part of LDS and writes them as vectors.
+  __syncthreads();
+  constexpr int C = 32 * FB, P = C + 8;  // a wave's columns; its rows 8 banks apart, for the halves' rows of 4 apart
+  static_assert(W / 2 * 32 * P * 4 <= sizeof(Lds), "");
+  float* part = (float*)(wave < W / 2 ? &lds0 : &lds1) + wave % (W / 2) * 32 * P;
 #pragma unroll
-  for (int x = 0; x < F; ++x) {
+  for (int x = 0; x < FA; ++x) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int row = wave / 2 * 32 * F + 32 * x + 8 * (e / 4) + 4 * half + e % 4;
-      if (row >= rows_a) continue;
-      char* p = (char*)out.p + ((i0 + row) * out.stride + j0) * T::kBytes;
+    for (int y = 0; y < FB; ++y)
 #pragma unroll
-      for (int y = 0; y < F; ++y)
-        if (row_b + 32 * y < rows_b) T::store(p, row_b + 32 * y, acc[x][y][e]);
+      for (int e = 0; e < 16; ++e) part[(8 * (e / 4) + 4 * half + e % 4) * P + 32 * y + lane % 32] = acc[x][y][e];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    constexpr int LANES = C / 8;  // lanes a row, 8 columns each
+#pragma unroll
+    for (int u = 0; u < 32 * LANES / 64; ++u) {
+      const int r = u * (64 / LANES) + lane / LANES, c = lane % LANES * 8, row = wave_row + 32 * x + r;
+      const v4f lo = *(const v4f*)(part + r * P + c), hi = *(const v4f*)(part + r * P + c + 4);
+      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      const int left = rows_b - wave_col - c;
+      char* p = (char*)out.p + ((i0 + row) * out.stride + j0 + wave_col + c) * T::kBytes;
+      if (row < rows_a && left >= 8) store8<T, false, false, true>(p, 8, 4, v);
+      else if (row < rows_a && left > 0) store8<T, false, false, false>(p, left, 4, v);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
 }
 
@@ -308,11 +365,12 @@ hipError_t pick_split(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, 
   return run_split<4, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
 }
 
-template <int F>
+template <int FA, int FB, int WA, int WB>
 hipError_t run_tile(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
-  const size_t tiles = ceil_div(m, 64 * F) * ceil_div(n, 64 * F);
-  const auto kernel = dtype == Elem::f32 ? tile_kernel<F, F32> : tile_kernel<F, B16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(kTileThreads), 0, stream, a, b, m, n,
+  constexpr int R = Tile<FA, FB, WA, WB>::R;
+  const size_t tiles = ceil_div(m, R) * ceil_div(n, R);
+  const auto kernel = dtype == Elem::f32 ? tile_kernel<FA, FB, WA, WB, F32> : tile_kernel<FA, FB, WA, WB, B16>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(64 * WA * WB), 0, stream, a, b, m, n,
                      (int)groups_of(k), out);
   return hipGetLastError();
 }
@@ -329,9 +387,9 @@ hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, M
   auto wgs = [&](int f) { return ceil_div(m, 64 * f) * ceil_div(n, 64 * f); };
   int pick = 0;
   if (m > 64 && n > 64 && k > 0) pick = wgs(4) >= 192 ? 4 : wgs(2) >= 192 ? 2 : wgs(1) >= 128 ? 1 : 0;
-  if (pick == 4) return run_tile<4>(a, b, m, n, k, out, dtype, stream);
-  if (pick == 2) return run_tile<2>(a, b, m, n, k, out, dtype, stream);
-  if (pick == 1) return run_tile<1>(a, b, m, n, k, out, dtype, stream);
+  if (pick == 4) return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
+  if (pick == 2) return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
+  if (pick == 1) return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
   return pick_split<false, F32>(a, {}, b, m, n, k, out, dtype, stream);
 }
 
