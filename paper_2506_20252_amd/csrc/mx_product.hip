@@ -237,7 +237,7 @@ constexpr int kSplitWaves = 8;
 
 template <int MT, int NT, bool FUSED, typename X, typename T>
 __global__ __launch_bounds__(64 * kSplitWaves) void split_kernel(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k,
-                                                                  int groups, MatOut out) {
+                                                                  int groups, Divisor per_row, MatOut out) {
   extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int64_t tiles_n = (n + 16 * NT - 1) / (16 * NT);
@@ -260,26 +260,26 @@ __global__ __launch_bounds__(64 * kSplitWaves) void split_kernel(MxMat a, Mat x,
     qb[y] = b.scales + j * (pitch / 16);
   }
 
-  if constexpr (FUSED) {
-    const int blocks = groups * 4;
-    for (int i = threadIdx.x; i < (int)m * blocks; i += 64 * kSplitWaves) {
-      const int r = i / blocks, c = i % blocks * 32;
-      const char* p = (const char*)x.p + (r * x.stride + c) * X::kBytes;
-      float v[32];
+  if constexpr (FUSED) {  // as quantize_kernel does it: 8 values a lane, 4 lanes a block, 16 a group
+    constexpr int U = 2, T512 = 64 * kSplitWaves;
+    const int total = (int)m * groups * 16, sub = threadIdx.x % 16;
+    for (int base = 0; base < total; base += T512 * U) {
+      Raw8<X> r[U];
+      int row[U], c[U];
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float part[8];
-        if (k - c >= 8 * w + 8) load8<X, false, false, true>(p + 8 * w * X::kBytes, 8, 4, part);
-        else load8<X, false, false, false>(p + 8 * w * X::kBytes, k - c - 8 * w, 4, part);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[8 * w + e] = part[e];
+      for (int u = 0; u < U; ++u) {
+        const uint32_t i = min(base + u * T512 + (int)threadIdx.x, total - 1), q = per_row.divide(i);
+        row[u] = q;
+        c[u] = (i - q * per_row.d) * 8;
+        r[u] = load_raw8<X>((const char*)x.p + (row[u] * x.stride + c[u]) * X::kBytes, k - c[u]);
       }
-      uint32_t high = 0;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) high = max(high, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-      const uint32_t s = mx_scale_byte(high);
-      *(v4u*)(lds + r * lds_pitch + c / 2) = mx_codes(v, s);
-      lds_scales[r * blocks + c / 32] = (uint8_t)s;
+      for (int u = 0; u < U; ++u) {
+        const uint32_t s = mx_scale_byte(max_of_4(high_bits(r[u])));
+        if (base + u * T512 + (int)threadIdx.x >= total) continue;  // whole groups of 16 lanes
+        *(uint32_t*)(lds + row[u] * lds_pitch + c[u] / 2) = mx_codes(r[u], s);
+        if (sub % 4 == 0) lds_scales[row[u] * groups * 4 + c[u] / 32] = (uint8_t)s;
+      }
     }
     __syncthreads();
   }
@@ -354,15 +354,26 @@ hipError_t run_split(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, M
   const size_t sums = (size_t)kSplitWaves * MT * NT * 1024, rows = FUSED ? (size_t)m * (groups * 68 + 16) : 0;
   const dim3 grid((unsigned)(ceil_div(m, 16 * MT) * ceil_div(n, 16 * NT))), block(64 * kSplitWaves);
   const auto kernel = dtype == Elem::f32 ? split_kernel<MT, NT, FUSED, X, F32> : split_kernel<MT, NT, FUSED, X, B16>;
-  hipLaunchKernelGGL(kernel, grid, block, std::max(sums, rows), stream, a, x, b, m, n, k, groups, out);
+  hipLaunchKernelGGL(kernel, grid, block, std::max(sums, rows), stream, a, x, b, m, n, k, groups,
+                     Divisor((uint32_t)std::max(groups, 1) * 16), out);
   return hipGetLastError();
+}
+
+template <int MT, bool FUSED, typename X>
+hipError_t pick_columns(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
+  // As many columns a workgroup as leave one for each of the 256 CUs: the rows of a are read and quantised once per
+  // workgroup.  us at 24 rows with 16, 32, 64 columns: 8.2, 9.2, 11.9 (n = k = 4096), 18, 14.6, 19 (8192), 18, 14.5, 13
+  // (n = 16384, k = 4096).
+  if (n <= 16 * 256) return run_split<MT, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  if (n <= 32 * 256) return run_split<MT, 2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  return run_split<MT, 4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
 }
 
 template <bool FUSED, typename X>
 hipError_t pick_split(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
-  if (m <= 16) return run_split<1, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  if (m <= 32) return run_split<2, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  return run_split<4, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  if (m <= 16) return pick_columns<1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  if (m <= 32) return pick_columns<2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  return pick_columns<4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
 }
 
 template <int FA, int FB, int WA, int WB>
@@ -375,8 +386,10 @@ hipError_t run_tile(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut ou
   return hipGetLastError();
 }
 
-// Rows that the fused form quantises in every workgroup: what 64 KB of LDS hold.
-bool fused_fits(int64_t m, int64_t k) { return m <= 64 && m * (groups_of(k) * 68 + 16) <= 64 << 10; }
+// Rows that every workgroup quantises for itself, and not a launch before: m * k up to 32768 values (us fused and not,
+// k = 4096: 4.5 and 5.8 for one row, 5.1 and 6.6 for 4, 8.6 and 7.3 for 16; k = 8192: 8.1 and 10.7, 10.4 and 11.6,
+// none and 12.6).  What they take in LDS stays below 32 KB.
+bool fused(int64_t m, int64_t k) { return m <= 64 && m * k <= 32768; }
 
 }  // namespace
 
@@ -384,21 +397,25 @@ size_t mx_matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
 
 hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, void*,
                             hipStream_t stream) {
-  auto wgs = [&](int f) { return ceil_div(m, 64 * f) * ceil_div(n, 64 * f); };
-  int pick = 0;
-  if (m > 64 && n > 64 && k > 0) pick = wgs(4) >= 192 ? 4 : wgs(2) >= 192 ? 2 : wgs(1) >= 128 ? 1 : 0;
-  if (pick == 4) return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
-  if (pick == 2) return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
-  if (pick == 1) return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
+  // The largest tile that gives more than half of the 256 CUs one.  A tile's time grows with its area only once the chip
+  // is full; us with tiles of 64, 128, 256 at n = k = 8192: 24, 30, 51 for m = 256 (512, 128, 32 tiles), 48, 32, 51 for
+  // m = 512, 85, 52, 54 for m = 1024, 161, 96, 72 for m = 2048.  Up to 48 rows or columns the split is as fast or
+  // faster (n = 8192: 19 against 20; n = k = 1024: 5 against 6).
+  auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, size); };
+  if (k > 0 && m > 48 && n > 48) {
+    if (tiles(256) > 128) return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
+    if (tiles(128) > 128) return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
+    return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
+  }
   return pick_split<false, F32>(a, {}, b, m, n, k, out, dtype, stream);
 }
 
 // Workspace of a linear that does not quantise on its way: the quantised rows, codes before scales.
-size_t mx_linear_workspace(int64_t m, int64_t, int64_t k) { return fused_fits(m, k) ? 0 : (size_t)(m * groups_of(k)) * 68; }
+size_t mx_linear_workspace(int64_t m, int64_t, int64_t k) { return fused(m, k) ? 0 : (size_t)(m * groups_of(k)) * 68; }
 
 hipError_t launch_mx_linear(Mat x, Elem x_dtype, MxMat w, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype,
                             void* workspace, hipStream_t stream) {
-  if (fused_fits(m, k)) {
+  if (fused(m, k)) {
     return x_dtype == Elem::f32 ? pick_split<true, F32>({}, x, w, m, n, k, out, dtype, stream)
                                 : pick_split<true, B16>({}, x, w, m, n, k, out, dtype, stream);
   }
