@@ -52,19 +52,17 @@ __global__ __launch_bounds__(256) void dequantize_kernel(MxMat q, uint32_t total
       const int64_t c = (int64_t)(g - row * groups.d) * 128 + sub * VALUES, left = cols - c;
       if (g >= total || left <= 0) continue;
       const uint32_t s = four[u] >> (sub * VALUES / 32 * 8) & 255u;
-      const float scale = mx_scale_value(s);
+      const float scale = mx_scale_operand(s);
       v4u v;
       if constexpr (VALUES == 8) {
         v[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], scale, 0));
         v[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], scale, 1));
         v[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], scale, 2));
         v[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[u], scale, 3));
-        if (s == 255u) v = v4u{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
       } else {
         const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], scale, 0);
         const v2f b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[u], scale, 1);
         v = __builtin_bit_cast(v4u, v4f{a[0], a[1], b[0], b[1]});
-        if (s == 255u) v = v4u{0x7FC00000u, 0x7FC00000u, 0x7FC00000u, 0x7FC00000u};
       }
       char* p = (char*)out.p + ((int64_t)row * out.stride + c) * T::kBytes;
       if (left >= VALUES) {

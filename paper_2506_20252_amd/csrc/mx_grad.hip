@@ -2,37 +2,48 @@
 // gradients of the 4-bit product.
 //
 // The sum runs over rows of q, across its blocks, so q is widened to bfloat16 (exactly) and multiplied by the bfloat16
-// matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane: a lane reads an
-// 8 x 8 patch of q (a word of codes from each of 8 rows), widens it and writes it to LDS turned round, one column of
-// 8 values at a time; likewise g where it is given by j.
+// matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane: a lane reads a
+// patch of q (a few codes from each of 8 rows), widens it and writes it to LDS turned round, one column of 8 values at
+// a time; likewise g where it is given by j.
 #include "ops_device.hpp"
 
 namespace pat {
 namespace {
 
-// A workgroup of 2 x 2 waves computes 64 * F rows by 64 * F columns, a wave F x F blocks of 32 x 32, going through j 64
-// at a time.  What the next 64 need is read into registers before these are multiplied, and widened into the other
-// half of LDS after.
-constexpr int kGradThreads = 256;
+// A workgroup of WA x WB waves computes a tile of R x R of out, a wave FA x FB blocks of 32 x 32, going through j 64 at a
+// time.  While a step's 64 are multiplied out of one half of LDS, the next step's are widened from registers into the
+// other, and what the step after that needs is on its way into these registers.  Of two waves on a SIMD one multiplies
+// first and the other widens first, so that the matrix unit and the vector unit both have work.
 
-template <int F>
-struct GradLds {
-  static constexpr int kRows = 64 * F;
-  uint8_t g[kRows * 128];  // rows of out: 64 values of j
-  uint8_t q[kRows * 128];  // columns of out: 64 values of j
+template <int FA, int FB, int WA, int WB>
+struct GradTile {
+  static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, R = 32 * FA * WA;
+  static_assert(R == 32 * FB * WB, "square");
+  static constexpr int PC = R * 8 / kThreads;  // columns of a patch: patches of 8 x PC, one a lane
+  static_assert(PC == 2 || PC == 4, "");
+  struct Lds {
+    uint8_t g[R * 128];  // rows of out: 64 values of j
+    uint8_t q[R * 128];  // columns of out: 64 values of j
+  };
 };
 
-// Where 16-byte block `block` (8 values of j) of a row stands: lanes that read one block of consecutive rows, and
-// lanes that write one block of every 8th row, both hit different banks.
-__device__ __forceinline__ int lds_at(int row, int block) { return row * 128 + ((block ^ row ^ row >> 3) & 7) * 16; }
+// Where 16-byte block `block` (8 values of j) of a row stands.  A row is half of the 64 banks; 16 lanes that read one
+// block of consecutive rows hit all banks once, 16 lanes that write one block of every fourth row all banks of two.
+// Rows 32 apart are a constant apart.
+__device__ __forceinline__ int swap02(int row) { return (row & ~5) | (row & 1) << 2 | (row >> 2 & 1); }
+__device__ __forceinline__ int lds_at(int row, int block) {
+  const int at = swap02(row);
+  return at * 128 + (block ^ (at & 7) ^ (at >> 3 & 3)) * 16;
+}
 
-// Turns 8 rows of 8 bfloat16 round: out[c] holds column c's 8 values.
-__device__ __forceinline__ void turn(const v4u (&rows)[8], v4u (&cols)[8]) {
+// Turns 8 rows of N bfloat16 (N / 2 words) round: column c's 8 values.
+template <int N>
+__device__ __forceinline__ v4u turned(const uint32_t (&rows)[8][N / 2], int c) {
+  v4u v;
 #pragma unroll
-  for (int c = 0; c < 8; ++c)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      cols[c][r] = __builtin_amdgcn_perm(rows[2 * r + 1][c / 2], rows[2 * r][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+  for (int r = 0; r < 4; ++r)
+    v[r] = __builtin_amdgcn_perm(rows[2 * r + 1][c / 2], rows[2 * r][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+  return v;
 }
 
 // Eight bfloat16 moved down by d places (0 to 8), zeros behind them.
@@ -44,167 +55,181 @@ __device__ __forceinline__ v4u move_down(v4u v, int d) {
   return v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
-// The 8 codes of a word as 8 bfloat16.
-__device__ __forceinline__ v4u widen8(uint32_t code, uint32_t s) {
-  const float scale = mx_scale_value(s);
-  auto pair = [&](v2bf v) { return __builtin_bit_cast(uint32_t, v); };
-  const v4u v = {pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 0)),
-                 pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 1)),
-                 pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 2)),
-                 pair(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, scale, 3))};
-  return s == 255u ? v4u{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : v;
+// Two codes of a byte (the I-th of a word) as two bfloat16.
+template <int I>
+__device__ __forceinline__ uint32_t widen2(uint32_t code, uint32_t s) {
+  const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, mx_scale_operand(s), I);
+  return __builtin_bit_cast(uint32_t, v);
 }
 
-template <int F, bool TRANSPOSED, typename T>
-__global__ __launch_bounds__(kGradThreads, F == 4 ? 1 : 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner,
-                                                                             int64_t cols, MatOut out) {
-  constexpr int R = 64 * F;
-  __shared__ __attribute__((aligned(16))) GradLds<F> lds[2];
+template <int FA, int FB, int WA, int WB, bool TRANSPOSED, typename T>
+__global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols,
+                                                               MatOut out) {
+  typedef GradTile<FA, FB, WA, WB> S;
+  typedef typename S::Lds Lds;
+  constexpr int R = S::R, PC = S::PC, W = S::kWaves, NT = S::kThreads;
+  __shared__ __attribute__((aligned(16))) Lds lds[2];
   TilePlace place;
   if (!tile_place((rows + R - 1) / R, (cols + R - 1) / R, &place)) return;
   const int64_t i0 = place.i * R, c0 = place.j * R;
   const int64_t pitch = (cols + 127) / 128 * 64;
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
 
-  // What a lane reads of 64 values of j.  q: a patch of 8 x 8, the columns' patches side by side over the lanes.
-  // g by rows: blocks of 8 values, 8 of them a row.  g by j: a patch like q's.
+  // What a lane reads of 64 values of j.  q: a patch of 8 x PC, the columns' patches side by side over the lanes.
+  // g by rows: PC blocks of 8 values, 8 of them a row.  g by j: a patch like q's.
   // Nothing is read beyond a matrix: rows of out beyond the last are the last again, j beyond the last likewise and
   // zeroed before they reach LDS, and a block or patch that would go over a row's end ends there instead.
-  const int patch_c = tid % (R / 8), patch_j = tid / (R / 8);
-  const bool has_patch = F == 4 || patch_j < 8;               // R patches in all: fewer than lanes below F = 4
-  const int64_t qc = min(c0 + patch_c * 8, pitch * 2 - 8);    // in the stored form, which is whole groups wide
-  const char* q_codes = (const char*)q.codes + qc / 2;
-  const char* q_scales = (const char*)q.scales + qc / 32;
-  const int64_t gi = min(i0 + patch_c * 8, rows - 8);         // TRANSPOSED: the patch's first row of out
+  const int patch_c = tid % (R / PC), patch_j = tid / (R / PC);
+  const int64_t qc = min(c0 + patch_c * PC, pitch * 2 - PC);  // in the stored form, which is whole groups wide
+  const uint32_t q_at = (uint32_t)(patch_j * 8 * pitch + qc / 2), q_scale_at = (uint32_t)(patch_j * 8 * (pitch / 16) + qc / 32);
+  const int64_t gi = min(i0 + patch_c * PC, rows - PC);       // TRANSPOSED: the patch's first row of out
   const int to_row = (int)(gi - i0);                          // its place in the tile, negative for a short last tile
-  constexpr int ROWS = TRANSPOSED ? 1 : 2 * F;
+  const int block = tid % 8, row_u = swap02(tid / 8);         // by rows: block and row of each NT / 8 rows
+  constexpr int ROWS = TRANSPOSED ? 1 : PC;
   const char* g_row[ROWS];
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
-    g_row[u] = (const char*)g.p + 2 * (TRANSPOSED ? gi : min(i0 + u * 32 + tid / 8, rows - 1) * g.stride);
+    g_row[u] = (const char*)g.p + 2 * (TRANSPOSED ? patch_j * 8 * g.stride + gi
+                                                  : min(i0 + u * (NT / 8) + row_u, rows - 1) * g.stride + block * 8);
 
   uint32_t code[8], scale[8];
-  v4u raw[TRANSPOSED ? 8 : 2 * F];
+  uint32_t raw_t[8][PC / 2];  // TRANSPOSED: 8 values of j by PC rows
+  v4u raw[PC];                // else: blocks of 8 j
 
-  // TAIL: fewer than 64 values of j are left.
+  // TAIL: perhaps fewer than 64 values of j are left.
   auto fetch = [&](int64_t j0, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
-    const int left = TAIL ? (int)(inner - j0) : 64;
-    if (has_patch) {
+    const int left = TAIL ? (int)min(inner - j0, (int64_t)64) : 64;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const uint32_t j = TAIL ? min(patch_j * 8 + r, left - 1) : patch_j * 8 + r;
-        code[r] = ldg<uint32_t, false>(q_codes + j0 * pitch + j * (uint32_t)pitch);
-        scale[r] = ldg<uint8_t, false>(q_scales + j0 * (pitch / 16) + j * (uint32_t)(pitch / 16));
-        if constexpr (TRANSPOSED) raw[r] = ldg<v4u, false, 2>(g_row[0] + 2 * j0 * g.stride + 2 * (uint64_t)j * g.stride);
+    for (int r = 0; r < 8; ++r) {
+      // a row's address is the workgroup's and a lane's part of 32 bits; rows beyond the last are it again
+      const int back = TAIL ? max(patch_j * 8 + r - (left - 1), 0) : 0;
+      const char* p = (const char*)q.codes + (j0 + r) * pitch + (TAIL ? -(int64_t)back * pitch + q_at : q_at);
+      code[r] = PC == 4 ? ldg<uint16_t, false>(p) : ldg<uint8_t, false>(p);
+      scale[r] = ldg<uint8_t, false>((const char*)q.scales + (j0 + r) * (pitch / 16) +
+                                     (TAIL ? -(int64_t)back * (pitch / 16) + q_scale_at : q_scale_at));
+      if constexpr (TRANSPOSED) {
+        const char* t = g_row[0] + 2 * (j0 + r - back) * g.stride;
+        if constexpr (PC == 4) {
+          const v2u v = ldg<v2u, false, 2>(t);
+          raw_t[r][0] = v[0], raw_t[r][PC / 2 - 1] = v[1];
+        } else {
+          raw_t[r][0] = ldg<uint32_t, false, 2>(t);
+        }
       }
     }
     if constexpr (!TRANSPOSED) {
-      const int64_t at = TAIL ? min(j0 + tid % 8 * 8, inner - 8) : j0 + tid % 8 * 8;
+      const int64_t at = TAIL ? min(j0, inner - 8 - block * 8) : j0;
 #pragma unroll
-      for (int u = 0; u < 2 * F; ++u) raw[u] = ldg<v4u, false, 2>(g_row[u] + 2 * at);
+      for (int u = 0; u < PC; ++u) raw[u] = ldg<v4u, false, 2>(g_row[u] + 2 * at);
     }
   };
-  auto place_lds = [&](GradLds<F>& l, int64_t j0, auto tail) {
+  auto widen = [&](Lds& l, int64_t j0, auto tail) {
     if constexpr (decltype(tail)::value) {
-      const int left = (int)(inner - j0);
+      const int left = (int)min(inner - j0, (int64_t)64);
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         const bool in = patch_j * 8 + r < left;
         code[r] = in ? code[r] : 0u;
         scale[r] = in ? scale[r] : 0u;
-        if constexpr (TRANSPOSED) raw[r] = in ? raw[r] : v4u{0, 0, 0, 0};
+        if constexpr (TRANSPOSED) {
+#pragma unroll
+          for (int w = 0; w < PC / 2; ++w) raw_t[r][w] = in ? raw_t[r][w] : 0u;
+        }
       }
       if constexpr (!TRANSPOSED) {
-        const int d = min(max(tid % 8 * 8 - (left - 8), 0), 8);
+        const int d = min(max(block * 8 - (left - 8), 0), 8);
 #pragma unroll
-        for (int u = 0; u < 2 * F; ++u) raw[u] = move_down(raw[u], d);
+        for (int u = 0; u < PC; ++u) raw[u] = move_down(raw[u], d);
       }
     }
-    if (has_patch) {
-      v4u wide[8], turned[8];
+    uint32_t wide[8][PC / 2];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) wide[r] = widen8(code[r], scale[r]);
-      turn(wide, turned);
-#pragma unroll
-      for (int c = 0; c < 8; ++c) *(v4u*)(l.q + lds_at(patch_c * 8 + c, patch_j)) = turned[c];
-      if constexpr (TRANSPOSED) {
-        turn(raw, turned);
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (to_row + c >= 0) *(v4u*)(l.g + lds_at(to_row + c, patch_j)) = turned[c];
-      }
+    for (int r = 0; r < 8; ++r) {
+      wide[r][0] = widen2<0>(code[r], scale[r]);
+      if constexpr (PC == 4) wide[r][PC / 2 - 1] = widen2<1>(code[r], scale[r]);
     }
-    if constexpr (!TRANSPOSED) {
 #pragma unroll
-      for (int u = 0; u < 2 * F; ++u) *(v4u*)(l.g + lds_at(u * 32 + tid / 8, tid % 8)) = raw[u];
+    for (int c = 0; c < PC; ++c) *(v4u*)(l.q + lds_at(patch_c * PC + c, patch_j)) = turned<PC>(wide, c);
+    if constexpr (TRANSPOSED) {
+#pragma unroll
+      for (int c = 0; c < PC; ++c)
+        if (to_row + c >= 0) *(v4u*)(l.g + lds_at(to_row + c, patch_j)) = turned<PC>(raw_t, c);
+    } else {
+#pragma unroll
+      for (int u = 0; u < PC; ++u) *(v4u*)(l.g + lds_at(u * (NT / 8) + row_u, block)) = raw[u];
     }
   };
 
-  const int row_g = wave / 2 * 32 * F + lane % 32, row_q = wave % 2 * 32 * F + lane % 32, half = lane / 32;
-  v16f acc[F][F];
+  const int half = lane / 32, wave_row = wave / WB * 32 * FA, wave_col = wave % WB * 32 * FB;
+  v16f acc[FA][FB];
 #pragma unroll
-  for (int x = 0; x < F; ++x)
+  for (int x = 0; x < FA; ++x)
 #pragma unroll
-    for (int y = 0; y < F; ++y)
+    for (int y = 0; y < FB; ++y)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
 
-  // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.
-  auto multiply = [&](const GradLds<F>& l) {
+  // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.  The next 16 values of j are
+  // read from LDS while these are multiplied.
+  struct Blocks {
+    v8bf g[FA], q[FB];
+  };
+  auto read = [&](const Lds& l, int step, Blocks& b) {
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-      v8bf fg[F], fq[F];
+    for (int x = 0; x < FA; ++x) b.g[x] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * x + lane % 32, step * 2 + half));
 #pragma unroll
-      for (int x = 0; x < F; ++x) {
-        fg[x] = *(const v8bf*)(l.g + lds_at(row_g + 32 * x, step * 2 + half));
-        fq[x] = *(const v8bf*)(l.q + lds_at(row_q + 32 * x, step * 2 + half));
-      }
+    for (int y = 0; y < FB; ++y) b.q[y] = *(const v8bf*)(l.q + lds_at(wave_col + 32 * y + lane % 32, step * 2 + half));
+  };
+  auto mul = [&](const Blocks& b) {
 #pragma unroll
-      for (int x = 0; x < F; ++x)
+    for (int x = 0; x < FA; ++x)
 #pragma unroll
-        for (int y = 0; y < F; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fg[x], fq[y], acc[x][y], 0, 0, 0);
-    }
+      for (int y = 0; y < FB; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.g[x], b.q[y], acc[x][y], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](const Lds& l) {
+    Blocks b0, b1;
+    read(l, 0, b0);
+    read(l, 1, b1);
+    mul(b0);
+    read(l, 2, b0);
+    mul(b1);
+    read(l, 3, b1);
+    mul(b0);
+    mul(b1);
   };
 
-  // The loop's body has no branch: with one, the accumulators would be moved at every turn.
-  const int64_t full = inner / 64;
-  int at = 0;
-  if (full) {
-    fetch(0, Bool<false>{});
-    place_lds(lds[0], 0, Bool<false>{});
-  }
-  for (int64_t step = 1; step < full; ++step, at ^= 1) {
-    fetch(step * 64, Bool<false>{});
-    __syncthreads();  // this half is written, and nobody reads the other any more
-    multiply(lds[at]);
-    place_lds(lds[at ^ 1], step * 64, Bool<false>{});
-  }
-  if (inner % 64) {
-    fetch(full * 64, Bool<true>{});
-    if (full) {
+  const int64_t steps = (inner + 63) / 64, whole = inner / 64;
+  fetch(0, Bool<true>{});
+  widen(lds[0], 0, Bool<true>{});
+  if (steps > 1) fetch(64, Bool<true>{});
+  // The loops' bodies have no branch: with one, the accumulators would be moved at every turn.
+  int64_t s = 0;
+  if (W == 4 || wave < 4) {
+    for (; s + 2 < whole; ++s) {
+      __syncthreads();  // this half is written, and nobody reads the other any more
+      multiply(lds[s & 1]);
+      widen(lds[~s & 1], s * 64 + 64, Bool<false>{});
+      fetch(s * 64 + 128, Bool<false>{});
+    }
+  } else {
+    for (; s + 2 < whole; ++s) {
       __syncthreads();
-      multiply(lds[at]);
-      at ^= 1;
+      widen(lds[~s & 1], s * 64 + 64, Bool<false>{});
+      fetch(s * 64 + 128, Bool<false>{});
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(lds[s & 1]);
     }
-    place_lds(lds[at], full * 64, Bool<true>{});
   }
-  __syncthreads();
-  multiply(lds[at]);
+  for (; s < steps; ++s) {  // the last two or three
+    __syncthreads();
+    multiply(lds[s & 1]);
+    if (s + 1 < steps) widen(lds[~s & 1], s * 64 + 64, Bool<true>{});
+    if (s + 2 < steps) fetch(s * 64 + 128, Bool<true>{});
+  }
 
-  // Lane l has column l mod 32 of a block and rows 8 * (e / 4) + 4 * (l / 32) + e mod 4.
-#pragma unroll
-  for (int x = 0; x < F; ++x) {
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int64_t i = i0 + wave / 2 * 32 * F + 32 * x + 8 * (e / 4) + 4 * half + e % 4;
-      if (i >= rows) continue;
-      char* p = (char*)out.p + (i * out.stride + c0) * T::kBytes;
-#pragma unroll
-      for (int y = 0; y < F; ++y)
-        if (c0 + row_q + 32 * y < cols) T::store(p, row_q + 32 * y, acc[x][y][e]);
-    }
-  }
+  write_tile<FA, FB, T>(acc, (float*)&lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
 }
 
 // The same product where the vectors of 8 above do not exist: fewer than 8 values of j, or of rows where g is given by
@@ -226,7 +251,7 @@ __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows
       const int64_t at = TRANSPOSED ? j * g.stride + i : i * g.stride + j;
       fg[e / 2] |= (uint32_t)ldg<uint16_t, false>((const char*)g.p + 2 * at) << (16 * (e & 1));
       const uint32_t code = q.codes[j * pitch + c / 2] >> (4 * (c & 1)), s = q.scales[j * (pitch / 16) + c / 32];
-      fq[e / 2] |= (widen8(code & 15u, s)[0] & 0xFFFFu) << (16 * (e & 1));
+      fq[e / 2] |= (widen2<0>(code & 15u, s) & 0xFFFFu) << (16 * (e & 1));
     }
     sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, fg), __builtin_bit_cast(v8bf, fq), sum, 0, 0, 0);
   }
@@ -236,11 +261,13 @@ __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows
     if (i0 + 4 * part + r < rows) T::store((char*)out.p, (i0 + 4 * part + r) * out.stride + c, sum[r]);
 }
 
-template <int F, bool TRANSPOSED>
+template <int FA, int FB, int WA, int WB, bool TRANSPOSED>
 hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, hipStream_t stream) {
-  const size_t tiles = ceil_div(rows, 64 * F) * ceil_div(cols, 64 * F);
-  const auto kernel = dtype == Elem::f32 ? grad_kernel<F, TRANSPOSED, F32> : grad_kernel<F, TRANSPOSED, B16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(kGradThreads), 0, stream, g, q, rows, inner,
+  constexpr int R = GradTile<FA, FB, WA, WB>::R;
+  const size_t tiles = ceil_div(rows, R) * ceil_div(cols, R);
+  const auto kernel = dtype == Elem::f32 ? grad_kernel<FA, FB, WA, WB, TRANSPOSED, F32>
+                                         : grad_kernel<FA, FB, WA, WB, TRANSPOSED, B16>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(64 * WA * WB), 0, stream, g, q, rows, inner,
                      cols, out);
   return hipGetLastError();
 }
@@ -254,9 +281,9 @@ hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, 
     return hipGetLastError();
   }
   auto wgs = [&](int f) { return ceil_div(rows, 64 * f) * ceil_div(cols, 64 * f); };
-  if (wgs(4) >= 192) return run_grad<4, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
-  if (wgs(2) >= 192) return run_grad<2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
-  return run_grad<1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
+  if (wgs(4) >= 192) return run_grad<4, 2, 2, 4, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
+  if (wgs(2) >= 192) return run_grad<2, 2, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
+  return run_grad<1, 1, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
 }
 
 }  // namespace

@@ -54,6 +54,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b,
   typedef Tile<FA, FB, WA, WB> S;
   typedef typename S::Lds Lds;
   constexpr int R = S::R, W = S::kWaves;
+  // Two objects, and not an array: the compiler then knows that the loads into one do not touch the other.
   __shared__ __attribute__((aligned(16))) Lds lds0;
   __shared__ __attribute__((aligned(16))) Lds lds1;
   TilePlace place;
@@ -196,32 +197,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b,
     }
   }
 
-  // Lane l has column l mod 32 of a block and rows 8 * (e / 4) + 4 * (l / 32) + e mod 4.  A wave turns 32 rows at a
-  // time round in its own part of LDS and writes them as vectors.
-  __syncthreads();
-  constexpr int C = 32 * FB, P = C + 8;  // a wave's columns; its rows 8 banks apart, for the halves' rows of 4 apart
-  static_assert(W / 2 * 32 * P * 4 <= sizeof(Lds), "");
-  float* part = (float*)(wave < W / 2 ? &lds0 : &lds1) + wave % (W / 2) * 32 * P;
-#pragma unroll
-  for (int x = 0; x < FA; ++x) {
-#pragma unroll
-    for (int y = 0; y < FB; ++y)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) part[(8 * (e / 4) + 4 * half + e % 4) * P + 32 * y + lane % 32] = acc[x][y][e];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    constexpr int LANES = C / 8;  // lanes a row, 8 columns each
-#pragma unroll
-    for (int u = 0; u < 32 * LANES / 64; ++u) {
-      const int r = u * (64 / LANES) + lane / LANES, c = lane % LANES * 8, row = wave_row + 32 * x + r;
-      const v4f lo = *(const v4f*)(part + r * P + c), hi = *(const v4f*)(part + r * P + c + 4);
-      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      const int left = rows_b - wave_col - c;
-      char* p = (char*)out.p + ((i0 + row) * out.stride + j0 + wave_col + c) * T::kBytes;
-      if (row < rows_a && left >= 8) store8<T, false, false, true>(p, 8, 4, v);
-      else if (row < rows_a && left > 0) store8<T, false, false, false>(p, left, 4, v);
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
+  write_tile<FA, FB, T>(acc, wave < W / 2 ? (float*)&lds0 : (float*)&lds1, wave % (W / 2), wave_row, wave_col, i0, j0, m, n, out);
 }
 
 // ---- few rows ------------------------------------------------------------------------------------------------

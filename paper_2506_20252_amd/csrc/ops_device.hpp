@@ -133,10 +133,9 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t high_bits) {
   const uint32_t field = high_bits >> 23;
   return field == 255u ? 255u : (field > 2u ? field - 2u : 0u);
 }
-// 2^(s - 127); s = 0 is the subnormal 2^-127, s = 255 NaN.
-__device__ __forceinline__ float mx_scale_value(uint32_t s) {
-  return __uint_as_float(s == 0u ? 0x00400000u : s == 255u ? 0x7FC00000u : s << 23);
-}
+// The scale operand of the conversion instructions, of which they take the exponent field alone: 2^(s - 127), 0 being
+// 2^-127 and 255 NaN.
+__device__ __forceinline__ float mx_scale_operand(uint32_t s) { return __uint_as_float(s << 23); }
 
 // Eight consecutive elements as they are in memory, those from n on zero; nothing is done with what is loaded, so
 // that several are in flight together.
@@ -180,7 +179,7 @@ __device__ __forceinline__ uint32_t high_bits(const Raw8<B16>& r) {
 
 // The codes of 8 elements under scale byte s, one word.
 __device__ __forceinline__ uint32_t mx_codes(const Raw8<F32>& r, uint32_t s) {
-  const float scale = mx_scale_value(s);
+  const float scale = mx_scale_operand(s);
   auto f = [&](int i) { return __uint_as_float(r.w[i / 4][i % 4]); };
   uint32_t c = 0;
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, f(0), f(1), scale, 0);
@@ -190,7 +189,7 @@ __device__ __forceinline__ uint32_t mx_codes(const Raw8<F32>& r, uint32_t s) {
   return s == 255u ? 0u : c;
 }
 __device__ __forceinline__ uint32_t mx_codes(const Raw8<B16>& r, uint32_t s) {
-  const float scale = mx_scale_value(s);
+  const float scale = mx_scale_operand(s);
   auto f = [&](int i) {
     const uint32_t w = r.w[0][i];  // __builtin_bit_cast of a vector's element itself takes its first one
     return __builtin_bit_cast(v2bf, w);
@@ -229,23 +228,6 @@ __device__ __forceinline__ uint32_t or_of_16_by_4(uint32_t v) {
   return v | dpp<0x128>(v);         // row_ror 8
 }
 
-// 32 values as 32 codes under one scale: the four words of a block's codes.
-__device__ __forceinline__ v4u mx_codes(const float (&v)[32], uint32_t s) {
-  v4u q = {0, 0, 0, 0};
-  if (s == 255u) return q;
-  const float scale = mx_scale_value(s);
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    uint32_t word = 0;
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w], v[8 * w + 1], scale, 0);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 2], v[8 * w + 3], scale, 1);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 4], v[8 * w + 5], scale, 2);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, v[8 * w + 6], v[8 * w + 7], scale, 3);
-    q[w] = word;
-  }
-  return q;
-}
-
 // Where a tile of the output is; neighbours in `t` share rows of a or b.
 struct TilePlace {
   int64_t i, j;
@@ -260,6 +242,40 @@ __device__ __forceinline__ bool tile_place(int64_t tiles_m, int64_t tiles_n, Til
   p->i = band * 8 + in_band % high;
   p->j = in_band / high;
   return true;
+}
+
+// Writes a wave's FA x FB blocks of 32 x 32, as the 32 x 32 matrix instructions leave them (lane l: column l mod 32, rows
+// 8 * (e / 4) + 4 * (l / 32) + e mod 4), to rows wave_row ... and columns wave_col ... of the tile at (i0, j0).  The wave
+// turns 32 rows at a time round in a part of LDS of its own, the `slot`-th at `lds` (tile_part floats each), and writes
+// them as vectors.  Nobody may still be reading that LDS when the last wave comes here: the barrier is in here.
+constexpr int tile_part(int fb) { return 32 * (32 * fb + 8); }  // rows 8 banks apart, for the halves' rows of 4 apart
+
+template <int FA, int FB, typename T>
+__device__ __forceinline__ void write_tile(const v16f (&acc)[FA][FB], float* lds, int slot, int wave_row, int wave_col,
+                                           int64_t i0, int64_t j0, int64_t rows, int64_t cols, MatOut out) {
+  constexpr int C = 32 * FB, P = C + 8, LANES = C / 8;  // columns, their pitch, lanes a row with 8 columns each
+  const int lane = threadIdx.x % 64, half = lane / 32;
+  __syncthreads();
+  float* part = lds + slot * tile_part(FB);
+#pragma unroll
+  for (int x = 0; x < FA; ++x) {
+#pragma unroll
+    for (int y = 0; y < FB; ++y)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) part[(8 * (e / 4) + 4 * half + e % 4) * P + 32 * y + lane % 32] = acc[x][y][e];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int u = 0; u < 32 * LANES / 64; ++u) {
+      const int r = u * (64 / LANES) + lane / LANES, c = lane % LANES * 8;
+      const int64_t i = i0 + wave_row + 32 * x + r, j = j0 + wave_col + c;
+      const v4f lo = *(const v4f*)(part + r * P + c), hi = *(const v4f*)(part + r * P + c + 4);
+      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      char* p = (char*)out.p + (i * out.stride + j) * T::kBytes;
+      if (i < rows && cols - j >= 8) store8<T, false, false, true>(p, 8, 4, v);
+      else if (i < rows && cols > j) store8<T, false, false, false>(p, cols - j, 4, v);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
 }
 
 }  // namespace
