@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, RowSplit sp
         }
         char* p = (char*)a.out.p + (r * a.out.stride + c) * T::kBytes;
         if (WHOLE || (c >= 0 && left >= 8)) {
-          store8<T, false, false, true>(p, 8, 4, y);
+          store8<T, false, false, kWhole>(p, 8, 4, y);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i)

@@ -18,42 +18,42 @@ __device__ __forceinline__ int64_t token_row(const char* tokens, int token_bytes
 }
 
 // A row is taken by `lanes` lanes, 8 columns each at a time; a workgroup holds 256 / lanes tokens side by side and
-// kLookupTokens of them in turn, whose table rows a lane reads before it writes any.
-constexpr int kLookupTokens = 4;
-
-template <typename TI, typename TO>
+// TOKENS of them in turn, whose table rows a lane reads before it writes any.template <int TOKENS, typename TI, typename TO>
+template <int TOKENS, typename TI, typename TO>
 __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int token_bytes, int64_t ntokens, Mat table,
                                                      int64_t first, int64_t rows, int64_t cols, float scale, MatOut out,
                                                      int lanes) {
   constexpr bool SPLIT = Split<TI, TO>::value;
   const int side = 256 / lanes, lane = threadIdx.x % lanes;
-  const int64_t step = (int64_t)side * kLookupTokens, gap = lane_gap<SPLIT>(lanes);
+  const int64_t step = (int64_t)side * TOKENS, gap = lane_gap<SPLIT>(lanes);
   for (int64_t t0 = blockIdx.x * step + threadIdx.x / lanes; t0 < ntokens; t0 += gridDim.x * step) {
-    int64_t row[kLookupTokens];
+    int64_t row[TOKENS];
 #pragma unroll
-    for (int u = 0; u < kLookupTokens; ++u) {
+    for (int u = 0; u < TOKENS; ++u) {
       const int64_t t = t0 + u * side;
       row[u] = t < ntokens ? token_row(tokens, token_bytes, t, first, rows) : -1;
     }
-    auto columns = [&](int64_t c, auto full) {
-      constexpr bool FULL = decltype(full)::value;
-      float v[kLookupTokens][8];
+    auto columns = [&](int64_t c, auto cover) {
+      constexpr Cover C = decltype(cover)::value;
+      float v[TOKENS][8];
 #pragma unroll
-      for (int u = 0; u < kLookupTokens; ++u)  // a token that the table does not hold reads row 0 and is zeroed below
-        load8<TI, SPLIT, false, FULL>((const char*)table.p + (max(row[u], (int64_t)0) * table.stride + c) * TI::kBytes,
-                                      rows ? cols - c : 0, gap, v[u]);
+      for (int u = 0; u < TOKENS; ++u)  // a token that the table does not hold reads row 0 and is zeroed below
+        load8<TI, SPLIT, false, C>((const char*)table.p + (max(row[u], (int64_t)0) * table.stride + c) * TI::kBytes,
+                                   rows ? cols - c : 0, gap, v[u]);
 #pragma unroll
-      for (int u = 0; u < kLookupTokens; ++u) {
+      for (int u = 0; u < TOKENS; ++u) {
         const int64_t t = t0 + u * side;
         if (t >= ntokens) break;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[u][i] = row[u] < 0 ? 0.0f : v[u][i] * scale;
-        store8<TO, SPLIT, true, FULL>((char*)out.p + (t * out.stride + c) * TO::kBytes, cols - c, gap, v[u]);
+        store8<TO, SPLIT, true, C>((char*)out.p + (t * out.stride + c) * TO::kBytes, cols - c, gap, v[u]);
       }
     };
     for (int64_t c = lane_column<SPLIT>(lane); c < cols; c += 8 * lanes) {
-      if (rows && cols - c >= gap + 4) columns(c, Bool<true>{});
-      else columns(c, Bool<false>{});
+      const Cover cover = rows ? cover_of(cols - c, gap, cols) : kFew;  // a table without rows is not read
+      if (cover == kWhole) columns(c, CoverOf<kWhole>{});
+      else if (cover == kEnd) columns(c, CoverOf<kEnd>{});
+      else columns(c, CoverOf<kFew>{});
     }
   }
 }
@@ -67,18 +67,22 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
 // reads the tokens themselves and leaves out those the table does not hold.
 
 constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64;
-constexpr int kMaxBins = 1 << 10;
+constexpr int kMaxBits = 10, kMaxBins = 1 << kMaxBits;
 
 struct SortPlan {
   int bits, passes;
   int64_t tile, tiles;  // entries per workgroup, workgroups
 };
 
+constexpr int kSmallBits = 8;                         // of the sort in one workgroup, below
+constexpr int64_t kSmallTokens = 4096;
+
 SortPlan sort_plan(int64_t ntokens, int64_t rows) {
   int kb = 1;
   while (((int64_t)1 << kb) < rows) ++kb;
+  const int most = ntokens <= kSmallTokens ? kSmallBits : kMaxBits;
   SortPlan s;
-  s.passes = (kb + 9) / 10;
+  s.passes = (kb + most - 1) / most;
   s.bits = (kb + s.passes - 1) / s.passes;
   s.tile = (int64_t)ceil_div(ceil_div(ntokens, 128), kSortThreads) * kSortThreads;
   if (s.tile < 1024) s.tile = 1024;
@@ -206,13 +210,89 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
   }
 }
 
-// First entry of keys[0, n) that is not below `key`.
-__device__ __forceinline__ int32_t lower_bound(const int32_t* keys, int32_t n, int32_t key) {
+// The whole sort in one workgroup, for so few tokens that launches are what it costs (us, 1001 tokens of 1251 rows: 14.5
+// in four launches).  Entries stay in LDS from pass to pass; a wave takes a section of them, 64 at a time.
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+
+__global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(SortArgs a, int passes) {
+  __shared__ int32_t next[kSmallWaves][1 << kSmallBits];
+  __shared__ int32_t key[2][kSmallTokens];
+  __shared__ int16_t pos[2][kSmallTokens];
+  __shared__ int32_t sums[1 << kSmallBits];
+  const int bins = 1 << a.bits, t = threadIdx.x, wave = t / 64, lane = t % 64;
+  for (int i = t; i < a.ntokens; i += kSmallThreads) {
+    key[0][i] = (int32_t)token_row(a.tokens, a.token_bytes, i, a.first, a.rows);
+    pos[0][i] = (int16_t)i;
+  }
+  int n = (int)a.ntokens, at = 0;  // the first pass drops the entries of key -1
+  for (int p = 0; p < passes; ++p, at ^= 1) {
+    const int shift = p * a.bits, section = (n + kSmallThreads - 1) / kSmallThreads * 64, begin = wave * section;
+    for (int i = t; i < kSmallWaves * bins; i += kSmallThreads) next[i / bins][i % bins] = 0;
+    __syncthreads();
+    for (int i = begin + lane; i < begin + section; i += 64) {
+      const int32_t k = i < n ? key[at][i] : -1;
+      if (k >= 0) atomicAdd(&next[wave][k >> shift & (bins - 1)], 1);
+    }
+    __syncthreads();
+    int32_t total = 0;
+    if (t < bins) {
+      for (int w = 0; w < kSmallWaves; ++w) total += next[w][t];
+      sums[t] = total;
+    }
+    __syncthreads();
+    for (int d = 1; d < bins; d <<= 1) {
+      const int32_t left = t < bins && t >= d ? sums[t - d] : 0;
+      __syncthreads();
+      if (t < bins) sums[t] += left;
+      __syncthreads();
+    }
+    if (t < bins) {
+      int32_t base = sums[t] - total;
+      for (int w = 0; w < kSmallWaves; ++w) {
+        const int32_t c = next[w][t];
+        next[w][t] = base;
+        base += c;
+      }
+    }
+    __syncthreads();
+    for (int i = begin + lane; i < begin + section; i += 64) {
+      const int32_t k = i < n ? key[at][i] : -1;
+      const int digit = k >> shift & (bins - 1);
+      uint64_t same = __ballot(k >= 0);
+      for (int b = 0; b < a.bits; ++b) {
+        const bool one = digit >> b & 1;
+        const uint64_t m = __ballot(one);
+        same &= one ? m : ~m;
+      }
+      if (k >= 0) {
+        const int leader = __builtin_ctzll(same);
+        int32_t to = 0;
+        if (lane == leader) to = atomicAdd(&next[wave][digit], __popcll(same));
+        to = __shfl(to, leader) + __popcll(same & (((uint64_t)1 << lane) - 1));
+        key[at ^ 1][to] = k;
+        pos[at ^ 1][to] = pos[at][i];
+      }
+    }
+    __syncthreads();
+    n = sums[bins - 1];
+    __syncthreads();
+  }
+  if (t == 0) *a.nvalid = n;
+  for (int i = t; i < n; i += kSmallThreads) {
+    a.keys_out[i] = key[at][i];
+    a.pos_out[i] = pos[at][i];
+  }
+}
+
+// First entry of keys[0, n) that is not below `key`, by a whole wave: 64 places are looked at together, so a search of
+// 2^18 entries waits for three loads in turn and not for 18.
+__device__ __forceinline__ int32_t wave_lower_bound(const int32_t* keys, int32_t n, int32_t key) {
   int32_t lo = 0, hi = n;
   while (lo < hi) {
-    const int32_t mid = lo + (hi - lo) / 2;
-    if (ldg<int32_t, false>((const char*)(keys + mid)) < key) lo = mid + 1;
-    else hi = mid;
+    const int32_t step = (hi - lo + 63) / 64, at = lo + (threadIdx.x % 64 + 1) * step - 1;
+    const int32_t below = __popcll(__ballot(at < hi && ldg<int32_t, false>((const char*)(keys + min(at, hi - 1))) < key));
+    hi = min(hi, lo + (below + 1) * step - 1);
+    lo += below * step;
   }
   return lo;
 }
@@ -240,30 +320,43 @@ constexpr int kZeroRows = 64;  // rows that one workgroup looks through for ones
 
 template <typename TO>
 __device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
-  __shared__ uint64_t absent;
+  __shared__ int32_t ends[2];
+  __shared__ unsigned long long present;
   const int64_t r0 = (int64_t)wg * kZeroRows;
-  if (threadIdx.x < 64) {
-    const int64_t r = r0 + threadIdx.x;
-    bool none = r < a.rows;
-    if (none && n) {
-      const int32_t at = lower_bound(a.keys, n, (int32_t)r);
-      none = at == n || a.keys[at] != (int32_t)r;
+  if (threadIdx.x == 0) present = 0;
+  if (threadIdx.x < 128) {
+    const int32_t end = wave_lower_bound(a.keys, n, (int32_t)min(r0 + (threadIdx.x / 64 ? kZeroRows : 0), a.rows));
+    if (threadIdx.x % 64 == 0) ends[threadIdx.x / 64] = end;
+  }
+  __syncthreads();
+  const int32_t lo = ends[0], hi = ends[1];
+  if (hi - lo <= 16 * 256) {  // the rows' entries, all looked at
+    unsigned long long mine = 0;
+    for (int32_t i = lo + (int)threadIdx.x; i < hi; i += 256) mine |= 1ull << (a.keys[i] - r0);
+    if (mine) atomicOr(&present, mine);
+  } else if (threadIdx.x < 64 && r0 + threadIdx.x < a.rows) {  // or each row searched for between them
+    const int32_t row = (int32_t)(r0 + threadIdx.x);
+    int32_t first = lo, end = hi;
+    while (first < end) {
+      const int32_t mid = first + (end - first) / 2;
+      if (a.keys[mid] < row) first = mid + 1;
+      else end = mid;
     }
-    const uint64_t m = __ballot(none);
-    if (threadIdx.x == 0) absent = m;
+    if (first < hi && a.keys[first] == row) atomicOr(&present, 1ull << threadIdx.x);
   }
   __syncthreads();
   constexpr bool SPLIT = Split<TO, TO>::value;
   const int side = 256 / a.lanes, lane = threadIdx.x % a.lanes;
   const int64_t gap = lane_gap<SPLIT>(a.lanes);
   const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  const uint64_t m = absent;
-  for (int i = threadIdx.x / a.lanes; i < kZeroRows; i += side) {
-    if (!(m >> i & 1)) continue;
+  const uint64_t m = present;
+  const int here = (int)min((int64_t)kZeroRows, a.rows - r0);
+  for (int i = threadIdx.x / a.lanes; i < here; i += side) {
+    if (m >> i & 1) continue;
     for (int64_t c = lane_column<SPLIT>(lane); c < a.cols; c += 8 * a.lanes) {
       char* p = (char*)a.out.p + ((r0 + i) * a.out.stride + c) * TO::kBytes;
-      if (a.cols - c >= gap + 4) store8<TO, SPLIT, true, true>(p, a.cols - c, gap, zero);
-      else store8<TO, SPLIT, true, false>(p, a.cols - c, gap, zero);
+      if (a.cols - c >= gap + 4) store8<TO, SPLIT, true, kWhole>(p, a.cols - c, gap, zero);
+      else store8<TO, SPLIT, true, kEnd>(p, a.cols - c, gap, zero);
     }
   }
 }
@@ -292,20 +385,20 @@ __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
   const bool open_left = i0 > 0 && a.keys[i0 - 1] == a.keys[i0];
   const bool open_right = i1 < n && a.keys[i1] == a.keys[i1 - 1];
 
-  auto columns = [&](auto full) {
-    constexpr bool FULL = decltype(full)::value;
+  auto columns = [&](auto cover) {
+    constexpr Cover C = decltype(cover)::value;
     float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     int32_t row = a.keys[i0];
     bool head = true;  // still in the row of the piece's first entry
     auto flush = [&](bool last) {
       if ((head && open_left) || (last && open_right)) {
         float* p = a.partial + (2 * piece + (head ? 0 : 1)) * a.pitch + c;
-        store8<F32, SPLIT, false, FULL>((char*)p, left, gap, sum);
+        store8<F32, SPLIT, false, C>((char*)p, left, gap, sum);
       } else {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = sum[j] * a.scale;
-        store8<TO, SPLIT, true, FULL>((char*)a.out.p + ((int64_t)row * a.out.stride + c) * TO::kBytes, left, gap, v);
+        store8<TO, SPLIT, true, C>((char*)a.out.p + ((int64_t)row * a.out.stride + c) * TO::kBytes, left, gap, v);
       }
     };
     constexpr int U = 8;
@@ -330,7 +423,7 @@ __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
           key[u] = a.keys[at];
           pos = a.pos[at];
         }
-        load8<TI, SPLIT, true, FULL>((const char*)a.g.p + (pos * a.g.stride + c) * TI::kBytes, left, gap, v[u]);
+        load8<TI, SPLIT, true, C>((const char*)a.g.p + (pos * a.g.stride + c) * TI::kBytes, left, gap, v[u]);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -349,8 +442,10 @@ __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
     flush(true);
   };
   // one way for the whole wave: entries are taken from every lane, so every lane has to be there
-  if (__all(left >= gap + 4)) columns(Bool<true>{});
-  else columns(Bool<false>{});
+  const Cover cover = cover_of(left, gap, a.cols);
+  if (cover == kWhole) columns(CoverOf<kWhole>{});
+  else if (cover == kEnd) columns(CoverOf<kEnd>{});
+  else columns(CoverOf<kFew>{});
 }
 
 // A workgroup looks at kJoinPieces boundaries between pieces, for 256 columns.  Where a row goes over a boundary and
@@ -452,9 +547,9 @@ GradSpace grad_space(char* base, int64_t ntokens, const SortPlan& s, const SumPl
   return w;
 }
 
-template <typename TI>
+template <int TOKENS, typename TI>
 auto lookup_of(Elem dtype) {
-  return dtype == Elem::f32 ? lookup_kernel<TI, F32> : lookup_kernel<TI, B16>;
+  return dtype == Elem::f32 ? lookup_kernel<TOKENS, TI, F32> : lookup_kernel<TOKENS, TI, B16>;
 }
 
 template <bool UNIFORM, typename TI>
@@ -467,9 +562,14 @@ auto sum_of(Elem dtype) {
 hipError_t launch_embedding(const void* tokens, int token_bytes, int64_t ntokens, Mat table, Elem table_dtype,
                             int64_t first, int64_t rows, int64_t cols, float scale, MatOut out, Elem dtype,
                             hipStream_t stream) {
-  const auto kernel = table_dtype == Elem::f32 ? lookup_of<F32>(dtype) : lookup_of<B16>(dtype);
   const int lanes = row_lanes((cols + 7) / 8, 256);
-  const size_t wgs = std::min<size_t>(ceil_div(ntokens, kLookupTokens * (256 / lanes)), 1 << 20);
+  // One token a lane where that leaves workgroups for the chip (1001 tokens of 333 columns: 63 of them with four).
+  // Large: 153 us with two in turn, 157 with four, 161 with eight (65536 tokens of 4096 bfloat16 columns).
+  const int tokens_each = ceil_div(ntokens, 2 * (256 / lanes)) < 1024 ? 1 : 2;
+  const bool f32 = table_dtype == Elem::f32;
+  const auto kernel = tokens_each == 1 ? (f32 ? lookup_of<1, F32>(dtype) : lookup_of<1, B16>(dtype))
+                                       : (f32 ? lookup_of<2, F32>(dtype) : lookup_of<2, B16>(dtype));
+  const size_t wgs = std::min<size_t>(ceil_div(ntokens, tokens_each * (256 / lanes)), 1 << 20);
   hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, stream, (const char*)tokens, token_bytes, ntokens, table,
                      first, rows, cols, scale, out, lanes);
   return hipGetLastError();
@@ -499,7 +599,13 @@ hipError_t launch_embedding_grad(const void* tokens, int token_bytes, int64_t nt
     a.tile = plan.tile;
     a.tiles = (int32_t)plan.tiles;
     const dim3 grid((unsigned)plan.tiles), block(kSortThreads);
-    for (int p = 0; p < plan.passes; ++p) {
+    const bool small = ntokens <= kSmallTokens;
+    if (small) {
+      a.keys_out = w.keys[0];
+      a.pos_out = w.pos[0];
+      hipLaunchKernelGGL(small_sort_kernel, dim3(1), dim3(kSmallThreads), 0, stream, a, plan.passes);
+    }
+    for (int p = 0; p < plan.passes && !small; ++p) {
       a.shift = p * plan.bits;
       a.keys_in = w.keys[at];
       a.pos_in = w.pos[at];

@@ -14,21 +14,29 @@ __global__ __launch_bounds__(256) void quantize_kernel(Mat x, uint32_t total, in
                                                        uint8_t* scales) {
   const uint32_t sub = threadIdx.x % 16;
   for (uint32_t base = blockIdx.x * (16 * kGroups); base < total; base += gridDim.x * (16 * kGroups)) {
-    Raw8<T> r[kGroups];
+    auto take = [&](auto cover) {
+      constexpr Cover C = decltype(cover)::value;
+      Raw8<T> r[kGroups];
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-      const uint32_t g = min(base + u * 16 + threadIdx.x / 16, total - 1), row = groups.divide(g);
-      const int64_t c = (int64_t)(g - row * groups.d) * 128 + sub * 8;
-      r[u] = load_raw8<T>((const char*)x.p + ((int64_t)row * x.stride + c) * T::kBytes, cols - c);
-    }
+      for (int u = 0; u < kGroups; ++u) {
+        const uint32_t g = min(base + u * 16 + threadIdx.x / 16, total - 1), row = groups.divide(g);
+        r[u] = load_raw8<T, C>((const char*)x.p + (int64_t)row * x.stride * T::kBytes,
+                               (int64_t)(g - row * groups.d) * 128 + sub * 8, cols);
+      }
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-      const uint32_t g = base + u * 16 + threadIdx.x / 16, s = mx_scale_byte(max_of_4(high_bits(r[u])));
-      const uint32_t word = mx_codes(r[u], s), four = or_of_16_by_4(s << (sub / 4 * 8));
-      if (g >= total) continue;
-      stg<false>((char*)codes + (int64_t)g * 64 + sub * 4, word);
-      if (sub == 0) stg<false>((char*)scales + (int64_t)g * 4, four);
-    }
+      for (int u = 0; u < kGroups; ++u) {
+        const uint32_t g = base + u * 16 + threadIdx.x / 16, h = min(g, total - 1), row = groups.divide(h);
+        settle<C>(r[u], (int64_t)(h - row * groups.d) * 128 + sub * 8, cols);
+        const uint32_t s = mx_scale_byte(max_of_4(high_bits(r[u])));
+        const uint32_t word = mx_codes(r[u], s), four = or_of_16_by_4(s << (sub / 4 * 8));
+        if (g >= total) continue;
+        stg<false>((char*)codes + (int64_t)g * 64 + sub * 4, word);
+        if (sub == 0) stg<false>((char*)scales + (int64_t)g * 4, four);
+      }
+    };
+    if (cols % 8 == 0) take(CoverOf<kWhole>{});  // a lane's 8 columns exist or do not
+    else if (cols >= 8) take(CoverOf<kEnd>{});
+    else take(CoverOf<kFew>{});
   }
 }
 

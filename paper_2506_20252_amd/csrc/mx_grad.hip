@@ -46,15 +46,6 @@ __device__ __forceinline__ v4u turned(const uint32_t (&rows)[8][N / 2], int c) {
   return v;
 }
 
-// Eight bfloat16 moved down by d places (0 to 8), zeros behind them.
-__device__ __forceinline__ v4u move_down(v4u v, int d) {
-  uint64_t lo = v[0] | (uint64_t)v[1] << 32, hi = v[2] | (uint64_t)v[3] << 32;
-  if (d >= 4) lo = hi, hi = 0, d -= 4;
-  if (d >= 4) lo = 0, d = 0;
-  if (d > 0) lo = lo >> 16 * d | hi << (64 - 16 * d), hi >>= 16 * d;
-  return v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
-}
-
 // Two codes of a byte (the I-th of a word) as two bfloat16.
 template <int I>
 __device__ __forceinline__ uint32_t widen2(uint32_t code, uint32_t s) {
@@ -94,7 +85,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
 
   uint32_t code[8], scale[8];
   uint32_t raw_t[8][PC / 2];  // TRANSPOSED: 8 values of j by PC rows
-  v4u raw[PC];                // else: blocks of 8 j
+  Raw8<B16> raw[PC];          // else: blocks of 8 j
 
   // TAIL: perhaps fewer than 64 values of j are left.
   auto fetch = [&](int64_t j0, auto tail) {
@@ -121,7 +112,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
     if constexpr (!TRANSPOSED) {
       const int64_t at = TAIL ? min(j0, inner - 8 - block * 8) : j0;
 #pragma unroll
-      for (int u = 0; u < PC; ++u) raw[u] = ldg<v4u, false, 2>(g_row[u] + 2 * at);
+      for (int u = 0; u < PC; ++u) raw[u].w[0] = ldg<v4u, false, 2>(g_row[u] + 2 * at);
     }
   };
   auto widen = [&](Lds& l, int64_t j0, auto tail) {
@@ -140,7 +131,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
       if constexpr (!TRANSPOSED) {
         const int d = min(max(block * 8 - (left - 8), 0), 8);
 #pragma unroll
-        for (int u = 0; u < PC; ++u) raw[u] = move_down(raw[u], d);
+        for (int u = 0; u < PC; ++u) move_down(raw[u], d);
       }
     }
     uint32_t wide[8][PC / 2];
@@ -157,7 +148,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
         if (to_row + c >= 0) *(v4u*)(l.g + lds_at(to_row + c, patch_j)) = turned<PC>(raw_t, c);
     } else {
 #pragma unroll
-      for (int u = 0; u < PC; ++u) *(v4u*)(l.g + lds_at(u * (NT / 8) + row_u, block)) = raw[u];
+      for (int u = 0; u < PC; ++u) *(v4u*)(l.g + lds_at(u * (NT / 8) + row_u, block)) = raw[u].w[0];
     }
   };
 

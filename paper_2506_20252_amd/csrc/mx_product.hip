@@ -240,22 +240,29 @@ __global__ __launch_bounds__(64 * kSplitWaves) void split_kernel(MxMat a, Mat x,
     constexpr int U = 2, T512 = 64 * kSplitWaves;
     const int total = (int)m * groups * 16, sub = threadIdx.x % 16;
     for (int base = 0; base < total; base += T512 * U) {
-      Raw8<X> r[U];
-      int row[U], c[U];
+      auto take = [&](auto cover) {
+        constexpr Cover C = decltype(cover)::value;
+        Raw8<X> r[U];
+        int row[U], c[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t i = min(base + u * T512 + (int)threadIdx.x, total - 1), q = per_row.divide(i);
-        row[u] = q;
-        c[u] = (i - q * per_row.d) * 8;
-        r[u] = load_raw8<X>((const char*)x.p + (row[u] * x.stride + c[u]) * X::kBytes, k - c[u]);
-      }
+        for (int u = 0; u < U; ++u) {
+          const uint32_t i = min(base + u * T512 + (int)threadIdx.x, total - 1), q = per_row.divide(i);
+          row[u] = q;
+          c[u] = (i - q * per_row.d) * 8;
+          r[u] = load_raw8<X, C>((const char*)x.p + row[u] * x.stride * X::kBytes, c[u], k);
+        }
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t s = mx_scale_byte(max_of_4(high_bits(r[u])));
-        if (base + u * T512 + (int)threadIdx.x >= total) continue;  // whole groups of 16 lanes
-        *(uint32_t*)(lds + row[u] * lds_pitch + c[u] / 2) = mx_codes(r[u], s);
-        if (sub % 4 == 0) lds_scales[row[u] * groups * 4 + c[u] / 32] = (uint8_t)s;
-      }
+        for (int u = 0; u < U; ++u) {
+          settle<C>(r[u], c[u], k);
+          const uint32_t s = mx_scale_byte(max_of_4(high_bits(r[u])));
+          if (base + u * T512 + (int)threadIdx.x >= total) continue;  // whole groups of 16 lanes
+          *(uint32_t*)(lds + row[u] * lds_pitch + c[u] / 2) = mx_codes(r[u], s);
+          if (sub % 4 == 0) lds_scales[row[u] * groups * 4 + c[u] / 32] = (uint8_t)s;
+        }
+      };
+      if (k % 8 == 0) take(CoverOf<kWhole>{});
+      else if (k >= 8) take(CoverOf<kEnd>{});
+      else take(CoverOf<kFew>{});
     }
     __syncthreads();
   }

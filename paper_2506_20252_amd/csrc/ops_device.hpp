@@ -72,38 +72,61 @@ __device__ __forceinline__ int64_t lane_gap(int lanes) {
 }
 
 // Loads and stores of such columns at p, of which those below n (counted from p) exist: others read as 0 and are not
-// written.  FULL: all exist; without the branch, the loads of several rows are in flight together.  NT: nontemporal.
-template <typename T, bool SPLIT, bool NT, bool FULL>
+// written.  Whether all exist is decided for a whole wave, and no load hides behind a branch of a lane's own, so the
+// loads of several rows are in flight together:
+//   kWhole  all exist;
+//   kEnd    a vector that would go over the row's end ends there and is moved down (rows of 4 columns and more);
+//   kFew    columns one by one.
+enum Cover { kWhole, kEnd, kFew };
+template <Cover C>
+struct CoverOf {
+  static constexpr Cover value = C;
+};
+__device__ __forceinline__ Cover cover_of(int64_t n, int64_t gap, int64_t cols) {
+  return __all(n >= gap + 4) ? kWhole : cols >= 4 ? kEnd : kFew;
+}
+
+// Four values moved down by d places, zeros behind them.
+__device__ __forceinline__ void move_down(float* v, int64_t d) {
+  const float t0 = d & 1 ? v[1] : v[0], t1 = d & 1 ? v[2] : v[1], t2 = d & 1 ? v[3] : v[2], t3 = d & 1 ? 0.0f : v[3];
+  v[0] = d >= 4 ? 0.0f : d & 2 ? t2 : t0;
+  v[1] = d >= 4 ? 0.0f : d & 2 ? t3 : t1;
+  v[2] = d >= 2 ? 0.0f : t2;
+  v[3] = d >= 2 ? 0.0f : t3;
+}
+
+template <typename T, bool SPLIT, bool NT, Cover C>
 __device__ __forceinline__ void load8(const char* p, int64_t n, int64_t gap, float (&v)[8]) {
-  if constexpr (FULL && !SPLIT && T::kBytes == 2) {
+  typedef typename T::vec4 V;
+  if constexpr (C == kWhole && !SPLIT && T::kBytes == 2) {
     const v4u a = ldg<v4u, NT, 2>(p);
     T::widen({a[0], a[1]}, v);
     T::widen({a[2], a[3]}, v + 4);
-  } else if constexpr (FULL) {
-    typedef typename T::vec4 V;
+  } else if constexpr (C == kWhole) {
     const V a = ldg<V, NT, T::kBytes>(p), b = ldg<V, NT, T::kBytes>(p + gap * T::kBytes);
     T::widen(a, v);
     T::widen(b, v + 4);
+  } else if constexpr (C == kEnd) {
+    const int64_t at = min((int64_t)0, n - 4), to = min(gap, n - 4);
+    const V a = ldg<V, NT, T::kBytes>(p + at * T::kBytes), b = ldg<V, NT, T::kBytes>(p + to * T::kBytes);
+    T::widen(a, v);
+    T::widen(b, v + 4);
+    move_down(v, -at);
+    move_down(v + 4, gap - to);
   } else {
-    typedef typename T::vec4 V;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t at = h * gap;
-      if (n - at >= 4) {
-        T::widen(ldg<V, NT, T::kBytes>(p + at * T::kBytes), v + 4 * h);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[4 * h + i] = at + i < n ? T::load(p, at + i) : 0.0f;
-      }
+    for (int i = 0; i < 8; ++i) {
+      const int64_t at = i < 4 ? i : gap + i - 4;
+      v[i] = at < n ? T::load(p, at) : 0.0f;
     }
   }
 }
-template <typename T, bool SPLIT, bool NT, bool FULL>
+template <typename T, bool SPLIT, bool NT, Cover C>
 __device__ __forceinline__ void store8(char* p, int64_t n, int64_t gap, const float (&v)[8]) {
-  if constexpr (FULL && !SPLIT && T::kBytes == 2) {
+  if constexpr (C == kWhole && !SPLIT && T::kBytes == 2) {
     const v2u a = T::narrow(v), b = T::narrow(v + 4);
     stg<NT, 2>(p, v4u{a[0], a[1], b[0], b[1]});
-  } else if constexpr (FULL) {
+  } else if constexpr (C == kWhole) {
     stg<NT, T::kBytes>(p, T::narrow(v));
     stg<NT, T::kBytes>(p + gap * T::kBytes, T::narrow(v + 4));
   } else {
@@ -137,29 +160,61 @@ __device__ __forceinline__ uint32_t mx_scale_byte(uint32_t high_bits) {
 // 2^-127 and 255 NaN.
 __device__ __forceinline__ float mx_scale_operand(uint32_t s) { return __uint_as_float(s << 23); }
 
-// Eight consecutive elements as they are in memory, those from n on zero; nothing is done with what is loaded, so
-// that several are in flight together.
+// Eight consecutive elements as they are in memory; nothing is done with what is loaded, so that several are in flight
+// together.
 template <typename T>
 struct Raw8 {
   v4u w[T::kBytes / 2];
 };
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_raw8(const char* p, int64_t n) {
-  Raw8<T> r;
+
+// The eight elements from column c of a row of `cols`, those behind it zero, as above: kWhole where eight exist or none,
+// kEnd for rows of 8 columns and more (settle() moves them once they are there), kFew else.
+__device__ __forceinline__ void move_down(Raw8<B16>& r, int d) {
+  uint64_t lo = r.w[0][0] | (uint64_t)r.w[0][1] << 32, hi = r.w[0][2] | (uint64_t)r.w[0][3] << 32;
+  if (d >= 4) lo = hi, hi = 0, d -= 4;
+  if (d >= 4) lo = 0, d = 0;
+  if (d > 0) lo = lo >> 16 * d | hi << (64 - 16 * d), hi >>= 16 * d;
+  r.w[0] = v4u{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+}
+__device__ __forceinline__ void move_down(Raw8<F32>& r, int d) {
 #pragma unroll
-  for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = v4u{0, 0, 0, 0};
-  if (n >= 8) {
-#pragma unroll
-    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(p + 16 * i);
-  } else if (n > 0) {
+  for (int s = 1; s <= 8; s *= 2) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if (i >= n) break;
-      if constexpr (T::kBytes == 4) r.w[i / 4][i % 4] = ldg<uint32_t, false>(p + 4 * i);
-      else r.w[0][i / 2] |= (uint32_t)ldg<uint16_t, false>(p + 2 * i) << (16 * (i & 1));
+      const uint32_t from = i + s < 8 ? r.w[(i + s) / 4 % 2][(i + s) % 4] : 0u;
+      r.w[i / 4][i % 4] = d & s ? from : r.w[i / 4][i % 4];
+    }
+  }
+}
+template <typename T, Cover C>
+__device__ __forceinline__ Raw8<T> load_raw8(const char* row, int64_t c, int64_t cols) {
+  Raw8<T> r;
+  if constexpr (C == kEnd) {
+    const int64_t at = min(c, cols - 8);
+#pragma unroll
+    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(row + at * T::kBytes + 16 * i);
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = v4u{0, 0, 0, 0};
+  if constexpr (C == kWhole) {
+    if (c < cols) {
+#pragma unroll
+      for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(row + c * T::kBytes + 16 * i);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (c + i >= cols) break;
+      if constexpr (T::kBytes == 4) r.w[i / 4][i % 4] = ldg<uint32_t, false>(row + 4 * (c + i));
+      else r.w[0][i / 2] |= (uint32_t)ldg<uint16_t, false>(row + 2 * (c + i)) << (16 * (i & 1));
     }
   }
   return r;
+}
+template <Cover C, typename T>
+__device__ __forceinline__ void settle(Raw8<T>& r, int64_t c, int64_t cols) {
+  if constexpr (C == kEnd) move_down(r, (int)min(max(c - (cols - 8), (int64_t)0), (int64_t)8));
 }
 
 // Largest magnitude of 8 elements, as float32 bits.
@@ -271,8 +326,8 @@ __device__ __forceinline__ void write_tile(const v16f (&acc)[FA][FB], float* lds
       const v4f lo = *(const v4f*)(part + r * P + c), hi = *(const v4f*)(part + r * P + c + 4);
       const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       char* p = (char*)out.p + (i * out.stride + j) * T::kBytes;
-      if (i < rows && cols - j >= 8) store8<T, false, false, true>(p, 8, 4, v);
-      else if (i < rows && cols > j) store8<T, false, false, false>(p, cols - j, 4, v);
+      if (i < rows && cols - j >= 8) store8<T, false, false, kWhole>(p, 8, 4, v);
+      else if (i < rows && cols > j) store8<T, false, false, kEnd>(p, cols - j, 4, v);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
