@@ -66,29 +66,8 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
 // take consecutive sections, a wave 64 entries at a time, entries of one digit by their lane.  The first pass
 // reads the tokens themselves and leaves out those the table does not hold.
 
-constexpr int kSortThreads = 256, kSortWaves = kSortThreads / 64;
-constexpr int kMaxBits = 10, kMaxBins = 1 << kMaxBits;
-
-struct SortPlan {
-  int bits, passes;
-  int64_t tile, tiles;  // entries per workgroup, workgroups
-};
-
-constexpr int kSmallBits = 8;                         // of the sort in one workgroup, below
-constexpr int64_t kSmallTokens = 4096;
-
-SortPlan sort_plan(int64_t ntokens, int64_t rows) {
-  int kb = 1;
-  while (((int64_t)1 << kb) < rows) ++kb;
-  const int most = ntokens <= kSmallTokens ? kSmallBits : kMaxBits;
-  SortPlan s;
-  s.passes = (kb + most - 1) / most;
-  s.bits = (kb + s.passes - 1) / s.passes;
-  s.tile = (int64_t)ceil_div(ceil_div(ntokens, 128), kSortThreads) * kSortThreads;
-  if (s.tile < 1024) s.tile = 1024;
-  s.tiles = (int64_t)ceil_div(ntokens, s.tile);
-  return s;
-}
+constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kMaxBins = 1 << kMaxBits;
 
 struct SortArgs {
   const char* tokens;  // first pass
@@ -316,8 +295,6 @@ struct SumArgs {
   int lanes, sum_wgs, zero_wgs;
 };
 
-constexpr int kZeroRows = 64;  // rows that one workgroup looks through for ones without an entry
-
 template <typename TO>
 __device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
   __shared__ int32_t ends[2];
@@ -497,28 +474,6 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(SumArgs a) {
     }
     __syncthreads();
   }
-}
-
-// How the sums are cut: lanes for the columns, entries per piece.  Longer pieces write and join fewer partial sums,
-// shorter ones give more workgroups; 2048 of them keep the chip's loads in flight.
-struct SumPlan {
-  int lanes;
-  int32_t piece;
-  int64_t pieces, pitch, sum_wgs, zero_wgs, col_wgs;
-};
-
-SumPlan sum_plan(int64_t ntokens, int64_t rows, int64_t cols) {
-  SumPlan s;
-  s.lanes = row_lanes((cols + 7) / 8, 256);
-  s.col_wgs = (int64_t)ceil_div(cols, 8 * s.lanes);
-  s.piece = 64;
-  while (s.piece > 16 && (int64_t)ceil_div(ntokens, s.piece) * s.lanes * s.col_wgs < 2048 * 256) s.piece /= 2;
-  while ((int64_t)ceil_div(ntokens, s.piece) > 1 << 20) s.piece *= 2;  // bounds the launches and the workspace
-  s.pieces = (int64_t)ceil_div(ntokens, s.piece);
-  s.pitch = (cols + 7) / 8 * 8;
-  s.sum_wgs = (int64_t)ceil_div(s.pieces, 256 / s.lanes);
-  s.zero_wgs = (int64_t)ceil_div(rows, kZeroRows);
-  return s;
 }
 
 // Workspace: the number of kept entries, two (keys, positions) pairs, the tiles' histograms, the partial sums.

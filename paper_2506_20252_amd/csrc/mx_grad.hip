@@ -5,6 +5,8 @@
 // matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane: a lane reads a
 // patch of q (a few codes from each of 8 rows), widens it and writes it to LDS turned round, one column of 8 values at
 // a time; likewise g where it is given by j.
+#include <algorithm>
+
 #include "ops_device.hpp"
 
 namespace pat {
@@ -12,8 +14,14 @@ namespace {
 
 // A workgroup of WA x WB waves computes a tile of R x R of out, a wave FA x FB blocks of 32 x 32, going through j 64 at a
 // time.  While a step's 64 are multiplied out of one half of LDS, the next step's are widened from registers into the
-// other, and what the step after that needs is on its way into these registers.  Of two waves on a SIMD one multiplies
+// other, and what the step after that needs is on its way into these registers.  The codes and scales of a wave's
+// patches come in one load each, 16 bytes and one byte a lane, and go to their lanes through a piece of LDS of the
+// wave's own: a load takes its 16 cycles of address work for 64 lanes whether they ask for one byte or 16 (with a load
+// for each row of a patch, 20 a wave and step, the loads took longer than the multiplications).  Of two waves on a SIMD one multiplies
 // first and the other widens first, so that the matrix unit and the vector unit both have work.
+//
+// PARTS: as many such groups of waves in a workgroup, each with its own part of j and its own LDS; their sums are added
+// in order at the end.  For few tiles, whose waves would otherwise wait for one another's latencies alone.
 
 template <int FA, int FB, int WA, int WB>
 struct GradTile {
@@ -21,9 +29,14 @@ struct GradTile {
   static_assert(R == 32 * FB * WB, "square");
   static constexpr int PC = R * 8 / kThreads;  // columns of a patch: patches of 8 x PC, one a lane
   static_assert(PC == 2 || PC == 4, "");
+  static constexpr int kRows = 64 / (R / PC) * 8;  // of q in a wave's patches
   struct Lds {
     uint8_t g[R * 128];  // rows of out: 64 values of j
     uint8_t q[R * 128];  // columns of out: 64 values of j
+  };
+  struct Stage {
+    uint8_t codes[kRows * (R / 2)];
+    uint8_t scales[kRows * (R / 32)];
   };
 };
 
@@ -53,26 +66,41 @@ __device__ __forceinline__ uint32_t widen2(uint32_t code, uint32_t s) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-template <int FA, int FB, int WA, int WB, bool TRANSPOSED, typename T>
-__global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols,
-                                                               MatOut out) {
+template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED, typename T>
+__global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner,
+                                                                       int64_t cols, MatOut out, int64_t slice) {
   typedef GradTile<FA, FB, WA, WB> S;
   typedef typename S::Lds Lds;
   constexpr int R = S::R, PC = S::PC, W = S::kWaves, NT = S::kThreads;
-  __shared__ __attribute__((aligned(16))) Lds lds[2];
+  __shared__ __attribute__((aligned(16))) Lds all_lds[PARTS][2];
+  __shared__ __attribute__((aligned(16))) typename S::Stage stages[PARTS][W];
   TilePlace place;
   if (!tile_place((rows + R - 1) / R, (cols + R - 1) / R, &place)) return;
   const int64_t i0 = place.i * R, c0 = place.j * R;
   const int64_t pitch = (cols + 127) / 128 * 64;
-  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  if (gridDim.y > 1) {  // this launch row's slice of j, into its own matrix
+    const int64_t j = blockIdx.y * slice;
+    g.p = (const char*)g.p + 2 * (TRANSPOSED ? j * g.stride : j);
+    q.codes += j * pitch;
+    q.scales += j * (pitch / 16);
+    out.p = (char*)out.p + (int64_t)blockIdx.y * rows * out.stride * T::kBytes;
+    inner = min(slice, inner - j);
+  }
+  const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
+  const int tid = threadIdx.x % NT, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  Lds* lds = all_lds[part];
+  typename S::Stage& stage = stages[part][wave];
 
   // What a lane reads of 64 values of j.  q: a patch of 8 x PC, the columns' patches side by side over the lanes.
   // g by rows: PC blocks of 8 values, 8 of them a row.  g by j: a patch like q's.
   // Nothing is read beyond a matrix: rows of out beyond the last are the last again, j beyond the last likewise and
   // zeroed before they reach LDS, and a block or patch that would go over a row's end ends there instead.
   const int patch_c = tid % (R / PC), patch_j = tid / (R / PC);
-  const int64_t qc = min(c0 + patch_c * PC, pitch * 2 - PC);  // in the stored form, which is whole groups wide
-  const uint32_t q_at = (uint32_t)(patch_j * 8 * pitch + qc / 2), q_scale_at = (uint32_t)(patch_j * 8 * (pitch / 16) + qc / 32);
+  constexpr int CHUNKS = R / 32, ROWS_Q = S::kRows;  // 16-byte pieces of a tile's row of codes, as many as its scales
+  const int first_j = wave * ROWS_Q;                 // of the wave's patches
+  const int q_row = lane / CHUNKS;                   // what this lane loads: a row's piece of codes and its scale
+  const uint32_t q_at = (uint32_t)(min(q_row, ROWS_Q - 1) * pitch + min(c0 / 2 + lane % CHUNKS * 16, pitch - 16));
+  const uint32_t q_scale_at = (uint32_t)(min(q_row, ROWS_Q - 1) * (pitch / 16) + min(c0 / 32 + lane % CHUNKS, pitch / 16 - 1));
   const int64_t gi = min(i0 + patch_c * PC, rows - PC);       // TRANSPOSED: the patch's first row of out
   const int to_row = (int)(gi - i0);                          // its place in the tile, negative for a short last tile
   const int block = tid % 8, row_u = swap02(tid / 8);         // by rows: block and row of each NT / 8 rows
@@ -83,7 +111,8 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
     g_row[u] = (const char*)g.p + 2 * (TRANSPOSED ? patch_j * 8 * g.stride + gi
                                                   : min(i0 + u * (NT / 8) + row_u, rows - 1) * g.stride + block * 8);
 
-  uint32_t code[8], scale[8];
+  v4u codes;
+  uint32_t scales;
   uint32_t raw_t[8][PC / 2];  // TRANSPOSED: 8 values of j by PC rows
   Raw8<B16> raw[PC];          // else: blocks of 8 j
 
@@ -91,15 +120,16 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
   auto fetch = [&](int64_t j0, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
     const int left = TAIL ? (int)min(inner - j0, (int64_t)64) : 64;
+    {  // an address is the wave's and a lane's part of 32 bits; rows beyond the last are it again
+      const int64_t j = j0 + first_j, back = TAIL ? max(first_j + min(q_row, ROWS_Q - 1) - (left - 1), 0) : 0;
+      codes = ldg<v4u, false>((const char*)q.codes + j * pitch + (TAIL ? q_at - back * pitch : q_at));
+      scales = ldg<uint8_t, false>((const char*)q.scales + j * (pitch / 16) +
+                                   (TAIL ? q_scale_at - back * (pitch / 16) : q_scale_at));
+    }
+    if constexpr (TRANSPOSED) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      // a row's address is the workgroup's and a lane's part of 32 bits; rows beyond the last are it again
-      const int back = TAIL ? max(patch_j * 8 + r - (left - 1), 0) : 0;
-      const char* p = (const char*)q.codes + (j0 + r) * pitch + (TAIL ? -(int64_t)back * pitch + q_at : q_at);
-      code[r] = PC == 4 ? ldg<uint16_t, false>(p) : ldg<uint8_t, false>(p);
-      scale[r] = ldg<uint8_t, false>((const char*)q.scales + (j0 + r) * (pitch / 16) +
-                                     (TAIL ? -(int64_t)back * (pitch / 16) + q_scale_at : q_scale_at));
-      if constexpr (TRANSPOSED) {
+      for (int r = 0; r < 8; ++r) {
+        const int back = TAIL ? max(patch_j * 8 + r - (left - 1), 0) : 0;
         const char* t = g_row[0] + 2 * (j0 + r - back) * g.stride;
         if constexpr (PC == 4) {
           const v2u v = ldg<v2u, false, 2>(t);
@@ -116,6 +146,19 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
     }
   };
   auto widen = [&](Lds& l, int64_t j0, auto tail) {
+    if (q_row < ROWS_Q) {
+      *(v4u*)(stage.codes + lane * 16) = codes;
+      stage.scales[lane] = (uint8_t)scales;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint32_t code[8], scale[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {  // of this lane's patch
+      const int row = lane / (R / PC) * 8 + r;
+      const uint8_t* p = stage.codes + row * (R / 2) + patch_c * (PC / 2);
+      code[r] = PC == 4 ? *(const uint16_t*)p : *p;
+      scale[r] = stage.scales[row * (R / 32) + patch_c * PC / 32];
+    }
     if constexpr (decltype(tail)::value) {
       const int left = (int)min(inner - j0, (int64_t)64);
 #pragma unroll
@@ -191,12 +234,15 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
     mul(b1);
   };
 
-  const int64_t steps = (inner + 63) / 64, whole = inner / 64;
-  fetch(0, Bool<true>{});
-  widen(lds[0], 0, Bool<true>{});
-  if (steps > 1) fetch(64, Bool<true>{});
+  const int64_t steps = (inner + 63) / 64, each = (steps + PARTS - 1) / PARTS;
+  const int64_t begin = part * each, end = min(begin + each, steps), whole = min(inner / 64, end);
+  int64_t s = begin;
+  if (s < end) {
+    fetch(s * 64, Bool<true>{});
+    widen(lds[s & 1], s * 64, Bool<true>{});
+  }
+  if (s + 1 < end) fetch(s * 64 + 64, Bool<true>{});
   // The loops' bodies have no branch: with one, the accumulators would be moved at every turn.
-  int64_t s = 0;
   if (W == 4 || wave < 4) {
     for (; s + 2 < whole; ++s) {
       __syncthreads();  // this half is written, and nobody reads the other any more
@@ -213,14 +259,45 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void grad_kernel(Mat g, MxMat q, i
       multiply(lds[s & 1]);
     }
   }
-  for (; s < steps; ++s) {  // the last two or three
+  for (; s < end; ++s) {  // the last two or three
     __syncthreads();
     multiply(lds[s & 1]);
-    if (s + 1 < steps) widen(lds[~s & 1], s * 64 + 64, Bool<true>{});
-    if (s + 2 < steps) fetch(s * 64 + 128, Bool<true>{});
+    if (s + 1 < end) widen(lds[~s & 1], s * 64 + 64, Bool<true>{});
+    if (s + 2 < end) fetch(s * 64 + 128, Bool<true>{});
   }
 
-  write_tile<FA, FB, T>(acc, (float*)&lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
+  if constexpr (PARTS > 1) {
+    for (s = max(end - begin, (int64_t)0); s < each; ++s) __syncthreads();  // a part of fewer steps
+    static_assert(PARTS * 2 * sizeof(Lds) >= (PARTS - 1) * W * FA * FB * 16 * 64 * 4, "");
+    float* sums = (float*)&all_lds;
+    auto at = [&](int p, int x, int y, int e) -> float& {
+      return sums[((((p - 1) * W + wave) * FA + x) * FB + y) * 1024 + e * 64 + lane];
+    };
+    __syncthreads();
+    if (part) {
+#pragma unroll
+      for (int x = 0; x < FA; ++x)
+#pragma unroll
+        for (int y = 0; y < FB; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) at(part, x, y, e) = acc[x][y][e];
+    }
+    __syncthreads();
+    if (part) {
+      __syncthreads();  // write_tile's
+      return;
+    }
+#pragma unroll
+    for (int p = 1; p < PARTS; ++p)
+#pragma unroll
+      for (int x = 0; x < FA; ++x)
+#pragma unroll
+        for (int y = 0; y < FB; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[x][y][e] += at(p, x, y, e);
+  }
+  static_assert(W * tile_part(FB) * 4 <= 2 * sizeof(Lds), "");
+  write_tile<FA, FB, T>(acc, (float*)lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
 }
 
 // The same product where the vectors of 8 above do not exist: fewer than 8 values of j, or of rows where g is given by
@@ -252,39 +329,78 @@ __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows
     if (i0 + 4 * part + r < rows) T::store((char*)out.p, (i0 + 4 * part + r) * out.stride + c, sum[r]);
 }
 
-template <int FA, int FB, int WA, int WB, bool TRANSPOSED>
-hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, hipStream_t stream) {
+// out = the sum of `parts` float32 matrices of rows x pitch, in order.  A row takes `lanes` lanes, 8 columns each.
+template <typename T>
+__global__ __launch_bounds__(256) void add_kernel(const float* sums, int parts, int64_t rows, int64_t cols, int64_t pitch,
+                                                  MatOut out, int lanes) {
+  const int side = 256 / lanes, lane = threadIdx.x % lanes;
+  for (int64_t i = (int64_t)blockIdx.x * side + threadIdx.x / lanes; i < rows; i += (int64_t)gridDim.x * side) {
+    for (int64_t c = 8 * lane; c < cols; c += 8 * lanes) {
+      v4f lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+#pragma unroll 4
+      for (int p = 0; p < parts; ++p) {  // the pitch is whole vectors; what is behind a row is not used
+        const char* at = (const char*)(sums + ((int64_t)p * rows + i) * pitch + c);
+        lo += ldg<v4f, false>(at);
+        hi += ldg<v4f, false>(at + 16);
+      }
+      const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      char* p = (char*)out.p + (i * out.stride + c) * T::kBytes;
+      if (cols - c >= 8) store8<T, false, false, kWhole>(p, 8, 4, v);
+      else store8<T, false, false, kEnd>(p, cols - c, 4, v);
+    }
+  }
+}
+
+int64_t slice_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED>
+hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, const GradPlan& p,
+                    void* workspace, hipStream_t stream) {
   constexpr int R = GradTile<FA, FB, WA, WB>::R;
   const size_t tiles = ceil_div(rows, R) * ceil_div(cols, R);
-  const auto kernel = dtype == Elem::f32 ? grad_kernel<FA, FB, WA, WB, TRANSPOSED, F32>
-                                         : grad_kernel<FA, FB, WA, WB, TRANSPOSED, B16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(64 * WA * WB), 0, stream, g, q, rows, inner,
-                     cols, out);
+  const bool sliced = p.slices > 1, f32 = dtype == Elem::f32;
+  const MatOut to = sliced ? MatOut{workspace, slice_pitch(cols)} : out;
+  const auto kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, F32>
+                                    : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, B16>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8), (unsigned)p.slices), dim3(64 * WA * WB * PARTS), 0,
+                     stream, g, q, rows, inner, cols, to, p.slice);
+  if (sliced) {
+    const int lanes = row_lanes((int64_t)ceil_div(cols, 8), 256);
+    const size_t wgs = std::min<size_t>(ceil_div(rows, 256 / lanes), 1 << 20);
+    hipLaunchKernelGGL(f32 ? add_kernel<F32> : add_kernel<B16>, dim3((unsigned)wgs), dim3(256), 0, stream,
+                       (const float*)workspace, p.slices, rows, cols, slice_pitch(cols), out, lanes);
+  }
   return hipGetLastError();
 }
 
+bool narrow(bool transposed, int64_t rows, int64_t inner) { return inner < 8 || (transposed && rows < 8); }
+
 template <bool TRANSPOSED>
-hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, hipStream_t stream) {
-  if (inner < 8 || (TRANSPOSED && rows < 8)) {
+hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, void* workspace,
+                     hipStream_t stream) {
+  if (narrow(TRANSPOSED, rows, inner)) {
     const auto kernel = dtype == Elem::f32 ? narrow_kernel<TRANSPOSED, F32> : narrow_kernel<TRANSPOSED, B16>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(rows, 16) * ceil_div(cols, 16))), dim3(64), 0, stream, g, q, rows,
                        inner, cols, out);
     return hipGetLastError();
   }
-  auto wgs = [&](int f) { return ceil_div(rows, 64 * f) * ceil_div(cols, 64 * f); };
-  if (wgs(4) >= 192) return run_grad<4, 2, 2, 4, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
-  if (wgs(2) >= 192) return run_grad<2, 2, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
-  return run_grad<1, 1, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, stream);
+  const GradPlan p = grad_plan(rows, inner, cols);
+  if (p.tile == 256) return run_grad<4, 2, 2, 4, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
+  if (p.tile == 128) return run_grad<2, 2, 2, 2, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
+  return run_grad<1, 1, 2, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
 }
 
 }  // namespace
 
-size_t mx_grad_workspace(int64_t, int64_t, int64_t) { return 0; }
+size_t mx_grad_workspace(int64_t rows, int64_t inner, int64_t cols) {
+  const GradPlan p = grad_plan(rows, inner, cols);
+  return p.slices > 1 ? (size_t)(p.slices * rows * slice_pitch(cols)) * 4 : 0;
+}
 
 hipError_t launch_mx_grad(Mat g, bool transposed, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out,
-                          Elem dtype, void*, hipStream_t stream) {
-  return transposed ? pick_grad<true>(g, q, rows, inner, cols, out, dtype, stream)
-                    : pick_grad<false>(g, q, rows, inner, cols, out, dtype, stream);
+                          Elem dtype, void* workspace, hipStream_t stream) {
+  return transposed ? pick_grad<true>(g, q, rows, inner, cols, out, dtype, workspace, stream)
+                    : pick_grad<false>(g, q, rows, inner, cols, out, dtype, workspace, stream);
 }
 
 }  // namespace pat

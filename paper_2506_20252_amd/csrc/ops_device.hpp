@@ -6,6 +6,7 @@
 
 #include "device_access.hpp"
 #include "ops.hpp"
+#include "ops_shape.hpp"
 
 namespace pat {
 namespace {
@@ -142,13 +143,6 @@ __device__ __forceinline__ void store8(char* p, int64_t n, int64_t gap, const fl
       }
     }
   }
-}
-
-// Lanes of a power of two that take a row of `vectors` vectors, at most a workgroup of `threads`.
-inline int row_lanes(int64_t vectors, int threads) {
-  int lanes = 1;
-  while (lanes < vectors && lanes < threads) lanes *= 2;
-  return lanes;
 }
 
 // 4-bit blocks: scale byte of the block's largest magnitude (as float32 bits), and the powers of two around it.

@@ -1,0 +1,100 @@
+// How the operators are cut into workgroups: sizes only, no device code.
+#pragma once
+
+#include <algorithm>
+#include <cstddef>
+#include <cstdint>
+
+#include "ops.hpp"
+
+namespace pat {
+
+// Lanes of a power of two that take a row of `vectors` vectors, at most a workgroup of `threads`.
+inline int row_lanes(int64_t vectors, int threads) {
+  int lanes = 1;
+  while (lanes < vectors && lanes < threads) lanes *= 2;
+  return lanes;
+}
+
+// ---- gradients of the 4-bit product ----------------------------------------------------------------------------
+
+// How a product is cut: the tile's size, and slices of j that get workgroups and a float32 matrix of their own, which
+// add_kernel adds up.
+//
+// The largest tile that gives more than half of the 256 CUs one, as for the 4-bit product (us with tiles of 64, 128, 256:
+// 153, 88, 102 for 2048 rows, 4096 columns and values of j; 305, 170, 121 for 4096 rows).  Below, few tiles of 128 and
+// a long sum are sliced (us, and with tiles of 64: 20 and 26 for 64 rows, 4096 columns and values of j; 22 and 55 for 512
+// rows and columns, 8192 values of j; but 22 and 18 for 1024 rows and columns, 2048 values of j), the others take tiles of
+// 64 with two groups of waves (16.2 us for 1001 x 1333 and 1000 values of j; with one group 16.5).
+struct GradPlan {
+  int tile, slices;
+  int64_t slice;
+};
+
+inline GradPlan grad_plan(int64_t rows, int64_t inner, int64_t cols) {
+  auto tiles = [&](int size) { return (int64_t)(ceil_div(rows, size) * ceil_div(cols, size)); };
+  GradPlan p{256, 1, inner};
+  if (tiles(256) > 128) return p;
+  p.tile = 128;
+  if (tiles(128) > 128) return p;
+  const int64_t slices = std::min<int64_t>(256 / tiles(128), inner / 512);
+  if (slices >= 8) {
+    p.slice = (int64_t)ceil_div(ceil_div(inner, slices), 64) * 64;
+    p.slices = (int)ceil_div(inner, p.slice);
+    // the kernel's vectors of 8 need 8 values of j in the last slice too
+    while (inner - (p.slices - 1) * p.slice < 8) p.slice += 64, p.slices = (int)ceil_div(inner, p.slice);
+    return p;
+  }
+  p.tile = 64;
+  return p;
+}
+
+// ---- embedding gradient ----------------------------------------------------------------------------------------
+
+constexpr int kSortThreads = 256, kMaxBits = 10;  // of a sorting workgroup; of a pass's digit
+constexpr int kZeroRows = 64;                     // rows that one workgroup looks through for ones without an entry
+
+struct SortPlan {
+  int bits, passes;
+  int64_t tile, tiles;  // entries per workgroup, workgroups
+};
+
+constexpr int kSmallBits = 8;                         // of the sort in one workgroup, below
+constexpr int64_t kSmallTokens = 4096;
+
+inline SortPlan sort_plan(int64_t ntokens, int64_t rows) {
+  int kb = 1;
+  while (((int64_t)1 << kb) < rows) ++kb;
+  const int most = ntokens <= kSmallTokens ? kSmallBits : kMaxBits;
+  SortPlan s;
+  s.passes = (kb + most - 1) / most;
+  s.bits = (kb + s.passes - 1) / s.passes;
+  s.tile = (int64_t)ceil_div(ceil_div(ntokens, 128), kSortThreads) * kSortThreads;
+  if (s.tile < 1024) s.tile = 1024;
+  s.tiles = (int64_t)ceil_div(ntokens, s.tile);
+  return s;
+}
+
+// How the sums are cut: lanes for the columns, entries per piece.  Longer pieces write and join fewer partial sums,
+// shorter ones give more workgroups; 2048 of them keep the chip's loads in flight.
+struct SumPlan {
+  int lanes;
+  int32_t piece;
+  int64_t pieces, pitch, sum_wgs, zero_wgs, col_wgs;
+};
+
+inline SumPlan sum_plan(int64_t ntokens, int64_t rows, int64_t cols) {
+  SumPlan s;
+  s.lanes = row_lanes((cols + 7) / 8, 256);
+  s.col_wgs = (int64_t)ceil_div(cols, 8 * s.lanes);
+  s.piece = 64;
+  while (s.piece > 16 && (int64_t)ceil_div(ntokens, s.piece) * s.lanes * s.col_wgs < 2048 * 256) s.piece /= 2;
+  while ((int64_t)ceil_div(ntokens, s.piece) > 1 << 20) s.piece *= 2;  // bounds the launches and the workspace
+  s.pieces = (int64_t)ceil_div(ntokens, s.piece);
+  s.pitch = (cols + 7) / 8 * 8;
+  s.sum_wgs = (int64_t)ceil_div(s.pieces, 256 / s.lanes);
+  s.zero_wgs = (int64_t)ceil_div(rows, kZeroRows);
+  return s;
+}
+
+}  // namespace pat

@@ -14,6 +14,8 @@ import ctypes
 import math
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -117,6 +119,21 @@ def test_oracle_quantisation_by_hand():
     assert codes[0, 32:64].tolist() == [0] * 32 and codes[0, 64] == 0 and codes[0, 96] == 6 and codes[0, 128] == 14
     v = O.mx_values(*O.mx_pack(codes, scales), 160)
     assert np.isnan(v[0, 32:64]).all() and v[0, 96] == 2.0**127 and v[0, 128] == -2.0**-100
+
+
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir("/opt/rocm/include/hip"),
+                    reason="no g++ or no HIP headers")
+def test_host_side_under_asan_ubsan(tmp_path):
+    """How sizes are cut into workgroups, slices and pieces, and what the entry points hand on."""
+    exe = tmp_path / "ops_check"
+    csrc = os.path.join(ROOT, "paper_2506_20252_amd", "csrc")
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", csrc, os.path.join(csrc, "ops.cpp"),
+           os.path.join(ROOT, "tests", "host", "ops_check.cpp"), "-o", str(exe)]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, (res.stdout[-2000:], res.stderr[-2000:])
+    assert " 0 failures" in res.stdout
 
 
 BASE = 1 << 32  # addresses that no call below may reach
@@ -294,7 +311,8 @@ def test_dequantize_every_code_and_scale():
 
 PRODUCTS = [(1, 1, 1), (1, 16, 32), (1, 300, 128), (2, 17, 129), (3, 33, 500), (16, 16, 512), (17, 100, 640), (24, 70, 1001),
             (40, 65, 300), (64, 64, 256), (65, 130, 96), (100, 129, 777), (128, 128, 1024), (130, 257, 384), (256, 256, 512),
-            (300, 270, 1300), (520, 260, 130), (5, 2000, 64), (2000, 3, 200), (1, 64, 20000), (48, 40, 8200)]
+            (300, 270, 1300), (520, 260, 130), (5, 2000, 64), (2000, 3, 200), (1, 64, 20000), (48, 40, 8200),
+            (3, 8000, 40), (20, 4200, 300), (40, 8300, 130), (49, 49, 500), (1500, 1500, 250), (2900, 2900, 140), (60, 100, 7)]
 
 
 @gpu
@@ -355,7 +373,8 @@ def test_products_carry_what_is_not_finite(m, n, k):
 
 
 GRADS = [(1, 1, 1), (1, 16, 32), (3, 40, 33), (16, 32, 128), (33, 65, 100), (64, 64, 64), (70, 129, 257), (128, 128, 128),
-         (130, 70, 300), (256, 128, 256), (300, 200, 520), (20, 3000, 40), (257, 1000, 129), (1000, 5, 130), (64, 31, 640)]
+         (130, 70, 300), (256, 128, 256), (300, 200, 520), (20, 3000, 40), (257, 1000, 129), (1000, 5, 130), (64, 31, 640), (100, 4096, 90), (64, 5761, 33), (40, 8449, 200), (130, 8, 64),
+         (9, 7, 300), (7, 500, 40), (520, 700, 600)]
 
 
 @gpu
