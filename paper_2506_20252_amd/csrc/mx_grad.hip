@@ -104,12 +104,14 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   const int64_t gi = min(i0 + patch_c * PC, rows - PC);       // TRANSPOSED: the patch's first row of out
   const int to_row = (int)(gi - i0);                          // its place in the tile, negative for a short last tile
   const int block = tid % 8, row_u = swap02(tid / 8);         // by rows: block and row of each NT / 8 rows
+  // of g: from the tile's corner, 32 bits (rows are not too far apart for that)
   constexpr int ROWS = TRANSPOSED ? 1 : PC;
-  const char* g_row[ROWS];
+  uint32_t g_at[ROWS];
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
-    g_row[u] = (const char*)g.p + 2 * (TRANSPOSED ? patch_j * 8 * g.stride + gi
-                                                  : min(i0 + u * (NT / 8) + row_u, rows - 1) * g.stride + block * 8);
+    g_at[u] = 2 * (uint32_t)(TRANSPOSED ? patch_j * 8 * g.stride + gi
+                                        : (min(i0 + u * (NT / 8) + row_u, rows - 1) - i0) * g.stride + block * 8);
+  const char* g_base = (const char*)g.p + (TRANSPOSED ? 0 : 2 * i0 * g.stride);
 
   v4u codes;
   uint32_t scales;
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         const int back = TAIL ? max(patch_j * 8 + r - (left - 1), 0) : 0;
-        const char* t = g_row[0] + 2 * (j0 + r - back) * g.stride;
+        const char* t = g_base + 2 * (j0 + r) * g.stride + (TAIL ? g_at[0] - 2 * back * g.stride : g_at[0]);
         if constexpr (PC == 4) {
           const v2u v = ldg<v2u, false, 2>(t);
           raw_t[r][0] = v[0], raw_t[r][PC / 2 - 1] = v[1];
@@ -140,9 +142,10 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
       }
     }
     if constexpr (!TRANSPOSED) {
-      const int64_t at = TAIL ? min(j0, inner - 8 - block * 8) : j0;
+      const int64_t back = TAIL ? max(j0 + block * 8 - (inner - 8), (int64_t)0) : 0;
 #pragma unroll
-      for (int u = 0; u < PC; ++u) raw[u].w[0] = ldg<v4u, false, 2>(g_row[u] + 2 * at);
+      for (int u = 0; u < PC; ++u)
+        raw[u].w[0] = ldg<v4u, false, 2>(g_base + 2 * j0 + (TAIL ? g_at[u] - 2 * back : g_at[u]));
     }
   };
   auto widen = [&](Lds& l, int64_t j0, auto tail) {
@@ -204,34 +207,30 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
 
-  // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.  The next 16 values of j are
-  // read from LDS while these are multiplied.
-  struct Blocks {
-    v8bf g[FA], q[FB];
-  };
-  auto read = [&](const Lds& l, int step, Blocks& b) {
-#pragma unroll
-    for (int x = 0; x < FA; ++x) b.g[x] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * x + lane % 32, step * 2 + half));
-#pragma unroll
-    for (int y = 0; y < FB; ++y) b.q[y] = *(const v8bf*)(l.q + lds_at(wave_col + 32 * y + lane % 32, step * 2 + half));
-  };
-  auto mul = [&](const Blocks& b) {
-#pragma unroll
-    for (int x = 0; x < FA; ++x)
-#pragma unroll
-      for (int y = 0; y < FB; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b.g[x], b.q[y], acc[x][y], 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-  };
+  // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.  A block of g is read from LDS
+  // two blocks before its instructions, those of q a step of 16 values of j before.
   auto multiply = [&](const Lds& l) {
-    Blocks b0, b1;
-    read(l, 0, b0);
-    read(l, 1, b1);
-    mul(b0);
-    read(l, 2, b0);
-    mul(b1);
-    read(l, 3, b1);
-    mul(b0);
-    mul(b1);
+    v8bf bg[3], bq[2][FB];
+    auto read_g = [&](int n) {
+      bg[n % 3] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * (n % FA) + lane % 32, n / FA * 2 + half));
+    };
+    auto read_q = [&](int step) {
+#pragma unroll
+      for (int y = 0; y < FB; ++y)
+        bq[step % 2][y] = *(const v8bf*)(l.q + lds_at(wave_col + 32 * y + lane % 32, step * 2 + half));
+    };
+    read_q(0);
+    read_g(0);
+    read_g(1);
+#pragma unroll
+    for (int n = 0; n < 4 * FA; ++n) {
+      if (n + 2 < 4 * FA) read_g(n + 2);
+      if (n % FA == 0 && n / FA < 3) read_q(n / FA + 1);
+#pragma unroll
+      for (int y = 0; y < FB; ++y)
+        acc[n % FA][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bg[n % 3], bq[n / FA % 2][y], acc[n % FA][y], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
 
   const int64_t steps = (inner + 63) / 64, each = (steps + PARTS - 1) / PARTS;
@@ -300,8 +299,8 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   write_tile<FA, FB, T>(acc, (float*)lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
 }
 
-// The same product where the vectors of 8 above do not exist: fewer than 8 values of j, or of rows where g is given by
-// j.  One wave per 16 x 16 of out; an instruction of 16 x 16 x 32 takes j = 8 * (l / 16) ... + 7 of row and column
+// The same product where the vectors of 8 above do not exist (fewer than 8 values of j, or of rows where g is given by j),
+// or where a tile's rows of g are so far apart that their offsets need more than 32 bits.  One wave per 16 x 16 of out; an instruction of 16 x 16 x 32 takes j = 8 * (l / 16) ... + 7 of row and column
 // l mod 16 in lane l, read one by one.
 template <bool TRANSPOSED, typename T>
 __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out) {
@@ -373,12 +372,14 @@ hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, M
   return hipGetLastError();
 }
 
-bool narrow(bool transposed, int64_t rows, int64_t inner) { return inner < 8 || (transposed && rows < 8); }
+bool narrow(bool transposed, int64_t rows, int64_t inner, int64_t stride) {
+  return inner < 8 || (transposed && rows < 8) || stride > 1 << 22;  // 256 rows of 2 bytes: below 2^31
+}
 
 template <bool TRANSPOSED>
 hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, void* workspace,
                      hipStream_t stream) {
-  if (narrow(TRANSPOSED, rows, inner)) {
+  if (narrow(TRANSPOSED, rows, inner, g.stride)) {
     const auto kernel = dtype == Elem::f32 ? narrow_kernel<TRANSPOSED, F32> : narrow_kernel<TRANSPOSED, B16>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(rows, 16) * ceil_div(cols, 16))), dim3(64), 0, stream, g, q, rows,
                        inner, cols, out);
