@@ -208,11 +208,11 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
       for (int e = 0; e < 16; ++e) acc[x][y][e] = 0.0f;
 
   // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.  A block of g is read from LDS
-  // two blocks before its instructions, those of q a step of 16 values of j before.
+  // a block before its instructions, those of q a step of 16 values of j before.
   auto multiply = [&](const Lds& l) {
-    v8bf bg[3], bq[2][FB];
+    v8bf bg[2], bq[2][FB];
     auto read_g = [&](int n) {
-      bg[n % 3] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * (n % FA) + lane % 32, n / FA * 2 + half));
+      bg[n % 2] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * (n % FA) + lane % 32, n / FA * 2 + half));
     };
     auto read_q = [&](int step) {
 #pragma unroll
@@ -221,14 +221,13 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
     };
     read_q(0);
     read_g(0);
-    read_g(1);
 #pragma unroll
     for (int n = 0; n < 4 * FA; ++n) {
-      if (n + 2 < 4 * FA) read_g(n + 2);
+      if (n + 1 < 4 * FA) read_g(n + 1);
       if (n % FA == 0 && n / FA < 3) read_q(n / FA + 1);
 #pragma unroll
       for (int y = 0; y < FB; ++y)
-        acc[n % FA][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bg[n % 3], bq[n / FA % 2][y], acc[n % FA][y], 0, 0, 0);
+        acc[n % FA][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(bg[n % 2], bq[n / FA % 2][y], acc[n % FA][y], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
