@@ -11,6 +11,7 @@ adds e times its value.  Codes, scales, widened values and masks are exact.
 """
 
 import ctypes
+import importlib.util
 import math
 import os
 import re
@@ -673,3 +674,55 @@ def test_offsets_beyond_32_bits():
     assert torch.equal(ops.mx_matmul_grad(g, q, B16, out=out), ops.mx_matmul_grad(g, q, B16))
     assert torch.equal(ops.embedding(tokens, small, 2.0, out=out), ops.embedding(tokens, small, 2.0))
     assert bool((room[:, cols:64] == 0).all()) and bool((room[:, 200:4096] == 0).all())
+
+
+# ---- the operators together, between the collectives
+
+def example():
+    spec = importlib.util.spec_from_file_location("sharded_step", os.path.join(ROOT, "examples", "sharded_step.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ranks", [1, 2, 4])
+def test_sharded_step(ranks):
+    """One step's loss and weights against the definitions, for the whole batch at once.
+
+    The embedding's scale (16) and the dropout's factor (2) are powers of two, so everything up to the 4-bit rows of
+    the layer's input is exact; after it the bounds follow each rounding: 32-bit sums of k or fewer terms, the
+    gradient's rounding to bfloat16 before the products and after the one for the input."""
+    vocabulary, width, outputs, batch, p, rate = 64, 256, 96, 128, 0.5, 2.0
+    step = example()
+    start = step.problem(vocabulary, width, outputs, batch)
+    losses, layer, table = step.train(ranks, 1, *start, p=p, rate=rate)
+
+    w, e, tokens, targets = f64(start[0]), f64(start[1].bfloat16()), start[2].cpu().numpy(), f64(start[3])
+    keep, factor = O.dropout_keep(batch, width, p, 1000, 0, width)
+    h = O.embedding(tokens, e, 16.0, 0) * keep * factor
+    hv, wv = (O.mx_values(*O.mx_pack(*O.mx_quantize(v)), width) for v in (h, w))
+    y = hv @ wv.T
+    y_err = (width + 3) * 2.0**-24 * (np.abs(hv) @ np.abs(wv).T + np.abs(targets))
+    err = y - targets
+    loss = np.sum(err**2) / (2 * batch * outputs)
+    assert abs(losses[0] - loss) <= 2.0**-11 * loss + np.sum(np.abs(err) * y_err) / (batch * outputs)
+
+    g = err / batch
+    g_err = 2.0**-8 * np.abs(g) + y_err / batch
+    sums = (batch + outputs) * 2.0**-24
+    dl, dl_err = g.T @ hv, g_err.T @ np.abs(hv) + sums * (np.abs(g).T @ np.abs(hv))
+    dh, dh_err = g @ wv, g_err @ np.abs(wv) + (sums + 2.0**-8) * (np.abs(g) @ np.abs(wv))
+    dt = O.embedding_grad(tokens, dh * keep * factor, vocabulary, 16.0, 0)
+    dt_err = O.embedding_grad(tokens, dh_err * keep * factor, vocabulary, 16.0, 0)
+    dt_err += sums * O.embedding_grad(tokens, np.abs(dh) * keep * factor, vocabulary, 16.0, 0)
+    for got, old, d, d_err in ((layer, w, dl, dl_err), (table, f64(start[1]), dt, dt_err)):
+        want, bound = old - rate / outputs * d, rate / outputs * d_err + 2.0**-22 * (np.abs(old) + np.abs(d))
+        assert np.all(np.abs(f64(got) - want) <= bound)
+
+
+@pytest.mark.gpu
+def test_sharded_steps_learn():
+    step = example()
+    losses, _, _ = step.train(8, 5, *step.problem())
+    assert all(b < a for a, b in zip(losses, losses[1:]))
