@@ -78,15 +78,13 @@ pat_status_t pat_mx_dequantize(const void* codes, const void* scales, size_t row
  * sum (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, size_t m,
-                           size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, void* workspace,
-                           size_t workspace_bytes, hipStream_t stream);
-size_t pat_mx_matmul_workspace(size_t m, size_t n, size_t k);
+                           size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, hipStream_t stream);
 
 /*
  * The same product of Q(x), where Q is pat_mx_quantize, with a weight w of n rows
  * in the stored form: out[i][j] = sum over c < k of Q(x)[i][c] * w[j][c].  Few
  * rows (single tokens, small batches) take one launch, which quantises x on its
- * way; the result is that of the two calls either way.
+ * way; the result is that of the two calls to the bit either way.
  */
 pat_status_t pat_mx_linear(const void* x, int64_t x_stride, pat_dtype_t x_dtype, const void* w_codes, const void* w_scales,
                            size_t m, size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, void* workspace,

@@ -210,6 +210,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b,
 // workgroup repeats that, which is little beside its part of b as long as the rows are few.
 
 constexpr int kSplitWaves = 8;
+constexpr int kSplitRows = 48;
 
 template <int MT, int NT, bool FUSED, typename X, typename T>
 __global__ __launch_bounds__(64 * kSplitWaves) void split_kernel(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k,
@@ -371,21 +372,19 @@ hipError_t run_tile(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut ou
 
 // Rows that every workgroup quantises for itself, and not a launch before: m * k up to 32768 values (us fused and not,
 // k = 4096: 4.5 and 5.8 for one row, 5.1 and 6.6 for 4, 8.6 and 7.3 for 16; k = 8192: 8.1 and 10.7, 10.4 and 11.6,
-// none and 12.6).  What they take in LDS stays below 32 KB.
-bool fused(int64_t m, int64_t k) { return m <= 64 && m * k <= 32768; }
+// none and 12.6).  What they take in LDS stays below 32 KB.  No more rows than the split takes of a product whose rows
+// are quantised before: the sums are then the same either way.
+bool fused(int64_t m, int64_t k) { return m <= kSplitRows && m * k <= 32768; }
 
 }  // namespace
 
-size_t mx_matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
-
-hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, void*,
-                            hipStream_t stream) {
+hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
   // The largest tile that gives more than half of the 256 CUs one.  A tile's time grows with its area only once the chip
   // is full; us with tiles of 64, 128, 256 at n = k = 8192: 24, 30, 51 for m = 256 (512, 128, 32 tiles), 48, 32, 51 for
   // m = 512, 85, 52, 54 for m = 1024, 161, 96, 72 for m = 2048.  Up to 48 rows or columns the split is as fast or
   // faster (n = 8192: 19 against 20; n = k = 1024: 5 against 6).
   auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, size); };
-  if (k > 0 && m > 48 && n > 48) {
+  if (k > 0 && m > kSplitRows && n > kSplitRows) {
     if (tiles(256) > 128) return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
     if (tiles(128) > 128) return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
     return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
@@ -408,7 +407,7 @@ hipError_t launch_mx_linear(Mat x, Elem x_dtype, MxMat w, int64_t m, int64_t n, 
     const hipError_t e = launch_mx_quantize(x, x_dtype, m, k, codes, scales, stream);
     if (e != hipSuccess) return e;
   }
-  return launch_mx_matmul({codes, scales}, w, m, n, k, out, dtype, nullptr, stream);
+  return launch_mx_matmul({codes, scales}, w, m, n, k, out, dtype, stream);
 }
 
 }  // namespace pat

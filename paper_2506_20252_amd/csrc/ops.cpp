@@ -125,27 +125,20 @@ pat_status_t pat_mx_dequantize(const void* codes, const void* scales, size_t row
                                             int64_t(rows), int64_t(cols), {out, out_stride}, e, stream));
 }
 
-size_t pat_mx_matmul_workspace(size_t m, size_t n, size_t k) {
-  if (!product_ok(m, n, k) || !m || !n) return 0;
-  return pat::mx_matmul_workspace(int64_t(m), int64_t(n), int64_t(k));
-}
-
 pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, size_t m,
-                           size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, void* workspace,
-                           size_t workspace_bytes, hipStream_t stream) {
+                           size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, hipStream_t stream) {
   Elem e;
   if (!elem_of(dtype, &e)) return PAT_ERR_UNSUPPORTED;
   if (!product_ok(m, n, k) || !groups_ok(m, k) || !groups_ok(n, k)) return PAT_ERR_UNSUPPORTED;
   if (m == 0 || n == 0) return PAT_OK;
-  Span ac, as, bc, bs, o, w;
+  Span ac, as, bc, bs, o;
   if (!mx_spans(a_codes, a_scales, m, k, &ac, &as) || !mx_spans(b_codes, b_scales, n, k, &bc, &bs) ||
       !matrix_span(out, out_stride, m, n, elem_bytes(e), &o))
     return PAT_ERR_INVALID_ARGUMENT;
-  if (pat_status_t st = workspace_span(workspace, workspace_bytes, pat_mx_matmul_workspace(m, n, k), &w)) return st;
-  if (any_overlap(o, {ac, as, bc, bs, w}) || any_overlap(w, {ac, as, bc, bs})) return PAT_ERR_INVALID_ARGUMENT;
+  if (any_overlap(o, {ac, as, bc, bs})) return PAT_ERR_INVALID_ARGUMENT;
   return launched(pat::launch_mx_matmul({static_cast<const uint8_t*>(a_codes), static_cast<const uint8_t*>(a_scales)},
                                         {static_cast<const uint8_t*>(b_codes), static_cast<const uint8_t*>(b_scales)},
-                                        int64_t(m), int64_t(n), int64_t(k), {out, out_stride}, e, workspace, stream));
+                                        int64_t(m), int64_t(n), int64_t(k), {out, out_stride}, e, stream));
 }
 
 size_t pat_mx_linear_workspace(size_t m, size_t n, size_t k) {

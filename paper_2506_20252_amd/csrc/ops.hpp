@@ -39,9 +39,7 @@ hipError_t launch_mx_quantize(Mat x, Elem dtype, int64_t rows, int64_t cols, uin
                               hipStream_t stream);
 hipError_t launch_mx_dequantize(MxMat q, int64_t rows, int64_t cols, MatOut out, Elem dtype, hipStream_t stream);
 
-size_t mx_matmul_workspace(int64_t m, int64_t n, int64_t k);
-hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, void* workspace,
-                            hipStream_t stream);
+hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream);
 size_t mx_linear_workspace(int64_t m, int64_t n, int64_t k);
 hipError_t launch_mx_linear(Mat x, Elem x_dtype, MxMat w, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype,
                             void* workspace, hipStream_t stream);

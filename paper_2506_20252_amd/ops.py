@@ -23,17 +23,16 @@ PAT_MX_GROUP = 128
 
 # Every function include/pat_ops.h declares.
 EXPORTS = (
-    "pat_mx_quantize", "pat_mx_dequantize", "pat_mx_matmul", "pat_mx_matmul_workspace", "pat_mx_linear",
-    "pat_mx_linear_workspace", "pat_mx_matmul_grad", "pat_mx_matmul_grad_workspace", "pat_embedding",
-    "pat_embedding_grad", "pat_embedding_grad_workspace", "pat_dropout",
+    "pat_mx_quantize", "pat_mx_dequantize", "pat_mx_matmul", "pat_mx_linear", "pat_mx_linear_workspace",
+    "pat_mx_matmul_grad", "pat_mx_matmul_grad_workspace", "pat_embedding", "pat_embedding_grad",
+    "pat_embedding_grad_workspace", "pat_dropout",
 )
 
 _P, _N, _S, _I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64, ctypes.c_int
 _SIGNATURES = {
     "pat_mx_quantize": ([_P, _S, _N, _N, _I, _P, _P, _P], _I),
     "pat_mx_dequantize": ([_P, _P, _N, _N, _P, _S, _I, _P], _I),
-    "pat_mx_matmul": ([_P, _P, _P, _P, _N, _N, _N, _P, _S, _I, _P, _N, _P], _I),
-    "pat_mx_matmul_workspace": ([_N, _N, _N], _N),
+    "pat_mx_matmul": ([_P, _P, _P, _P, _N, _N, _N, _P, _S, _I, _P], _I),
     "pat_mx_linear": ([_P, _S, _I, _P, _P, _N, _N, _N, _P, _S, _I, _P, _N, _P], _I),
     "pat_mx_linear_workspace": ([_N, _N, _N], _N),
     "pat_mx_matmul_grad": ([_P, _S, _I, _P, _P, _N, _N, _N, _P, _S, _I, _P, _N, _P], _I),
@@ -73,30 +72,24 @@ def _address(b):
 
 def pat_mx_quantize(x, x_stride, rows, cols, dtype, codes, scales, stream=None):
     return _c.pat_mx_quantize(_address(x), x_stride, rows, cols, pat._dtype(dtype), _address(codes),
-                                  _address(scales), pat._stream(stream))
+                              _address(scales), pat._stream(stream))
 
 
 def pat_mx_dequantize(codes, scales, rows, cols, out, out_stride, dtype, stream=None):
     return _c.pat_mx_dequantize(_address(codes), _address(scales), rows, cols, _address(out), out_stride,
-                                    pat._dtype(dtype), pat._stream(stream))
+                                pat._dtype(dtype), pat._stream(stream))
 
 
-def pat_mx_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, out_stride, dtype, workspace, workspace_bytes,
-                  stream=None):
+def pat_mx_matmul(a_codes, a_scales, b_codes, b_scales, m, n, k, out, out_stride, dtype, stream=None):
     return _c.pat_mx_matmul(_address(a_codes), _address(a_scales), _address(b_codes), _address(b_scales), m, n, k,
-                                _address(out), out_stride, pat._dtype(dtype), _address(workspace), workspace_bytes,
-                                pat._stream(stream))
-
-
-def pat_mx_matmul_workspace(m, n, k):
-    return _c.pat_mx_matmul_workspace(m, n, k)
+                            _address(out), out_stride, pat._dtype(dtype), pat._stream(stream))
 
 
 def pat_mx_linear(x, x_stride, x_dtype, w_codes, w_scales, m, n, k, out, out_stride, dtype, workspace, workspace_bytes,
                   stream=None):
     return _c.pat_mx_linear(_address(x), x_stride, pat._dtype(x_dtype), _address(w_codes), _address(w_scales), m, n, k,
-                                _address(out), out_stride, pat._dtype(dtype), _address(workspace), workspace_bytes,
-                                pat._stream(stream))
+                            _address(out), out_stride, pat._dtype(dtype), _address(workspace), workspace_bytes,
+                            pat._stream(stream))
 
 
 def pat_mx_linear_workspace(m, n, k):
@@ -106,8 +99,8 @@ def pat_mx_linear_workspace(m, n, k):
 def pat_mx_matmul_grad(g, g_stride, transposed, q_codes, q_scales, rows, inner, cols, out, out_stride, dtype, workspace,
                        workspace_bytes, stream=None):
     return _c.pat_mx_matmul_grad(_address(g), g_stride, int(transposed), _address(q_codes), _address(q_scales), rows,
-                                     inner, cols, _address(out), out_stride, pat._dtype(dtype), _address(workspace),
-                                     workspace_bytes, pat._stream(stream))
+                                 inner, cols, _address(out), out_stride, pat._dtype(dtype), _address(workspace),
+                                 workspace_bytes, pat._stream(stream))
 
 
 def pat_mx_matmul_grad_workspace(rows, inner, cols):
@@ -117,15 +110,15 @@ def pat_mx_matmul_grad_workspace(rows, inner, cols):
 def pat_embedding(tokens, token_bytes, ntokens, table, table_stride, table_dtype, first, rows, cols, scale, out,
                   out_stride, dtype, stream=None):
     return _c.pat_embedding(_address(tokens), token_bytes, ntokens, _address(table), table_stride,
-                                pat._dtype(table_dtype), first, rows, cols, scale, _address(out), out_stride,
-                                pat._dtype(dtype), pat._stream(stream))
+                            pat._dtype(table_dtype), first, rows, cols, scale, _address(out), out_stride,
+                            pat._dtype(dtype), pat._stream(stream))
 
 
 def pat_embedding_grad(tokens, token_bytes, ntokens, g, g_stride, g_dtype, first, rows, cols, scale, out, out_stride,
                        dtype, workspace, workspace_bytes, stream=None):
     return _c.pat_embedding_grad(_address(tokens), token_bytes, ntokens, _address(g), g_stride, pat._dtype(g_dtype),
-                                     first, rows, cols, scale, _address(out), out_stride, pat._dtype(dtype),
-                                     _address(workspace), workspace_bytes, pat._stream(stream))
+                                 first, rows, cols, scale, _address(out), out_stride, pat._dtype(dtype),
+                                 _address(workspace), workspace_bytes, pat._stream(stream))
 
 
 def pat_embedding_grad_workspace(ntokens, rows, cols):
@@ -135,7 +128,7 @@ def pat_embedding_grad_workspace(ntokens, rows, cols):
 def pat_dropout(x, x_stride, residual, residual_stride, out, out_stride, rows, cols, dtype, p, seed, index, index_stride,
                 stream=None):
     return _c.pat_dropout(_address(x), x_stride, _address(residual), residual_stride, _address(out), out_stride, rows,
-                              cols, pat._dtype(dtype), p, seed, index, index_stride, pat._stream(stream))
+                          cols, pat._dtype(dtype), p, seed, index, index_stride, pat._stream(stream))
 
 
 # ---------------------------------------------------------------------------
@@ -223,7 +216,7 @@ def _empty(shape, dtype, like, stream):
     """New memory for a call on `stream`: that stream's own (torch hands memory out again in the order of the stream
     that it was allocated on), so that neither earlier nor later work on the current stream meets it."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype)
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(pat._stream(stream), device=like.device)
     with torch.cuda.stream(stream):
@@ -279,11 +272,9 @@ def mx_matmul(a, b, dtype=torch.bfloat16, out=None, stream=None):
         raise ValueError(f"a has {k} columns, b has {b.cols}")
     code = _float(dtype, "dtype")
     out, stride = _output(out, m, n, dtype, a.codes, stream, "mx_matmul")
-    on = _on(stream, a.codes, a.scales, b.codes, b.scales, out)
-    need = _c.pat_mx_matmul_workspace(m, n, k)
-    work, hold = _work(need, out, stream)
     pat.check(_c.pat_mx_matmul(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, k,
-                               out.data_ptr(), stride, code, work, need, on), "pat_mx_matmul")
+                               out.data_ptr(), stride, code, _on(stream, a.codes, a.scales, b.codes, b.scales, out)),
+              "pat_mx_matmul")
     return out
 
 

@@ -19,8 +19,7 @@ static hipError_t launched() {
 }
 hipError_t launch_mx_quantize(Mat, Elem, int64_t, int64_t, uint8_t*, uint8_t*, hipStream_t) { return launched(); }
 hipError_t launch_mx_dequantize(MxMat, int64_t, int64_t, MatOut, Elem, hipStream_t) { return launched(); }
-size_t mx_matmul_workspace(int64_t, int64_t, int64_t) { return 0; }
-hipError_t launch_mx_matmul(MxMat, MxMat, int64_t, int64_t, int64_t, MatOut, Elem, void*, hipStream_t) { return launched(); }
+hipError_t launch_mx_matmul(MxMat, MxMat, int64_t, int64_t, int64_t, MatOut, Elem, hipStream_t) { return launched(); }
 size_t mx_linear_workspace(int64_t m, int64_t, int64_t k) { return (size_t)(m * groups_of(k)) * 68; }
 hipError_t launch_mx_linear(Mat, Elem, MxMat, int64_t, int64_t, int64_t, MatOut, Elem, void*, hipStream_t) {
   return launched();
@@ -102,7 +101,7 @@ static void check_calls() {
         "stride");
   CHECK(pat_embedding(at(0), 8, SIZE_MAX, at(0x1000), 8, PAT_FLOAT32, 0, 4, 8, 1.0f, at(0x2000), 8, PAT_FLOAT32, nullptr) ==
             PAT_ERR_UNSUPPORTED, "tokens");
-  CHECK(pat_mx_matmul_workspace(SIZE_MAX, 1, 1) == 0 && pat_embedding_grad_workspace(SIZE_MAX, 1, 1) == 0, "workspace");
+  CHECK(pat_mx_linear_workspace(SIZE_MAX, 1, 1) == 0 && pat_embedding_grad_workspace(SIZE_MAX, 1, 1) == 0, "workspace");
   // dropout: P and the scale of what is kept; in place and not
   const int before = g_launches;
   CHECK(pat_dropout(at(0), 8, nullptr, 0, at(0), 8, 4, 8, PAT_FLOAT32, 0.5, 7, 9, 8, nullptr) == PAT_OK, "in place");

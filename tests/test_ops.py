@@ -147,7 +147,7 @@ def quantize_args(**kw):
 
 def matmul_args(**kw):
     a = dict(a_codes=BASE, a_scales=BASE + 0x1000, b_codes=BASE + 0x2000, b_scales=BASE + 0x4000, m=3, n=5, k=200,
-             out=BASE + 0x5000, out_stride=5, dtype="float32", workspace=BASE + 0x8000, workspace_bytes=1 << 20)
+             out=BASE + 0x5000, out_stride=5, dtype="float32")
     return list({**a, **kw}.values())
 
 
@@ -332,7 +332,7 @@ def test_matmul(m, n, k, dtype):
 @pytest.mark.parametrize("m,n,k", PRODUCTS)
 @pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (B16, B16), (B16, F32)])
 def test_linear(m, n, k, dtype, out_dtype):
-    """Against the plain form, and to the bit against quantising first where both take the same kernel's sums."""
+    """Against the plain form, and to the bit against quantising first."""
     x = values((m, k), m * n + k, dtype)
     w, vw = random_mx(n, k, k + n)
     vx = O.mx_values(*O.mx_pack(*O.mx_quantize(f64(x))), k)
@@ -341,6 +341,7 @@ def test_linear(m, n, k, dtype, out_dtype):
         ops.mx_linear(view, w, out_dtype, out)
         assert untouched()
         within(out, vx @ vw.T, np.abs(vx) @ np.abs(vw).T, k, out_dtype)
+        assert torch.equal(out, ops.mx_matmul(ops.mx_quantize(view), w, out_dtype))
 
 
 @gpu
