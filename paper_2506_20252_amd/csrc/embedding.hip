@@ -18,7 +18,10 @@ __device__ __forceinline__ int64_t token_row(const char* tokens, int token_bytes
 }
 
 // A row is taken by `lanes` lanes, 8 columns each at a time; a workgroup holds 256 / lanes tokens side by side and
-// TOKENS of them in turn, whose table rows a lane reads before it writes any.template <int TOKENS, typename TI, typename TO>
+// TOKENS of them in turn, whose table rows a lane reads before it writes any.
+//
+// Bound by memory: 65536 random tokens of 4096 bfloat16 columns, a table of 32768 rows, in 153 us: 649 MB if each row were
+// read once, 833 MB counted (a row that comes again is mostly gone from the caches), 5.4 TB/s.
 template <int TOKENS, typename TI, typename TO>
 __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int token_bytes, int64_t ntokens, Mat table,
                                                      int64_t first, int64_t rows, int64_t cols, float scale, MatOut out,
@@ -65,6 +68,8 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
 // its tile (smaller digits anywhere, equal digits in earlier tiles), then places its entries in order: its waves
 // take consecutive sections, a wave 64 entries at a time, entries of one digit by their lane.  The first pass
 // reads the tokens themselves and leaves out those the table does not hold.
+//
+// Bound by latency, not by bytes: 131072 tokens of 65536 rows, two passes, 33 us (5 + 12 each) for 3 MB.
 
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kMaxBins = 1 << kMaxBits;
@@ -190,7 +195,7 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
 }
 
 // The whole sort in one workgroup, for so few tokens that launches are what it costs (us, 1001 tokens of 1251 rows: 14.5
-// in four launches).  Entries stay in LDS from pass to pass; a wave takes a section of them, 64 at a time.
+// in four launches, 6.8 in this one).  Entries stay in LDS from pass to pass; a wave takes a section of them, 64 at a time.
 constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(SortArgs a, int passes) {
@@ -283,6 +288,9 @@ __device__ __forceinline__ int32_t wave_lower_bound(const int32_t* keys, int32_t
 // what a row has in several pieces goes to the workspace, a row of float32 per piece, and join_kernel adds these in
 // order.  A piece has two such rows at most: slot 0 for the row of its first entry, slot 1 for that of its last.
 // Rows without an entry are zeroed by workgroups of their own in the same launch.
+//
+// Bound by memory: 131072 tokens of 2048 bfloat16 columns into 65536 float32 rows (1.07 GB) in 210 us, 5.1 TB/s, and
+// 18 us for the rows over pieces.  1001 tokens of 333 columns: 9 and 4 us, launches and one chain of loads.
 
 struct SumArgs {
   const int32_t *keys, *pos, *nvalid;  // nvalid == nullptr: there are no entries

@@ -7,6 +7,9 @@ namespace {
 // A lane takes 8 values at a time, 4 lanes a block, 16 lanes a group of 128; the stored form of groups that follow
 // each other, also from row to row, is consecutive, so codes and scales leave as whole words in order.  A workgroup
 // takes 16 groups side by side and kGroups of those in turn, all read before any is written.
+//
+// Bound by memory: 8192 x 8192 bfloat16 (170 MB) in 28 us, 6.0 TB/s (36 where the input comes from HBM and the output
+// evicts it); 1001 x 1000 float32 (4.5 MB) in 3.6 us, of which 3 are a launch of anything.
 constexpr int kGroups = 4;
 
 template <typename T>
@@ -40,7 +43,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(Mat x, uint32_t total, in
   }
 }
 
-// A lane takes VALUES columns at a time (8 bfloat16 or 4 float32: 16 bytes), 128 / VALUES lanes a group.
+// A lane takes VALUES columns at a time (8 bfloat16 or 4 float32: 16 bytes), 128 / VALUES lanes a group: stores are whole
+// vectors of consecutive lanes.  Bound by memory: 8192 x 8192 to bfloat16 in 25 us, 6.8 TB/s.
 template <typename T>
 __global__ __launch_bounds__(256) void dequantize_kernel(MxMat q, uint32_t total, int64_t cols, Divisor groups, MatOut out) {
   constexpr int VALUES = 16 / T::kBytes, LANES = 128 / VALUES, SIDE = 256 / LANES;

@@ -17,8 +17,12 @@ namespace {
 // other, and what the step after that needs is on its way into these registers.  The codes and scales of a wave's
 // patches come in one load each, 16 bytes and one byte a lane, and go to their lanes through a piece of LDS of the
 // wave's own: a load takes its 16 cycles of address work for 64 lanes whether they ask for one byte or 16 (with a load
-// for each row of a patch, 20 a wave and step, the loads took longer than the multiplications).  Of two waves on a SIMD one multiplies
-// first and the other widens first, so that the matrix unit and the vector unit both have work.
+// for each row of a patch, 20 a wave and step, the loads took longer than the multiplications).  Of two waves on a SIMD
+// one multiplies first and the other widens first, so that the matrix unit and the vector unit both have work.
+//
+// Bound by the matrix instructions: 8192 x 4096 x 4096 in 236 us (g as given) and 247 us (g by j, float32 out), 1160 and
+// 1110 TFLOP/s, beside 1395 of a large bfloat16 library product.  1001 x 1000 x 1333: 16 and 18 us, the latency of 8
+// steps in turn with one workgroup a CU.
 //
 // PARTS: as many such groups of waves in a workgroup, each with its own part of j and its own LDS; their sums are added
 // in order at the end.  For few tiles, whose waves would otherwise wait for one another's latencies alone.
@@ -299,8 +303,9 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 }
 
 // The same product where the vectors of 8 above do not exist (fewer than 8 values of j, or of rows where g is given by j),
-// or where a tile's rows of g are so far apart that their offsets need more than 32 bits.  One wave per 16 x 16 of out; an instruction of 16 x 16 x 32 takes j = 8 * (l / 16) ... + 7 of row and column
-// l mod 16 in lane l, read one by one.
+// or where a tile's rows of g are so far apart that their offsets need more than 32 bits.  One wave per 16 x 16 of out; an
+// instruction of 16 x 16 x 32 takes j = 8 * (l / 16) ... + 7 of row and column l mod 16 in lane l, read one by one: right
+// for any stride, and slow (every value is a load of its own).
 template <bool TRANSPOSED, typename T>
 __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out) {
   const int64_t pitch = (cols + 127) / 128 * 64;

@@ -23,6 +23,7 @@ import pytest
 import torch
 
 from oracle import operators as O
+from paper_2506_20252_amd import build as B
 from paper_2506_20252_amd import ops, pat
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -135,6 +136,24 @@ def test_host_side_under_asan_ubsan(tmp_path):
     res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
     assert res.returncode == 0, (res.stdout[-2000:], res.stderr[-2000:])
     assert " 0 failures" in res.stdout
+
+
+@pytest.mark.parametrize("source", ["mx.hip", "mx_product.hip", "mx_grad.hip", "embedding.hip", "dropout.hip"])
+def test_kernels_as_compiled(source, tmp_path):
+    """No scratch memory, no packed fp32; a workgroup of eight waves and more leaves two waves a SIMD their registers."""
+    if shutil.which(B.hipcc()) is None:
+        pytest.skip("hipcc not available")
+    out = tmp_path / "kernels.s"
+    flags = [f for f in B.HIPCC_FLAGS if f not in ("-fPIC", "-shared")]
+    subprocess.run([B.hipcc(), *flags, "--cuda-device-only", "-S", "-I", os.path.join(ROOT, "include"),
+                    os.path.join(B.CSRC, source), "-o", str(out)], check=True, capture_output=True, timeout=600)
+    asm = out.read_text()
+    names, private, vgprs = (re.findall(rf"^\s+\.{field}:\s+(\S+)$", asm, re.M)
+                             for field in ("name", "private_segment_fixed_size", "vgpr_count"))
+    assert names and len(names) == len(private) == len(vgprs)
+    assert not [(n, p) for n, p in zip(names, private) if p != "0"]
+    assert not [(n, v) for n, v in zip(names, vgprs) if int(v) > 256]
+    assert not re.search(r"\bv_pk_(add|mul|fma)_f32\b", asm)
 
 
 BASE = 1 << 32  # addresses that no call below may reach
