@@ -61,6 +61,128 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
   }
 }
 
+// ---- gradient of few tokens, in one launch ----------------------------------------------------------------
+//
+// A workgroup of 16 waves takes `each` rows a wave in turn and reads all tokens itself, one a lane.  Those of its rows
+// are listed in order; then a wave adds up its rows one by one, or writes zeros.  A row with far more than its share of
+// the list is added up by all waves, a section of the list each, and the waves' sums in order.
+//
+// Bound by latency: a load of tokens, a load of rows of g after it, and a launch: 5 us for 1001 tokens of 333 columns and
+// 1251 rows, of which 3 are a launch of anything (sorted first, in three launches: 19).
+
+constexpr int kFewWaves = 16, kFewMostEach = 8;
+static_assert(kFewTokens == 64 * kFewWaves, "a token a lane");
+
+struct FewArgs {
+  const char* tokens;
+  int token_bytes, ntokens, each;
+  int64_t first, rows, cols;
+  Mat g;
+  MatOut out;
+  float scale;
+};
+
+template <typename TI, typename TO>
+__global__ __launch_bounds__(kFewTokens) void few_kernel(FewArgs a) {
+  constexpr bool SPLIT = Split<TI, TO>::value;
+  __shared__ uint32_t list[kFewTokens];  // the token's number, and its row in the bits above
+  __shared__ int32_t totals[kFewWaves], counts[kFewWaves * kFewMostEach], crowd[8], crowds;
+  __shared__ float part[kFewWaves][8 * 64];
+  const int t = threadIdx.x, lane = t % 64, wave = __builtin_amdgcn_readfirstlane(t / 64), here = kFewWaves * a.each;
+  const int64_t gap = lane_gap<SPLIT>(64);
+  for (int64_t r0 = (int64_t)blockIdx.x * here; r0 < a.rows; r0 += (int64_t)gridDim.x * here) {
+    if (t < here) counts[t] = 0;
+    if (t == 0) crowds = 0;
+    __syncthreads();
+    const int64_t r = t < a.ntokens ? token_row(a.tokens, a.token_bytes, t, a.first, a.rows) - r0 : -1;
+    const bool listed = r >= 0 && r < here;
+    const uint64_t ours = __ballot(listed);
+    if (listed) atomicAdd(&counts[r], 1);
+    if (lane == 0) totals[wave] = __popcll(ours);
+    __syncthreads();
+    int at = 0, n = 0;
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      if (w == wave) at = n;
+      n += totals[w];
+    }
+    n = __builtin_amdgcn_readfirstlane(n);
+    if (listed) list[at + __popcll(ours & (((uint64_t)1 << lane) - 1))] = (uint32_t)(t | (int)r << 10);
+    // more than an eighth of the list, and more than a wave adds up before the others have met: seven rows at most
+    const int many = 32 + n / 8;
+    if (t < here && counts[t] > many) crowd[atomicAdd(&crowds, 1)] = t;
+    __syncthreads();
+
+    auto columns = [&](int64_t c, auto cover) {
+      constexpr Cover C = decltype(cover)::value;
+      const int64_t left = a.cols - c;
+      // adds a row's entries of list[from, to) to `sum`, in order, U loads at a time
+      auto add = [&](int row, int from, int to, float (&sum)[8]) {
+        constexpr int U = C == kWhole ? 8 : 4;
+        for (int i = from; i < to; i += 64) {
+          const uint32_t entry = i + lane < to ? list[i + lane] : 0xFFFFFFFFu;
+          uint64_t mine = __ballot((int)(entry >> 10) == row);
+          while (mine) {
+            const int have = min(__popcll(mine), U);
+            float v[U][8];
+            int src = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              src = mine ? __builtin_ctzll(mine) : src;  // beyond the last the last again, not added
+              mine &= mine - 1;
+              const int64_t token = __builtin_amdgcn_readlane(entry, src) & (kFewTokens - 1);
+              load8<TI, SPLIT, false, C>((const char*)a.g.p + (token * a.g.stride + c) * TI::kBytes, left, gap, v[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              if (u >= have) break;
+#pragma unroll
+              for (int j = 0; j < 8; ++j) sum[j] += v[u][j];
+            }
+          }
+        }
+      };
+      auto write = [&](int row, float (&sum)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[j] *= a.scale;
+        store8<TO, SPLIT, true, C>((char*)a.out.p + ((r0 + row) * a.out.stride + c) * TO::kBytes, left, gap, sum);
+      };
+      for (int row = wave; row < here && r0 + row < a.rows; row += kFewWaves) {
+        const int count = __builtin_amdgcn_readfirstlane(counts[row]);
+        if (count > many) continue;
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (count) add(row, 0, n, sum);
+        write(row, sum);
+      }
+      const int rest = __builtin_amdgcn_readfirstlane(crowds), section = (n + kFewTokens - 1) / kFewTokens * 64;
+      for (int x = 0; x < rest; ++x) {
+        const int row = __builtin_amdgcn_readfirstlane(crowd[x]);
+        float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        add(row, wave * section, min(n, (wave + 1) * section), sum);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[wave][64 * j + lane] = sum[j];
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll 1
+          for (int w = 1; w < kFewWaves; ++w)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += part[w][64 * j + lane];
+          write(row, sum);
+        }
+        __syncthreads();
+      }
+    };
+    for (int64_t c0 = (int64_t)blockIdx.y * 512; c0 < a.cols; c0 += (int64_t)gridDim.y * 512) {
+      const int64_t c = c0 + lane_column<SPLIT>(lane);
+      const Cover cover = cover_of(a.cols - c, gap, a.cols);  // the same for every wave
+      if (cover == kWhole) columns(c, CoverOf<kWhole>{});
+      else if (cover == kEnd) columns(c, CoverOf<kEnd>{});
+      else columns(c, CoverOf<kFew>{});
+    }
+    __syncthreads();  // all have read the list
+  }
+}
+
 // ---- stable radix sort of (row, token index) by row -------------------------------------------------------
 //
 // A pass takes `bits` bits of the row, the low ones first.  Its input is cut into tiles of consecutive entries,
@@ -293,7 +415,7 @@ __device__ __forceinline__ int32_t wave_lower_bound(const int32_t* keys, int32_t
 // 18 us for the rows over pieces.  1001 tokens of 333 columns: 9 and 4 us, launches and one chain of loads.
 
 struct SumArgs {
-  const int32_t *keys, *pos, *nvalid;  // nvalid == nullptr: there are no entries
+  const int32_t *keys, *pos, *nvalid;
   Mat g;
   MatOut out;
   float* partial;  // [pieces][2][pitch]
@@ -350,7 +472,7 @@ __device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
 // per lane, and takes each from its lane into scalar registers: no load of a row waits for a load of its entry.
 template <bool UNIFORM, typename TI, typename TO>
 __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {
-  const int32_t n = a.nvalid ? *a.nvalid : 0;
+  const int32_t n = *a.nvalid;
   // both kinds of workgroups in turn, as long as there are both
   const int both = 2 * min(a.sum_wgs, a.zero_wgs), rest = (int)blockIdx.x - both;
   const bool zeroes = rest < 0 ? blockIdx.x & 1 : a.zero_wgs > a.sum_wgs;
@@ -539,55 +661,67 @@ hipError_t launch_embedding(const void* tokens, int token_bytes, int64_t ntokens
 }
 
 size_t embedding_grad_workspace(int64_t ntokens, int64_t rows, int64_t cols) {
-  return ntokens ? grad_space(nullptr, ntokens, sort_plan(ntokens, rows), sum_plan(ntokens, rows, cols)).bytes : 0;
+  if (few_tokens(ntokens, rows)) return 0;
+  return grad_space(nullptr, ntokens, sort_plan(ntokens, rows), sum_plan(ntokens, rows, cols)).bytes;
 }
 
 hipError_t launch_embedding_grad(const void* tokens, int token_bytes, int64_t ntokens, Mat g, Elem g_dtype, int64_t first,
                                  int64_t rows, int64_t cols, float scale, MatOut out, Elem dtype, void* workspace,
                                  hipStream_t stream) {
+  if (few_tokens(ntokens, rows)) {
+    // rows a wave: as many as leave two workgroups a CU, to list and wait once for all
+    const int each = (int)std::min<size_t>(ceil_div(rows, kFewWaves * 512), kFewMostEach);
+    FewArgs a{(const char*)tokens, token_bytes, (int)ntokens, each, first, rows, cols, g, out, scale};
+    const size_t blocks = ceil_div(rows, kFewWaves * each);
+    // workgroups side by side in a row where the rows alone do not fill the chip
+    const size_t side = std::min(ceil_div(cols, 512), ceil_div(512, blocks));
+    const auto kernel = g_dtype == Elem::f32 ? (dtype == Elem::f32 ? few_kernel<F32, F32> : few_kernel<F32, B16>)
+                                             : (dtype == Elem::f32 ? few_kernel<B16, F32> : few_kernel<B16, B16>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<size_t>(blocks, 1 << 20), (unsigned)side), dim3(kFewTokens), 0, stream,
+                       a);
+    return hipGetLastError();
+  }
   const SortPlan plan = sort_plan(ntokens, rows);
   const SumPlan cut = sum_plan(ntokens, rows, cols);
   const GradSpace w = grad_space((char*)workspace, ntokens, plan, cut);
+  SortArgs a{};
+  a.tokens = (const char*)tokens;
+  a.token_bytes = token_bytes;
+  a.ntokens = ntokens;
+  a.first = first;
+  a.rows = rows;
+  a.counts = w.counts;
+  a.nvalid = w.nvalid;
+  a.bits = plan.bits;
+  a.tile = plan.tile;
+  a.tiles = (int32_t)plan.tiles;
+  const dim3 grid((unsigned)plan.tiles), block(kSortThreads);
+  const bool small = ntokens <= kSmallTokens;
   int at = 0;
-  if (ntokens) {
-    SortArgs a{};
-    a.tokens = (const char*)tokens;
-    a.token_bytes = token_bytes;
-    a.ntokens = ntokens;
-    a.first = first;
-    a.rows = rows;
-    a.counts = w.counts;
-    a.nvalid = w.nvalid;
-    a.bits = plan.bits;
-    a.tile = plan.tile;
-    a.tiles = (int32_t)plan.tiles;
-    const dim3 grid((unsigned)plan.tiles), block(kSortThreads);
-    const bool small = ntokens <= kSmallTokens;
-    if (small) {
-      a.keys_out = w.keys[0];
-      a.pos_out = w.pos[0];
-      hipLaunchKernelGGL(small_sort_kernel, dim3(1), dim3(kSmallThreads), 0, stream, a, plan.passes);
-    }
-    for (int p = 0; p < plan.passes && !small; ++p) {
-      a.shift = p * plan.bits;
-      a.keys_in = w.keys[at];
-      a.pos_in = w.pos[at];
-      at ^= 1;
-      a.keys_out = w.keys[at];
-      a.pos_out = w.pos[at];
-      if (p == 0) {
-        hipLaunchKernelGGL(count_kernel<true>, grid, block, 0, stream, a);
-        hipLaunchKernelGGL(scatter_kernel<true>, grid, block, 0, stream, a);
-      } else {
-        hipLaunchKernelGGL(count_kernel<false>, grid, block, 0, stream, a);
-        hipLaunchKernelGGL(scatter_kernel<false>, grid, block, 0, stream, a);
-      }
+  if (small) {
+    a.keys_out = w.keys[0];
+    a.pos_out = w.pos[0];
+    hipLaunchKernelGGL(small_sort_kernel, dim3(1), dim3(kSmallThreads), 0, stream, a, plan.passes);
+  }
+  for (int p = 0; p < plan.passes && !small; ++p) {
+    a.shift = p * plan.bits;
+    a.keys_in = w.keys[at];
+    a.pos_in = w.pos[at];
+    at ^= 1;
+    a.keys_out = w.keys[at];
+    a.pos_out = w.pos[at];
+    if (p == 0) {
+      hipLaunchKernelGGL(count_kernel<true>, grid, block, 0, stream, a);
+      hipLaunchKernelGGL(scatter_kernel<true>, grid, block, 0, stream, a);
+    } else {
+      hipLaunchKernelGGL(count_kernel<false>, grid, block, 0, stream, a);
+      hipLaunchKernelGGL(scatter_kernel<false>, grid, block, 0, stream, a);
     }
   }
   SumArgs u{};
   u.keys = w.keys[at];
   u.pos = w.pos[at];
-  u.nvalid = ntokens ? w.nvalid : nullptr;
+  u.nvalid = w.nvalid;
   u.g = g;
   u.out = out;
   u.partial = w.partial;

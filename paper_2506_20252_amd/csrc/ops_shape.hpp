@@ -54,12 +54,22 @@ inline GradPlan grad_plan(int64_t rows, int64_t inner, int64_t cols) {
 constexpr int kSortThreads = 256, kMaxBits = 10;  // of a sorting workgroup; of a pass's digit
 constexpr int kZeroRows = 64;                     // rows that one workgroup looks through for ones without an entry
 
+// Few tokens take one launch without a sort, in which each workgroup looks at all tokens; unless one workgroup would have
+// many for few rows.  us, and sorted: 9.3 and 15.3 (256 tokens of 64 columns, 32768 rows), 28 and 40 (1024, 1024, 32768),
+// 8.7 and 16.9 (1024, 1024, 100), but 24.6 and 12.1 (1024, 8, 16), 14.7 and 11.4 (512, 4096, 1).
+constexpr int64_t kFewTokens = 1024;
+inline bool few_tokens(int64_t ntokens, int64_t rows) {
+  return ntokens <= 256 || (ntokens <= kFewTokens && ntokens <= 16 * rows);
+}
+
 struct SortPlan {
   int bits, passes;
   int64_t tile, tiles;  // entries per workgroup, workgroups
 };
 
-constexpr int kSmallBits = 8;                         // of the sort in one workgroup, below
+// The sort of not many tokens is one workgroup's.  us, and in workgroups of their own: 20 and 29 (2048 tokens of 64 columns,
+// 32768 rows), 26 and 33 (4096, 64, 50000).
+constexpr int kSmallBits = 8;
 constexpr int64_t kSmallTokens = 4096;
 
 inline SortPlan sort_plan(int64_t ntokens, int64_t rows) {

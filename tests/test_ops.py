@@ -189,9 +189,9 @@ def embedding_args(**kw):
 
 
 def embedding_grad_args(**kw):
-    a = dict(tokens=BASE, token_bytes=4, ntokens=7, g=BASE + 0x1000, g_stride=200, g_dtype="float32", first=0, rows=5,
-             cols=200, scale=1.0, out=BASE + 0x5000, out_stride=200, dtype="float32", workspace=BASE + 0x8000,
-             workspace_bytes=1 << 20)
+    a = dict(tokens=BASE, token_bytes=4, ntokens=5000, g=BASE + 0x10000, g_stride=200, g_dtype="float32", first=0, rows=5,
+             cols=200, scale=1.0, out=BASE + 0x1000000, out_stride=200, dtype="float32", workspace=BASE + 0x2000000,
+             workspace_bytes=1 << 24)
     return list({**a, **kw}.values())
 
 
@@ -227,9 +227,9 @@ REFUSED = [
         (dict(token_bytes=8, tokens=BASE + 4), INVALID), (dict(table=0), INVALID), (dict(table_dtype="int32"), UNSUPPORTED),
         (dict(out=BASE + 0x1000), INVALID), (dict(out_stride=1), INVALID), (dict(ntokens=1 << 31), UNSUPPORTED)]),
     (ops.pat_embedding_grad, embedding_grad_args, [
-        (dict(tokens=0), INVALID), (dict(token_bytes=1), UNSUPPORTED), (dict(g=0), INVALID), (dict(out=BASE + 0x1000), INVALID),
-        (dict(workspace=BASE + 0x5000), INVALID), (dict(workspace=BASE + 0x1000), INVALID), (dict(workspace=0), INVALID),
-        (dict(workspace=BASE + 0x8008), INVALID), (dict(workspace_bytes=16), TOO_LARGE), (dict(g_dtype="int32"), UNSUPPORTED)]),
+        (dict(tokens=0), INVALID), (dict(token_bytes=1), UNSUPPORTED), (dict(g=0), INVALID), (dict(out=BASE + 0x10000), INVALID),
+        (dict(workspace=BASE + 0x1000000), INVALID), (dict(workspace=BASE + 0x10000), INVALID), (dict(workspace=0), INVALID),
+        (dict(workspace=BASE + 0x2000008), INVALID), (dict(workspace_bytes=16), TOO_LARGE), (dict(g_dtype="int32"), UNSUPPORTED)]),
     (ops.pat_dropout, dropout_args, [
         (dict(p=-0.01), INVALID), (dict(p=1.01), INVALID), (dict(p=math.nan), INVALID), (dict(x=0), INVALID),
         (dict(out=BASE + 4), INVALID), (dict(out=BASE, out_stride=201), INVALID), (dict(out=BASE + 0x10004), INVALID),
@@ -475,6 +475,14 @@ def token_sets():
     yield "shard", g.integers(0, 1000, size=3000), 250, 500
     yield "frequent and rare", np.minimum(np.exp(g.random(5000) * 8).astype(np.int64), 1999), 2000, 0
     yield "more rows than one pass sorts", g.integers(0, 5000, size=2500), 5000, 0
+    yield "few, and a frequent row", np.where(g.random(1024) < 0.7, 3, g.integers(0, 400, size=1024)), 400, 0
+    yield "few, and two frequent rows", np.where(g.random(1000) < 0.8, 9 + 4 * g.integers(0, 2, 1000), 1), 70, 0
+    yield "few, of many rows", g.integers(0, 30000, size=600), 30000, 0
+    yield "many, all the same", np.full(6000, 4), 9, 0
+    yield "many, none inside", np.arange(5000) + 100, 20, 0
+    yield "many, each once, falling", np.arange(4500)[::-1].copy(), 4500, 0
+    yield "many, one row", g.integers(-1, 2, size=4097), 1, 0
+    yield "many, shard", g.integers(0, 2000, size=7000), 250, 500
     yield "two passes and a frequent row", np.where(g.random(9000) < 0.4, 4000, g.integers(0, 70000, size=9000)), 70000, 0
 
 
@@ -499,7 +507,7 @@ def test_embedding_grad(name, tokens, rows, first, cols, dtype, out_dtype):
 
 
 @gpu
-@pytest.mark.parametrize("ntokens,cols", [(0, 5), (2000, 2100), (20, 4100)])
+@pytest.mark.parametrize("ntokens,cols", [(0, 5), (2000, 2100), (20, 4100), (600, 1500)])
 def test_embedding_grad_of_wide_rows_and_none(ntokens, cols):
     tokens = np.random.default_rng(3).integers(0, 40, size=ntokens)
     tokens[: ntokens // 2] = 7
