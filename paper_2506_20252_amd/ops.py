@@ -155,39 +155,39 @@ def mx_empty(rows, cols, device="cuda"):
 
 
 def _float(dtype, what):
-    if dtype not in _CODE:
+    code = _CODE.get(dtype)
+    if code is None:
         raise ValueError(f"{what}: float32 or bfloat16, got {dtype}")
-    return _CODE[dtype]
+    return code
 
 
-def _matrix(t, what, shape=None):
-    """Checks a float matrix and returns its row stride."""
-    if t.dim() != 2 or not t.is_cuda:
-        raise ValueError(f"{what}: a 2-D GPU tensor")
+def _matrix(t, what):
+    """Checks a float matrix; returns its rows, columns, row stride and type."""
     size = t.shape
-    if shape is not None and size != shape:
-        raise ValueError(f"{what}: shape {tuple(shape)} is needed, got {tuple(size)}")
-    if t.dtype not in _CODE:
+    if len(size) != 2 or not t.is_cuda:
+        raise ValueError(f"{what}: a 2-D GPU tensor")
+    code = _CODE.get(t.dtype)
+    if code is None:
         _float(t.dtype, what)
     rows, cols = size
     stride, unit = t.stride()
     if stride == cols and unit == 1:
-        return stride
+        return rows, cols, stride, code
     if rows and cols > 1 and unit != 1:
         raise ValueError(f"{what}: the elements of a row must be consecutive in memory")
     if rows > 1 and cols and stride < cols:
         raise ValueError(f"{what}: rows overlap")
-    return max(stride, cols)
+    return rows, cols, max(stride, cols), code
 
 
 def _stored(q, what):
-    """Checks an Mx and returns its row count."""
+    """Checks an Mx; returns its codes, scales, rows and columns."""
     codes, scales, cols = q
     groups = -(-cols // PAT_MX_GROUP)
     rows = codes.shape[0] if codes.dim() == 2 else -1
     if (codes.shape == (rows, 64 * groups) and scales.shape == (rows, 4 * groups) and codes.dtype is scales.dtype is torch.uint8
             and codes.is_cuda and scales.is_cuda and codes.is_contiguous() and scales.is_contiguous()):
-        return rows
+        return codes, scales, rows, cols
     raise ValueError(f"{what}: codes (rows, {64 * groups}) and scales (rows, {4 * groups}) must be contiguous uint8 GPU tensors, "
                      f"got {codes.dtype} {tuple(codes.shape)} and {scales.dtype} {tuple(scales.shape)}")
 
@@ -210,7 +210,7 @@ def _on(stream, *tensors):
 
 
 # The current stream's handle without a Stream object and the current device, where this torch has them: two microseconds
-# less per call, which takes seven or eight and the GPU three.
+# less per call, which takes six to eight and the GPU three.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -226,13 +226,14 @@ def _empty(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _output(out, rows, cols, dtype, like, stream, what):
-    """The output tensor and its row stride; a new one is on the device of `like`."""
-    if out is None:
-        return (like.new_empty((rows, cols), dtype=dtype) if stream is None else _empty((rows, cols), dtype, like, stream)), cols
+def _output(out, rows, cols, dtype, what):
+    """Checks a given output; returns its row stride."""
     if out.dtype != dtype:
         raise ValueError(f"{what}: out is {out.dtype}, not {dtype}")
-    return out, _matrix(out, "out", (rows, cols))
+    r, c, stride, _ = _matrix(out, "out")
+    if r != rows or c != cols:
+        raise ValueError(f"out: shape {(rows, cols)} is needed, got {(r, c)}")
+    return stride
 
 
 def _work(nbytes, like, stream):
@@ -245,107 +246,143 @@ def _work(nbytes, like, stream):
 
 def mx_quantize(x, out=None, stream=None):
     """4-bit blocks of a float32 or bfloat16 matrix, as an Mx."""
-    stride = _matrix(x, "x")
-    rows, cols = x.shape
+    rows, cols, stride, code = _matrix(x, "x")
     if out is None:
         groups = -(-cols // PAT_MX_GROUP)
-        out = Mx(_empty((rows, 64 * groups), torch.uint8, x, stream), _empty((rows, 4 * groups), torch.uint8, x, stream), cols)
-    elif _stored(out, "out") != rows or out.cols != cols:
-        raise ValueError(f"out: an Mx of {rows} x {cols} is needed")
-    codes, scales, _ = out
-    pat.check(_c.pat_mx_quantize(x.data_ptr(), stride, rows, cols, _CODE[x.dtype], codes.data_ptr(), scales.data_ptr(),
-                                 _on(stream, x, codes, scales)), "pat_mx_quantize")
+        codes, scales = _empty((rows, 64 * groups), torch.uint8, x, stream), _empty((rows, 4 * groups), torch.uint8, x, stream)
+        on, out = _on(stream, x), Mx(codes, scales, cols)
+    else:
+        codes, scales, out_rows, out_cols = _stored(out, "out")
+        if out_rows != rows or out_cols != cols:
+            raise ValueError(f"out: an Mx of {rows} x {cols} is needed")
+        on = _on(stream, x, codes, scales)
+    status = _c.pat_mx_quantize(x.data_ptr(), stride, rows, cols, code, codes.data_ptr(), scales.data_ptr(), on)
+    if status:
+        pat.check(status, "pat_mx_quantize")
     return out
 
 
 def mx_dequantize(q, dtype=torch.bfloat16, out=None, stream=None):
     """The matrix that an Mx stands for, in `dtype` (exact)."""
-    rows, code = _stored(q, "q"), _float(dtype, "dtype")
-    codes, scales, cols = q
-    out, stride = _output(out, rows, cols, dtype, codes, stream, "mx_dequantize")
-    pat.check(_c.pat_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, code,
-                                   _on(stream, codes, scales, out)), "pat_mx_dequantize")
+    codes, scales, rows, cols = _stored(q, "q")
+    code = _float(dtype, "dtype")
+    if out is None:
+        out, stride, on = _empty((rows, cols), dtype, codes, stream), cols, _on(stream, codes, scales)
+    else:
+        stride, on = _output(out, rows, cols, dtype, "mx_dequantize"), _on(stream, codes, scales, out)
+    status = _c.pat_mx_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, code, on)
+    if status:
+        pat.check(status, "pat_mx_dequantize")
     return out
 
 
 def mx_matmul(a, b, dtype=torch.bfloat16, out=None, stream=None):
     """a b^T of two Mx with the same number of columns."""
-    m, n, k = _stored(a, "a"), _stored(b, "b"), a.cols
-    if b.cols != k:
-        raise ValueError(f"a has {k} columns, b has {b.cols}")
+    a_codes, a_scales, m, k = _stored(a, "a")
+    b_codes, b_scales, n, b_cols = _stored(b, "b")
+    if b_cols != k:
+        raise ValueError(f"a has {k} columns, b has {b_cols}")
     code = _float(dtype, "dtype")
-    out, stride = _output(out, m, n, dtype, a.codes, stream, "mx_matmul")
-    pat.check(_c.pat_mx_matmul(a.codes.data_ptr(), a.scales.data_ptr(), b.codes.data_ptr(), b.scales.data_ptr(), m, n, k,
-                               out.data_ptr(), stride, code, _on(stream, a.codes, a.scales, b.codes, b.scales, out)),
-              "pat_mx_matmul")
+    if out is None:
+        out, stride, on = _empty((m, n), dtype, a_codes, stream), n, _on(stream, a_codes, a_scales, b_codes, b_scales)
+    else:
+        stride, on = _output(out, m, n, dtype, "mx_matmul"), _on(stream, a_codes, a_scales, b_codes, b_scales, out)
+    status = _c.pat_mx_matmul(a_codes.data_ptr(), a_scales.data_ptr(), b_codes.data_ptr(), b_scales.data_ptr(), m, n, k,
+                              out.data_ptr(), stride, code, on)
+    if status:
+        pat.check(status, "pat_mx_matmul")
     return out
 
 
 def mx_linear(x, w, dtype=None, out=None, stream=None):
     """Q(x) w^T: the rows of x, quantised on the way, times an Mx; `dtype` is x's by default."""
-    stride, n = _matrix(x, "x"), _stored(w, "w")
-    m, k = x.shape
-    codes, scales, cols = w
+    m, k, x_stride, x_code = _matrix(x, "x")
+    codes, scales, n, cols = _stored(w, "w")
     if cols != k:
         raise ValueError(f"x has {k} columns, w has {cols}")
-    dtype = x.dtype if dtype is None else dtype
-    code = _float(dtype, "dtype")
-    out, out_stride = _output(out, m, n, dtype, x, stream, "mx_linear")
-    on = _on(stream, x, codes, scales, out)
+    if dtype is None:
+        dtype, code = x.dtype, x_code
+    else:
+        code = _float(dtype, "dtype")
+    if out is None:
+        out, stride, on = _empty((m, n), dtype, x, stream), n, _on(stream, x, codes, scales)
+    else:
+        stride, on = _output(out, m, n, dtype, "mx_linear"), _on(stream, x, codes, scales, out)
     need = _c.pat_mx_linear_workspace(m, n, k)
-    work, hold = _work(need, out, stream)
-    pat.check(_c.pat_mx_linear(x.data_ptr(), stride, _CODE[x.dtype], codes.data_ptr(), scales.data_ptr(), m, n, k,
-                               out.data_ptr(), out_stride, code, work, need, on), "pat_mx_linear")
+    work, hold = _work(need, x, stream)
+    status = _c.pat_mx_linear(x.data_ptr(), x_stride, x_code, codes.data_ptr(), scales.data_ptr(), m, n, k, out.data_ptr(),
+                              stride, code, work, need, on)
+    if status:
+        pat.check(status, "pat_mx_linear")
     return out
 
 
 def mx_matmul_grad(g, q, dtype=torch.bfloat16, transposed=False, out=None, stream=None):
     """g q, or g^T q where `transposed`: with g the bfloat16 gradient of a b^T, the gradient of a is
     ``mx_matmul_grad(g, b)`` and that of b is ``mx_matmul_grad(g, a, transposed=True)``."""
-    stride, inner = _matrix(g, "g"), _stored(q, "q")
+    rows, terms, g_stride, _ = _matrix(g, "g")
+    codes, scales, inner, cols = _stored(q, "q")
     if g.dtype != torch.bfloat16:
         raise ValueError(f"g: bfloat16, got {g.dtype}")
-    codes, scales, cols = q
-    rows = g.shape[1 if transposed else 0]
-    if g.shape[0 if transposed else 1] != inner:
+    if transposed:
+        rows, terms = terms, rows
+    if terms != inner:
         raise ValueError(f"g: {tuple(g.shape)} does not match q's {inner} rows")
     code = _float(dtype, "dtype")
-    out, out_stride = _output(out, rows, cols, dtype, g, stream, "mx_matmul_grad")
-    on = _on(stream, g, codes, scales, out)
+    if out is None:
+        out, stride, on = _empty((rows, cols), dtype, g, stream), cols, _on(stream, g, codes, scales)
+    else:
+        stride, on = _output(out, rows, cols, dtype, "mx_matmul_grad"), _on(stream, g, codes, scales, out)
     need = _c.pat_mx_matmul_grad_workspace(rows, inner, cols)
-    work, hold = _work(need, out, stream)
-    pat.check(_c.pat_mx_matmul_grad(g.data_ptr(), stride, transposed, codes.data_ptr(), scales.data_ptr(), rows, inner,
-                                    cols, out.data_ptr(), out_stride, code, work, need, on), "pat_mx_matmul_grad")
+    work, hold = _work(need, g, stream)
+    status = _c.pat_mx_matmul_grad(g.data_ptr(), g_stride, bool(transposed), codes.data_ptr(), scales.data_ptr(), rows, inner,
+                                   cols, out.data_ptr(), stride, code, work, need, on)
+    if status:
+        pat.check(status, "pat_mx_matmul_grad")
     return out
 
 
 def embedding(tokens, table, scale=1.0, first=0, dtype=None, out=None, stream=None):
     """out[t] = scale * table[tokens[t] - first], zero for a token that the table's rows do not hold; `dtype` is
     the table's by default."""
-    size, stride = _indices(tokens, "tokens"), _matrix(table, "table")
-    rows, cols = table.shape
-    dtype = table.dtype if dtype is None else dtype
-    code, n = _float(dtype, "dtype"), tokens.shape[0]
-    out, out_stride = _output(out, n, cols, dtype, table, stream, "embedding")
-    pat.check(_c.pat_embedding(tokens.data_ptr(), size, n, table.data_ptr(), stride, _CODE[table.dtype], first, rows, cols,
-                               scale, out.data_ptr(), out_stride, code, _on(stream, tokens, table, out)), "pat_embedding")
+    size = _indices(tokens, "tokens")
+    rows, cols, table_stride, table_code = _matrix(table, "table")
+    n = tokens.shape[0]
+    if dtype is None:
+        dtype, code = table.dtype, table_code
+    else:
+        code = _float(dtype, "dtype")
+    if out is None:
+        out, stride, on = _empty((n, cols), dtype, table, stream), cols, _on(stream, tokens, table)
+    else:
+        stride, on = _output(out, n, cols, dtype, "embedding"), _on(stream, tokens, table, out)
+    status = _c.pat_embedding(tokens.data_ptr(), size, n, table.data_ptr(), table_stride, table_code, first, rows, cols, scale,
+                              out.data_ptr(), stride, code, on)
+    if status:
+        pat.check(status, "pat_embedding")
     return out
 
 
 def embedding_grad(tokens, g, rows, scale=1.0, first=0, dtype=None, out=None, stream=None):
     """The gradient of ``embedding`` with respect to a table of `rows` rows, dense; `dtype` is g's by default."""
-    size, stride = _indices(tokens, "tokens"), _matrix(g, "g")
-    n, cols = g.shape
+    size = _indices(tokens, "tokens")
+    n, cols, g_stride, g_code = _matrix(g, "g")
     if tokens.shape[0] != n:
         raise ValueError(f"g has {n} rows for {tokens.shape[0]} tokens")
-    dtype = g.dtype if dtype is None else dtype
-    code = _float(dtype, "dtype")
-    out, out_stride = _output(out, rows, cols, dtype, g, stream, "embedding_grad")
-    on = _on(stream, tokens, g, out)
+    if dtype is None:
+        dtype, code = g.dtype, g_code
+    else:
+        code = _float(dtype, "dtype")
+    if out is None:
+        out, stride, on = _empty((rows, cols), dtype, g, stream), cols, _on(stream, tokens, g)
+    else:
+        stride, on = _output(out, rows, cols, dtype, "embedding_grad"), _on(stream, tokens, g, out)
     need = _c.pat_embedding_grad_workspace(n, rows, cols)
-    work, hold = _work(need, out, stream)
-    pat.check(_c.pat_embedding_grad(tokens.data_ptr(), size, n, g.data_ptr(), stride, _CODE[g.dtype], first, rows, cols,
-                                    scale, out.data_ptr(), out_stride, code, work, need, on), "pat_embedding_grad")
+    work, hold = _work(need, g, stream)
+    status = _c.pat_embedding_grad(tokens.data_ptr(), size, n, g.data_ptr(), g_stride, g_code, first, rows, cols, scale,
+                                   out.data_ptr(), stride, code, work, need, on)
+    if status:
+        pat.check(status, "pat_embedding_grad")
     return out
 
 
@@ -354,17 +391,22 @@ def dropout(x, p, seed, index=0, index_stride=None, residual=None, out=None, str
     and the element's place: element (r, c) has number index + r * index_stride + c in the whole tensor
     (`index_stride`: x's columns by default, the whole's for a shard of its columns).  The gradient is the same
     call on the output's gradient.  `out` may be x or the residual."""
-    stride = _matrix(x, "x")
-    rows, cols = x.shape
-    out, out_stride = _output(out, rows, cols, x.dtype, x, stream, "dropout")
+    rows, cols, x_stride, code = _matrix(x, "x")
+    if out is None:
+        out, stride, on = _empty((rows, cols), x.dtype, x, stream), cols, _on(stream, x)
+    else:
+        stride, on = _output(out, rows, cols, x.dtype, "dropout"), _on(stream, x, out)
     address, residual_stride = None, 0
     if residual is not None:
-        residual_stride = _matrix(residual, "residual", x.shape)
-        if residual.dtype != x.dtype:
+        r, c, residual_stride, residual_code = _matrix(residual, "residual")
+        if r != rows or c != cols:
+            raise ValueError(f"residual: shape {(rows, cols)} is needed, got {(r, c)}")
+        if residual_code != code:
             raise ValueError(f"residual is {residual.dtype}, x is {x.dtype}")
+        _on(stream, residual)
         address = residual.data_ptr()
-    on = _on(stream, x, out) if residual is None else _on(stream, x, out, residual)
-    pat.check(_c.pat_dropout(x.data_ptr(), stride, address, residual_stride, out.data_ptr(), out_stride, rows, cols,
-                             _CODE[x.dtype], p, seed, index, cols if index_stride is None else index_stride, on),
-              "pat_dropout")
+    status = _c.pat_dropout(x.data_ptr(), x_stride, address, residual_stride, out.data_ptr(), stride, rows, cols, code, p, seed,
+                            index, cols if index_stride is None else index_stride, on)
+    if status:
+        pat.check(status, "pat_dropout")
     return out
