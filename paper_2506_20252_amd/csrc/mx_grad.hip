@@ -21,7 +21,7 @@ namespace {
 // one multiplies first and the other widens first, so that the matrix unit and the vector unit both have work.
 //
 // Bound by the matrix instructions: 8192 x 4096 x 4096 in 236 us (g as given) and 247 us (g by j, float32 out), 1160 and
-// 1110 TFLOP/s, beside 1395 of a large bfloat16 library product.  1001 x 1000 x 1333: 16 and 18 us, the latency of 8
+// 1110 TFLOP/s, beside 1395 of a large bfloat16 library product.  1001 x 1000 x 1333: 15 and 17 us, the latency of 8
 // steps in turn with one workgroup a CU.
 //
 // PARTS: as many such groups of waves in a workgroup, each with its own part of j and its own LDS; their sums are added
@@ -40,7 +40,7 @@ struct GradTile {
   };
   struct Stage {
     uint8_t codes[kRows * (R / 2)];
-    uint8_t scales[kRows * (R / 32)];
+    uint8_t scales[(R / 32) * kRows];  // of 32 columns row after row, so that a patch's 8 are one load
   };
 };
 
@@ -102,6 +102,7 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   const int patch_c = tid % (R / PC), patch_j = tid / (R / PC);
   constexpr int CHUNKS = R / 32, ROWS_Q = S::kRows;  // 16-byte pieces of a tile's row of codes, as many as its scales
   const int first_j = wave * ROWS_Q;                 // of the wave's patches
+  const int patch_row = lane / (R / PC) * 8, patch_shift = patch_c * PC % 8 * 4;  // of a patch in these; in a word of codes
   const int q_row = lane / CHUNKS;                   // what this lane loads: a row's piece of codes and its scale
   const uint32_t q_at = (uint32_t)(min(q_row, ROWS_Q - 1) * pitch + min(c0 / 2 + lane % CHUNKS * 16, pitch - 16));
   const uint32_t q_scale_at = (uint32_t)(min(q_row, ROWS_Q - 1) * (pitch / 16) + min(c0 / 32 + lane % CHUNKS, pitch / 16 - 1));
@@ -155,16 +156,15 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   auto widen = [&](Lds& l, int64_t j0, auto tail) {
     if (q_row < ROWS_Q) {
       *(v4u*)(stage.codes + lane * 16) = codes;
-      stage.scales[lane] = (uint8_t)scales;
+      stage.scales[lane % CHUNKS * ROWS_Q + q_row] = (uint8_t)scales;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     uint32_t code[8], scale[8];
+    const v2u s8 = *(const v2u*)(stage.scales + patch_c * PC / 32 * ROWS_Q + patch_row);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {  // of this lane's patch
-      const int row = lane / (R / PC) * 8 + r;
-      const uint8_t* p = stage.codes + row * (R / 2) + patch_c * (PC / 2);
-      code[r] = PC == 4 ? *(const uint16_t*)p : *p;
-      scale[r] = stage.scales[row * (R / 32) + patch_c * PC / 32];
+    for (int r = 0; r < 8; ++r) {  // of this lane's patch; whole words, which LDS gives two at a time
+      code[r] = *(const uint32_t*)(stage.codes + (patch_row + r) * (R / 2) + patch_c * PC / 8 * 4) >> patch_shift;
+      scale[r] = s8[r / 4] >> (r % 4 * 8) & 255u;
     }
     if constexpr (decltype(tail)::value) {
       const int left = (int)min(inner - j0, (int64_t)64);

@@ -25,7 +25,8 @@ inline int row_lanes(int64_t vectors, int threads) {
 // 153, 88, 102 for 2048 rows, 4096 columns and values of j; 305, 170, 121 for 4096 rows).  Below, few tiles of 128 and
 // a long sum are sliced (us, and with tiles of 64: 20 and 26 for 64 rows, 4096 columns and values of j; 22 and 55 for 512
 // rows and columns, 8192 values of j; but 22 and 18 for 1024 rows and columns, 2048 values of j), the others take tiles of
-// 64 with two groups of waves (16.2 us for 1001 x 1333 and 1000 values of j; with one group 16.5).
+// 64 with two groups of waves (us, and with one group: 15.5 and 15.3 for 1001 x 1333 and 1000 values of j, 39 and 43 for 4000,
+// 27 and 38 for one tile).
 struct GradPlan {
   int tile, slices;
   int64_t slice;
