@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
 // the list is added up by all waves, a section of the list each, and the waves' sums in order.
 //
 // Bound by latency: a load of tokens, a load of rows of g after it, and a launch: 5 us for 1001 tokens of 333 columns and
-// 1251 rows, of which 3 are a launch of anything (sorted first, in three launches: 19).
+// 1251 rows, of which 3 are a launch of anything (sorted first, in three launches: 19).  7.7 with one of them 64 times.
 
 constexpr int kFewWaves = 16, kFewMostEach = 8;
 static_assert(kFewTokens == 64 * kFewWaves, "a token a lane");
@@ -108,8 +108,9 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(FewArgs a) {
     }
     n = __builtin_amdgcn_readfirstlane(n);
     if (listed) list[at + __popcll(ours & (((uint64_t)1 << lane) - 1))] = (uint32_t)(t | (int)r << 10);
-    // more than an eighth of the list, and more than a wave adds up before the others have met: seven rows at most
-    const int many = 32 + n / 8;
+    // more than an eighth of the list (seven rows at most), and more than a wave adds up before all have met: a row of 32
+    // tokens 7.0 us so and 10.2 by one wave, one of 16 tokens 7.3 and 7.1
+    const int many = 16 + n / 8;
     if (t < here && counts[t] > many) crowd[atomicAdd(&crowds, 1)] = t;
     __syncthreads();
 
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(FewArgs a) {
       const int64_t left = a.cols - c;
       // adds a row's entries of list[from, to) to `sum`, in order, U loads at a time
       auto add = [&](int row, int from, int to, float (&sum)[8]) {
-        constexpr int U = C == kWhole ? 8 : 4;
+        constexpr int U = C == kFew ? 4 : 8;
         for (int i = from; i < to; i += 64) {
           const uint32_t entry = i + lane < to ? list[i + lane] : 0xFFFFFFFFu;
           uint64_t mine = __ballot((int)(entry >> 10) == row);
@@ -154,7 +155,7 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(FewArgs a) {
         if (count) add(row, 0, n, sum);
         write(row, sum);
       }
-      const int rest = __builtin_amdgcn_readfirstlane(crowds), section = (n + kFewTokens - 1) / kFewTokens * 64;
+      const int rest = __builtin_amdgcn_readfirstlane(crowds), section = (n + kFewWaves - 1) / kFewWaves;
       for (int x = 0; x < rest; ++x) {
         const int row = __builtin_amdgcn_readfirstlane(crowd[x]);
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};

@@ -56,11 +56,12 @@ constexpr int kSortThreads = 256, kMaxBits = 10;  // of a sorting workgroup; of 
 constexpr int kZeroRows = 64;                     // rows that one workgroup looks through for ones without an entry
 
 // Few tokens take one launch without a sort, in which each workgroup looks at all tokens; unless one workgroup would have
-// many for few rows.  us, and sorted: 9.3 and 15.3 (256 tokens of 64 columns, 32768 rows), 28 and 40 (1024, 1024, 32768),
-// 8.7 and 16.9 (1024, 1024, 100), but 24.6 and 12.1 (1024, 8, 16), 14.7 and 11.4 (512, 4096, 1).
+// many for few rows.  us, and sorted: 10 and 15 (256 tokens of 64 columns, 32768 rows), 9.5 and 10.1 (256, 64, 1 row), 28 and
+// 40 (1024, 1024, 32768), 7.3 and 16.7 (1024, 1024, 100), 13.1 and 14.7 (1024, 64, 48), but 15.7 and 14.0 (1024, 64, 32), 26
+// and 13 (1024, 8, 16).
 constexpr int64_t kFewTokens = 1024;
 inline bool few_tokens(int64_t ntokens, int64_t rows) {
-  return ntokens <= 256 || (ntokens <= kFewTokens && ntokens <= 16 * rows);
+  return ntokens <= 256 || (ntokens <= kFewTokens && ntokens <= 24 * rows);
 }
 
 struct SortPlan {
