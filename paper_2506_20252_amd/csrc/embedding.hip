@@ -192,7 +192,7 @@ __global__ __launch_bounds__(kFewTokens) void few_kernel(FewArgs a) {
 // take consecutive sections, a wave 64 entries at a time, entries of one digit by their lane.  The first pass
 // reads the tokens themselves and leaves out those the table does not hold.
 //
-// Bound by latency, not by bytes: 131072 tokens of 65536 rows, two passes, 33 us (5 + 12 each) for 3 MB.
+// Bound by latency, not by bytes: 131072 tokens of 65536 rows, two passes, 27 us (5 + 9 and 5 + 8) for 3 MB.
 
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kMaxBins = 1 << kMaxBits;
@@ -210,17 +210,25 @@ struct SortArgs {
   int32_t tiles;
 };
 
-// Entry i of a pass: its row (-1: none) and token index.
+// Entries i, i + step ... of a pass, below `end`: their rows (-1: none) and token indices.  All loads are in flight together.
+constexpr int kEntries = 4;
 template <bool FIRST>
-__device__ __forceinline__ int32_t entry(const SortArgs& a, int64_t i, int64_t n, int32_t* pos) {
-  if (i >= n) return -1;
-  if constexpr (FIRST) {
-    *pos = (int32_t)i;
-    return (int32_t)token_row(a.tokens, a.token_bytes, i, a.first, a.rows);
-  } else {
-    *pos = ldg<int32_t, false>((const char*)(a.pos_in + i));
-    return ldg<int32_t, false>((const char*)(a.keys_in + i));
+__device__ __forceinline__ void entries(const SortArgs& a, int64_t i, int64_t step, int64_t end, int32_t (&key)[kEntries],
+                                        int32_t (&pos)[kEntries]) {
+#pragma unroll
+  for (int u = 0; u < kEntries; ++u) {
+    const int64_t at = min(i + u * step, end - 1);
+    if constexpr (FIRST) {
+      pos[u] = (int32_t)at;
+      key[u] = (int32_t)token_row(a.tokens, a.token_bytes, at, a.first, a.rows);
+    } else {
+      pos[u] = ldg<int32_t, false>((const char*)(a.pos_in + at));
+      key[u] = ldg<int32_t, false>((const char*)(a.keys_in + at));
+    }
   }
+#pragma unroll
+  for (int u = 0; u < kEntries; ++u)
+    if (i + u * step >= end) key[u] = -1;
 }
 
 template <bool FIRST>
@@ -230,10 +238,13 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a) {
   for (int b = threadIdx.x; b < bins; b += kSortThreads) hist[b] = 0;
   __syncthreads();
   const int64_t n = FIRST ? a.ntokens : *a.nvalid, begin = blockIdx.x * a.tile;
-  for (int64_t i = begin + threadIdx.x; i < begin + a.tile; i += kSortThreads) {
-    int32_t pos;
-    const int32_t key = entry<FIRST>(a, i, n, &pos);
-    if (key >= 0) atomicAdd(&hist[key >> a.shift & (bins - 1)], 1);
+  const int64_t end = min(begin + a.tile, n);
+  for (int64_t i = begin + threadIdx.x; i < end; i += kEntries * kSortThreads) {
+    int32_t key[kEntries], pos[kEntries];
+    entries<FIRST>(a, i, kSortThreads, end, key, pos);
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u)
+      if (key[u] >= 0) atomicAdd(&hist[key[u] >> a.shift & (bins - 1)], 1);
   }
   __syncthreads();
   for (int b = threadIdx.x; b < bins; b += kSortThreads) a.counts[(int64_t)blockIdx.x * bins + b] = hist[b];
@@ -242,6 +253,7 @@ __global__ __launch_bounds__(kSortThreads) void count_kernel(SortArgs a) {
 template <bool FIRST>
 __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
   __shared__ int32_t next[kSortWaves][kMaxBins];  // per wave and digit: where its next entry goes
+  __shared__ __attribute__((aligned(16))) int32_t totals[kSortWaves][kMaxBins], befores[kSortWaves][kMaxBins];
   __shared__ int32_t sums[kSortThreads];
   const int bins = 1 << a.bits, t = threadIdx.x, wave = t / 64, lane = t % 64;
   const int64_t n = FIRST ? a.ntokens : *a.nvalid;
@@ -249,11 +261,30 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
 
   for (int i = t; i < kSortWaves * bins; i += kSortThreads) next[i / bins][i % bins] = 0;
   __syncthreads();
-  for (int64_t i = begin + lane; i < begin + section; i += 64) {
-    int32_t pos;
-    const int32_t key = entry<FIRST>(a, i, n, &pos);
-    if (key >= 0) atomicAdd(&next[wave][key >> a.shift & (bins - 1)], 1);
+  const int64_t end = min(begin + section, n);
+  for (int64_t i = begin; i < end; i += kEntries * 64) {
+    int32_t key[kEntries], pos[kEntries];
+    entries<FIRST>(a, i + lane, 64, end, key, pos);
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u)
+      if (key[u] >= 0) atomicAdd(&next[wave][key[u] >> a.shift & (bins - 1)], 1);
   }
+
+  // What the tiles' histograms hold, in all and before this tile: a wave adds up a quarter of them, four digits a lane.
+  const int32_t quarter = (a.tiles + kSortWaves - 1) / kSortWaves;
+  const int32_t w0 = wave * quarter, w1 = min(w0 + quarter, a.tiles);
+  for (int b = 4 * lane; b < bins; b += 256) {
+    v4i total = {0, 0, 0, 0}, before = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int32_t w = w0; w < w1; ++w) {
+      const v4i c = ldg<v4i, false>((const char*)(a.counts + (int64_t)w * bins + b));
+      total += c;
+      if (w < (int32_t)blockIdx.x) before += c;
+    }
+    *(v4i*)&totals[wave][b] = total;
+    *(v4i*)&befores[wave][b] = before;
+  }
+  __syncthreads();
 
   // digits of lane t: consecutive ones, so that the scan over lanes is the scan over digits
   const int per = (bins + kSortThreads - 1) / kSortThreads;
@@ -261,17 +292,12 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
 #pragma unroll
   for (int j = 0; j < kMaxBins / kSortThreads; ++j) {
     const int b = t * per + j;
-    before[j] = 0;
+    before[j] = all;
     if (j >= per || b >= bins) continue;
-    int32_t total = 0;
-#pragma unroll 16
-    for (int32_t w = 0; w < a.tiles; ++w) {
-      const int32_t c = a.counts[(int64_t)w * bins + b];
-      before[j] += w < (int32_t)blockIdx.x ? c : 0;
-      total += c;
+    for (int w = 0; w < kSortWaves; ++w) {
+      before[j] += befores[w][b];
+      all += totals[w][b];
     }
-    before[j] += all;
-    all += total;
   }
   sums[t] = all;
   __syncthreads();
@@ -296,23 +322,27 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
   }
   __syncthreads();
 
-  for (int64_t i = begin + lane; i < begin + section; i += 64) {
-    int32_t pos = 0;
-    const int32_t key = entry<FIRST>(a, i, n, &pos);
-    const int digit = key >> a.shift & (bins - 1);
-    uint64_t same = __ballot(key >= 0);  // lanes of this lane's digit
-    for (int b = 0; b < a.bits; ++b) {
-      const bool one = digit >> b & 1;
-      const uint64_t m = __ballot(one);
-      same &= one ? m : ~m;
-    }
-    if (key >= 0) {
-      const int leader = __builtin_ctzll(same);
-      int32_t at = 0;
-      if (lane == leader) at = atomicAdd(&next[wave][digit], __popcll(same));
-      at = __shfl(at, leader) + __popcll(same & (((uint64_t)1 << lane) - 1));
-      a.keys_out[at] = key;
-      a.pos_out[at] = pos;
+  for (int64_t i = begin; i < end; i += kEntries * 64) {
+    int32_t keys[kEntries], pos[kEntries];
+    entries<FIRST>(a, i + lane, 64, end, keys, pos);
+#pragma unroll
+    for (int u = 0; u < kEntries; ++u) {
+      const int32_t key = keys[u];
+      const int digit = key >> a.shift & (bins - 1);
+      uint64_t same = __ballot(key >= 0);  // lanes of this lane's digit
+      for (int b = 0; b < a.bits; ++b) {
+        const bool one = digit >> b & 1;
+        const uint64_t m = __ballot(one);
+        same &= one ? m : ~m;
+      }
+      if (key >= 0) {
+        const int leader = __builtin_ctzll(same);
+        int32_t at = 0;
+        if (lane == leader) at = atomicAdd(&next[wave][digit], __popcll(same));
+        at = __shfl(at, leader) + __popcll(same & (((uint64_t)1 << lane) - 1));
+        a.keys_out[at] = key;
+        a.pos_out[at] = pos[u];
+      }
     }
   }
 }

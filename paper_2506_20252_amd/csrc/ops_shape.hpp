@@ -80,7 +80,7 @@ inline SortPlan sort_plan(int64_t ntokens, int64_t rows) {
   const int most = ntokens <= kSmallTokens ? kSmallBits : kMaxBits;
   SortPlan s;
   s.passes = (kb + most - 1) / most;
-  s.bits = (kb + s.passes - 1) / s.passes;
+  s.bits = std::max((kb + s.passes - 1) / s.passes, 2);  // histograms are read four digits at a time
   s.tile = (int64_t)ceil_div(ceil_div(ntokens, 128), kSortThreads) * kSortThreads;
   if (s.tile < 1024) s.tile = 1024;
   s.tiles = (int64_t)ceil_div(ntokens, s.tile);
