@@ -2,9 +2,9 @@
 // gradients of the 4-bit product.
 //
 // The sum runs over rows of q, across its blocks, so q is widened to bfloat16 (exactly) and multiplied by the bfloat16
-// matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane: a lane reads a
-// patch of q (a few codes from each of 8 rows), widens it and writes it to LDS turned round, one column of 8 values at
-// a time; likewise g where it is given by j.
+// matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane, while q, and g where
+// it is given by j, have consecutive columns in memory: they stand in LDS as they come, and gfx950's transposing reads
+// (ds_read_b64_tr_b16) turn them round on the way to the registers.
 #include <algorithm>
 
 #include "ops_device.hpp"
@@ -14,15 +14,15 @@ namespace {
 
 // A workgroup of WA x WB waves computes a tile of R x R of out, a wave FA x FB blocks of 32 x 32, going through j 64 at a
 // time.  While a step's 64 are multiplied out of one half of LDS, the next step's are widened from registers into the
-// other, and what the step after that needs is on its way into these registers.  The codes and scales of a wave's
-// patches come in one load each, 16 bytes and one byte a lane, and go to their lanes through a piece of LDS of the
-// wave's own: a load takes its 16 cycles of address work for 64 lanes whether they ask for one byte or 16 (with a load
-// for each row of a patch, 20 a wave and step, the loads took longer than the multiplications).  Of two waves on a SIMD
-// one multiplies first and the other widens first, so that the matrix unit and the vector unit both have work.
+// other, and what the step after that needs is on its way into these registers.  A wave's scales come in one load, a byte a
+// lane, and go to their lanes by a permutation: a load takes 16 cycles of address work however little it asks for.  Of two
+// waves on a SIMD one multiplies first and the other widens first, so that the matrix unit and the vector unit both have
+// work.
 //
-// Bound by the matrix instructions: 8192 x 4096 x 4096 in 236 us (g as given) and 247 us (g by j, float32 out), 1160 and
-// 1110 TFLOP/s, beside 1395 of a large bfloat16 library product.  1001 x 1000 x 1333: 15 and 17 us, the latency of 8
-// steps in turn with one workgroup a CU.
+// Bound by the matrix instructions: 8192 x 4096 x 4096 in 222 us (g as given) and 221 us (g by j, float32 out), 1240
+// TFLOP/s, beside 1395 of a large bfloat16 library product; turning q and g round by vector instructions on their way into
+// LDS took 228 and 240.  1001 x 1000 x 1333: 12.3 and 12.9 us (15 and 17), the latency of 8 steps in turn with one or two
+// workgroups a CU.
 //
 // PARTS: as many such groups of waves in a workgroup, each with its own part of j and its own LDS; their sums are added
 // in order at the end.  For few tiles, whose waves would otherwise wait for one another's latencies alone.
@@ -31,16 +31,11 @@ template <int FA, int FB, int WA, int WB>
 struct GradTile {
   static constexpr int kWaves = WA * WB, kThreads = 64 * kWaves, R = 32 * FA * WA;
   static_assert(R == 32 * FB * WB, "square");
-  static constexpr int PC = R * 8 / kThreads;  // columns of a patch: patches of 8 x PC, one a lane
-  static_assert(PC == 2 || PC == 4, "");
-  static constexpr int kRows = 64 / (R / PC) * 8;  // of q in a wave's patches
+  // A step's 64 rows of q are cut into pieces of 8 columns; a thread takes kEach of them, kSide rows apart.
+  static constexpr int kPieces = R / 8, kEach = 64 * kPieces / kThreads, kSide = kThreads / kPieces;
   struct Lds {
-    uint8_t g[R * 128];  // rows of out: 64 values of j
-    uint8_t q[R * 128];  // columns of out: 64 values of j
-  };
-  struct Stage {
-    uint8_t codes[kRows * (R / 2)];
-    uint8_t scales[(R / 32) * kRows];  // of 32 columns row after row, so that a patch's 8 are one load
+    uint8_t g[R * 128];  // 64 values of j for every row of out; where g is given by j, as q
+    uint8_t q[R * 128];  // 64 rows of q, widened
   };
 };
 
@@ -53,14 +48,22 @@ __device__ __forceinline__ int lds_at(int row, int block) {
   return at * 128 + (block ^ (at & 7) ^ (at >> 3 & 3)) * 16;
 }
 
-// Turns 8 rows of N bfloat16 (N / 2 words) round: column c's 8 values.
-template <int N>
-__device__ __forceinline__ v4u turned(const uint32_t (&rows)[8][N / 2], int c) {
-  v4u v;
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    v[r] = __builtin_amdgcn_perm(rows[2 * r + 1][c / 2], rows[2 * r][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
-  return v;
+// What is given by j stands by j, 64 rows of R values: a transposing read gives a lane 4 values of j of one column.  32 lanes
+// read 64 bytes of 4 rows that follow each other, so the 64-byte parts of a row are exchanged by its number, and all banks
+// are hit once.
+template <int R>
+__device__ __forceinline__ int exchange(int j) {
+  return R == 64 ? j >> 1 & 1 : j & 3;
+}
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s* LdsV4s;
+// Lane l's operand of a 32 x 32 x 16 instruction, j0 + 8 * (l / 32) ... + 7 of column l mod 32 of those 32 whose first part
+// for this lane is at `at`.
+template <int R>
+__device__ __forceinline__ v8bf read_turned(const uint8_t* at, int j0) {
+  const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4s)(at + j0 * 2 * R));
+  const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsV4s)(at + (j0 + 4) * 2 * R));
+  return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
 // Two codes of a byte (the I-th of a word) as two bfloat16.
@@ -70,14 +73,13 @@ __device__ __forceinline__ uint32_t widen2(uint32_t code, uint32_t s) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED, typename T>
+template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED, bool EDGE, typename T>
 __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner,
                                                                        int64_t cols, MatOut out, int64_t slice) {
   typedef GradTile<FA, FB, WA, WB> S;
   typedef typename S::Lds Lds;
-  constexpr int R = S::R, PC = S::PC, W = S::kWaves, NT = S::kThreads;
+  constexpr int R = S::R, W = S::kWaves, NT = S::kThreads, PIECES = S::kPieces, EACH = S::kEach, SIDE = S::kSide;
   __shared__ __attribute__((aligned(16))) Lds all_lds[PARTS][2];
-  __shared__ __attribute__((aligned(16))) typename S::Stage stages[PARTS][W];
   TilePlace place;
   if (!tile_place((rows + R - 1) / R, (cols + R - 1) / R, &place)) return;
   const int64_t i0 = place.i * R, c0 = place.j * R;
@@ -93,112 +95,79 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / NT);
   const int tid = threadIdx.x % NT, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   Lds* lds = all_lds[part];
-  typename S::Stage& stage = stages[part][wave];
 
-  // What a lane reads of 64 values of j.  q: a patch of 8 x PC, the columns' patches side by side over the lanes.
-  // g by rows: PC blocks of 8 values, 8 of them a row.  g by j: a patch like q's.
+  // What a lane reads of 64 values of j.  q: the codes of 8 columns of EACH rows, and the scale of one of the wave's 16 * EACH
+  // groups of 32.  g by j: 8 rows of out at the same EACH j.  g by rows: blocks of 8 values of j, 8 of them a row.
   // Nothing is read beyond a matrix: rows of out beyond the last are the last again, j beyond the last likewise and
-  // zeroed before they reach LDS, and a block or patch that would go over a row's end ends there instead.
-  const int patch_c = tid % (R / PC), patch_j = tid / (R / PC);
-  constexpr int CHUNKS = R / 32, ROWS_Q = S::kRows;  // 16-byte pieces of a tile's row of codes, as many as its scales
-  const int first_j = wave * ROWS_Q;                 // of the wave's patches
-  const int patch_row = lane / (R / PC) * 8, patch_shift = patch_c * PC % 8 * 4;  // of a patch in these; in a word of codes
-  const int q_row = lane / CHUNKS;                   // what this lane loads: a row's piece of codes and its scale
-  const uint32_t q_at = (uint32_t)(min(q_row, ROWS_Q - 1) * pitch + min(c0 / 2 + lane % CHUNKS * 16, pitch - 16));
-  const uint32_t q_scale_at = (uint32_t)(min(q_row, ROWS_Q - 1) * (pitch / 16) + min(c0 / 32 + lane % CHUNKS, pitch / 16 - 1));
-  const int64_t gi = min(i0 + patch_c * PC, rows - PC);       // TRANSPOSED: the patch's first row of out
-  const int to_row = (int)(gi - i0);                          // its place in the tile, negative for a short last tile
-  const int block = tid % 8, row_u = swap02(tid / 8);         // by rows: block and row of each NT / 8 rows
+  // zeroed before they reach LDS, and a piece or block that would go over a row's end ends there instead.
+  const int piece = tid % PIECES, first = tid / PIECES;
+  const int put = first * 2 * R + (piece / 4 ^ exchange<R>(first)) * 64 + piece % 4 * 16;  // in LDS
+  constexpr int GROUPS = R / 32;
+  const int scale_j = wave * (64 / PIECES) + lane % 16 / GROUPS + min(lane / 16, EACH - 1) * SIDE;
+  const int scale_of = 4 * (lane / PIECES * GROUPS + piece / 4);  // the lane that has this lane's, 16 lanes further for each row
+  const uint32_t q_at = (uint32_t)(first * pitch + min(c0 / 2 + piece * 4, pitch - 4));
+  const uint32_t q_scale_at = (uint32_t)(scale_j * (pitch / 16) + min(c0 / 32 + lane % GROUPS, pitch / 16 - 1));
+  const int64_t gi = min(i0 + piece * 8, rows - 8);  // TRANSPOSED: the first row of out that is read
+  const int over = (int)min(i0 + piece * 8 - gi, (int64_t)8);
+  constexpr int BLOCKS = R * 8 / NT;
+  const int block = tid % 8, row_u = swap02(tid / 8);  // by rows: block and row of each NT / 8 rows
   // of g: from the tile's corner, 32 bits (rows are not too far apart for that)
-  constexpr int ROWS = TRANSPOSED ? 1 : PC;
+  constexpr int ROWS = TRANSPOSED ? 1 : BLOCKS, VECTORS = TRANSPOSED ? EACH : BLOCKS;
   uint32_t g_at[ROWS];
 #pragma unroll
   for (int u = 0; u < ROWS; ++u)
-    g_at[u] = 2 * (uint32_t)(TRANSPOSED ? patch_j * 8 * g.stride + gi
+    g_at[u] = 2 * (uint32_t)(TRANSPOSED ? first * g.stride + gi
                                         : (min(i0 + u * (NT / 8) + row_u, rows - 1) - i0) * g.stride + block * 8);
   const char* g_base = (const char*)g.p + (TRANSPOSED ? 0 : 2 * i0 * g.stride);
 
-  v4u codes;
-  uint32_t scales;
-  uint32_t raw_t[8][PC / 2];  // TRANSPOSED: 8 values of j by PC rows
-  Raw8<B16> raw[PC];          // else: blocks of 8 j
+  uint32_t codes[EACH], scales;
+  Raw8<B16> raw[VECTORS];
 
   // TAIL: perhaps fewer than 64 values of j are left.
   auto fetch = [&](int64_t j0, auto tail) {
     constexpr bool TAIL = decltype(tail)::value;
     const int left = TAIL ? (int)min(inner - j0, (int64_t)64) : 64;
-    {  // an address is the wave's and a lane's part of 32 bits; rows beyond the last are it again
-      const int64_t j = j0 + first_j, back = TAIL ? max(first_j + min(q_row, ROWS_Q - 1) - (left - 1), 0) : 0;
-      codes = ldg<v4u, false>((const char*)q.codes + j * pitch + (TAIL ? q_at - back * pitch : q_at));
-      scales = ldg<uint8_t, false>((const char*)q.scales + j * (pitch / 16) +
-                                   (TAIL ? q_scale_at - back * (pitch / 16) : q_scale_at));
-    }
-    if constexpr (TRANSPOSED) {
+    // an address is the wave's and a lane's part of 32 bits; rows beyond the last are it again
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const int back = TAIL ? max(patch_j * 8 + r - (left - 1), 0) : 0;
-        const char* t = g_base + 2 * (j0 + r) * g.stride + (TAIL ? g_at[0] - 2 * back * g.stride : g_at[0]);
-        if constexpr (PC == 4) {
-          const v2u v = ldg<v2u, false, 2>(t);
-          raw_t[r][0] = v[0], raw_t[r][PC / 2 - 1] = v[1];
-        } else {
-          raw_t[r][0] = ldg<uint32_t, false, 2>(t);
-        }
-      }
+    for (int u = 0; u < EACH; ++u) {
+      const int64_t j = j0 + u * SIDE, back = TAIL ? max(first + u * SIDE - (left - 1), 0) : 0;
+      codes[u] = ldg<uint32_t, false>((const char*)q.codes + j * pitch + (TAIL ? q_at - back * pitch : q_at));
+      if constexpr (TRANSPOSED)
+        raw[u].w[0] = ldg<v4u, false, 2>(g_base + 2 * j * g.stride + (TAIL ? g_at[0] - 2 * back * g.stride : g_at[0]));
+    }
+    {
+      const int64_t back = TAIL ? max(scale_j - (left - 1), 0) : 0;
+      scales = ldg<uint8_t, false>((const char*)q.scales + j0 * (pitch / 16) +
+                                   (TAIL ? q_scale_at - back * (pitch / 16) : q_scale_at));
     }
     if constexpr (!TRANSPOSED) {
       const int64_t back = TAIL ? max(j0 + block * 8 - (inner - 8), (int64_t)0) : 0;
 #pragma unroll
-      for (int u = 0; u < PC; ++u)
+      for (int u = 0; u < BLOCKS; ++u)
         raw[u].w[0] = ldg<v4u, false, 2>(g_base + 2 * j0 + (TAIL ? g_at[u] - 2 * back : g_at[u]));
     }
   };
   auto widen = [&](Lds& l, int64_t j0, auto tail) {
-    if (q_row < ROWS_Q) {
-      *(v4u*)(stage.codes + lane * 16) = codes;
-      stage.scales[lane % CHUNKS * ROWS_Q + q_row] = (uint8_t)scales;
-    }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    uint32_t code[8], scale[8];
-    const v2u s8 = *(const v2u*)(stage.scales + patch_c * PC / 32 * ROWS_Q + patch_row);
+    constexpr bool TAIL = decltype(tail)::value;
+    const int left = TAIL ? (int)min(inner - j0, (int64_t)64) : 64;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {  // of this lane's patch; whole words, which LDS gives two at a time
-      code[r] = *(const uint32_t*)(stage.codes + (patch_row + r) * (R / 2) + patch_c * PC / 8 * 4) >> patch_shift;
-      scale[r] = s8[r / 4] >> (r % 4 * 8) & 255u;
-    }
-    if constexpr (decltype(tail)::value) {
-      const int left = (int)min(inner - j0, (int64_t)64);
-#pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const bool in = patch_j * 8 + r < left;
-        code[r] = in ? code[r] : 0u;
-        scale[r] = in ? scale[r] : 0u;
-        if constexpr (TRANSPOSED) {
-#pragma unroll
-          for (int w = 0; w < PC / 2; ++w) raw_t[r][w] = in ? raw_t[r][w] : 0u;
-        }
-      }
-      if constexpr (!TRANSPOSED) {
-        const int d = min(max(block * 8 - (left - 8), 0), 8);
-#pragma unroll
-        for (int u = 0; u < PC; ++u) move_down(raw[u], d);
+    for (int u = 0; u < EACH; ++u) {
+      uint32_t code = codes[u], s = __builtin_amdgcn_ds_bpermute(scale_of + 64 * u, scales);
+      const bool in = !TAIL || first + u * SIDE < left;
+      if (TAIL) code = in ? code : 0u, s = in ? s : 0u;
+      *(v4u*)(l.q + put + u * SIDE * 2 * R) = v4u{widen2<0>(code, s), widen2<1>(code, s), widen2<2>(code, s), widen2<3>(code, s)};
+      if constexpr (TRANSPOSED) {
+        if constexpr (EDGE) move_down(raw[u], over);
+        if (TAIL && !in) raw[u].w[0] = v4u{0, 0, 0, 0};
+        *(v4u*)(l.g + put + u * SIDE * 2 * R) = raw[u].w[0];
       }
     }
-    uint32_t wide[8][PC / 2];
+    if constexpr (!TRANSPOSED) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      wide[r][0] = widen2<0>(code[r], scale[r]);
-      if constexpr (PC == 4) wide[r][PC / 2 - 1] = widen2<1>(code[r], scale[r]);
-    }
-#pragma unroll
-    for (int c = 0; c < PC; ++c) *(v4u*)(l.q + lds_at(patch_c * PC + c, patch_j)) = turned<PC>(wide, c);
-    if constexpr (TRANSPOSED) {
-#pragma unroll
-      for (int c = 0; c < PC; ++c)
-        if (to_row + c >= 0) *(v4u*)(l.g + lds_at(to_row + c, patch_j)) = turned<PC>(raw_t, c);
-    } else {
-#pragma unroll
-      for (int u = 0; u < PC; ++u) *(v4u*)(l.g + lds_at(u * (NT / 8) + row_u, block)) = raw[u].w[0];
+      for (int u = 0; u < BLOCKS; ++u) {
+        if constexpr (TAIL) move_down(raw[u], min(max(block * 8 - (left - 8), 0), 8));
+        *(v4u*)(l.g + lds_at(u * (NT / 8) + row_u, block)) = raw[u].w[0];
+      }
     }
   };
 
@@ -213,15 +182,22 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 
   // An instruction of 32 x 32 x 16: lane l has row l mod 32 and j = 8 * (l / 32) ... + 7.  A block of g is read from LDS
   // a block before its instructions, those of q a step of 16 values of j before.
+  const int turned_j = lane % 16 / 4 + 8 * half, turned_part = lane / 16 % 2 * 32 + lane % 4 * 8;
+  auto turned_at = [&](int column) {  // of 32 columns, for read_turned
+    return turned_j * 2 * R + (column / 32 ^ exchange<R>(turned_j)) * 64 + turned_part;
+  };
+  int g_first = lds_at(wave_row + lane % 32, half);  // by rows: of the wave's first block; the others' places follow from it
   auto multiply = [&](const Lds& l) {
     v8bf bg[2], bq[2][FB];
+    // made here every time: kept over the loop, the places of all blocks would cost the registers that are left
+    if constexpr (!TRANSPOSED) asm volatile("" : "+v"(g_first));
     auto read_g = [&](int n) {
-      bg[n % 2] = *(const v8bf*)(l.g + lds_at(wave_row + 32 * (n % FA) + lane % 32, n / FA * 2 + half));
+      if constexpr (TRANSPOSED) bg[n % 2] = read_turned<R>(l.g + turned_at(wave_row + 32 * (n % FA)), n / FA * 16);
+      else bg[n % 2] = *(const v8bf*)(l.g + (g_first ^ n / FA * 32) + n % FA * 4096);
     };
     auto read_q = [&](int step) {
 #pragma unroll
-      for (int y = 0; y < FB; ++y)
-        bq[step % 2][y] = *(const v8bf*)(l.q + lds_at(wave_col + 32 * y + lane % 32, step * 2 + half));
+      for (int y = 0; y < FB; ++y) bq[step % 2][y] = read_turned<R>(l.q + turned_at(wave_col + 32 * y), step * 16);
     };
     read_q(0);
     read_g(0);
@@ -363,8 +339,11 @@ hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, M
   const size_t tiles = ceil_div(rows, R) * ceil_div(cols, R);
   const bool sliced = p.slices > 1, f32 = dtype == Elem::f32;
   const MatOut to = sliced ? MatOut{workspace, slice_pitch(cols)} : out;
-  const auto kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, F32>
-                                    : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, B16>;
+  auto kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, false, F32>
+                              : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, false, B16>;
+  if (TRANSPOSED && rows % 8)
+    kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, F32>
+                           : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, B16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8), (unsigned)p.slices), dim3(64 * WA * WB * PARTS), 0,
                      stream, g, q, rows, inner, cols, to, p.slice);
   if (sliced) {

@@ -395,7 +395,7 @@ def test_products_carry_what_is_not_finite(m, n, k):
 
 GRADS = [(1, 1, 1), (1, 16, 32), (3, 40, 33), (16, 32, 128), (33, 65, 100), (64, 64, 64), (70, 129, 257), (128, 128, 128),
          (130, 70, 300), (256, 128, 256), (300, 200, 520), (20, 3000, 40), (257, 1000, 129), (1000, 5, 130), (64, 31, 640), (100, 4096, 90), (64, 5761, 33), (40, 8449, 200), (130, 8, 64),
-         (9, 7, 300), (7, 500, 40), (520, 700, 600)]
+         (9, 7, 300), (7, 500, 40), (520, 700, 600), (1500, 330, 1490), (1537, 70, 1501), (2901, 390, 2900), (2896, 261, 2950)]
 
 
 @gpu
