@@ -22,11 +22,10 @@ inline int row_lanes(int64_t vectors, int threads) {
 // add_kernel adds up.
 //
 // The largest tile that gives more than half of the 256 CUs one, as for the 4-bit product (us with tiles of 64, 128, 256:
-// 153, 88, 102 for 2048 rows, 4096 columns and values of j; 305, 170, 121 for 4096 rows).  Below, few tiles of 128 and
-// a long sum are sliced (us, and with tiles of 64: 20 and 26 for 64 rows, 4096 columns and values of j; 22 and 55 for 512
-// rows and columns, 8192 values of j; but 22 and 18 for 1024 rows and columns, 2048 values of j), the others take tiles of
-// 64 with two groups of waves (us, and with one group: 15.5 and 15.3 for 1001 x 1333 and 1000 values of j, 39 and 43 for 4000,
-// 27 and 38 for one tile).
+// 134, 80, 95 for 2048 rows, 4096 columns and values of j; 263, 154, 112 for 4096 rows).  Below, few tiles of 128 and
+// a long sum are sliced (us, and with tiles of 64: 21 and 36 for 512 rows and columns, 8192 values of j; 19 and 20 for 64
+// rows, 4096 columns and values of j), the others take tiles of 64 with two groups of waves (us, and with one group: 10.0 and
+// 9.5, 13.7 and 13.6, 33 and 37 for 1001 x 1333 and 500, 1000, 4000 values of j; 19 and 27 for one tile and 4096).
 struct GradPlan {
   int tile, slices;
   int64_t slice;
