@@ -120,8 +120,8 @@ pat_status_t pat_embedding(const void* tokens, int token_bytes, size_t ntokens, 
 /*
  * Its gradient, dense: out[v][c] = scale * sum of g[t][c] over the t with
  * tokens[t] == first + v, 0 where there is none.  g: ntokens x cols; out: rows x
- * cols, every element written.  Tokens are sorted (stable) first; a row's sum runs
- * over its tokens in rising t, in pieces whose partial sums are added in order.
+ * cols, every element written.  A row's sum runs over its tokens in rising t, in
+ * pieces whose partial sums are added in order.
  * Fewer than 2^28 tokens and rows, 2^23 columns (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_embedding_grad(const void* tokens, int token_bytes, size_t ntokens, const void* g, int64_t g_stride,

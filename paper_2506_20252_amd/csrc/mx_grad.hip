@@ -17,7 +17,7 @@ namespace {
 // other, and what the step after that needs is on its way into these registers.  A wave's scales come in one load, a byte a
 // lane, and go to their lanes by a permutation: a load takes 16 cycles of address work however little it asks for.  Of two
 // waves on a SIMD one multiplies first and the other widens first, so that the matrix unit and the vector unit both have
-// work.
+// work (229 and 226 us for the sizes below on one card, 236 and 235 with all in the same order).
 //
 // Bound by the matrix instructions: 8192 x 4096 x 4096 in 222 us (g as given) and 221 us (g by j, float32 out), 1240
 // TFLOP/s, beside 1395 of a large bfloat16 library product; turning q and g round by vector instructions on their way into
@@ -39,14 +39,9 @@ struct GradTile {
   };
 };
 
-// Where 16-byte block `block` (8 values of j) of a row stands.  A row is half of the 64 banks; 16 lanes that read one
-// block of consecutive rows hit all banks once, 16 lanes that write one block of every fourth row all banks of two.
-// Rows 32 apart are a constant apart.
-__device__ __forceinline__ int swap02(int row) { return (row & ~5) | (row & 1) << 2 | (row >> 2 & 1); }
-__device__ __forceinline__ int lds_at(int row, int block) {
-  const int at = swap02(row);
-  return at * 128 + (block ^ (at & 7) ^ (at >> 3 & 3)) * 16;
-}
+// Where 16-byte block `block` (8 values of j) of a row of g given by rows stands.  A row is half of the 64 banks: 16 lanes
+// that read one block of consecutive rows, or write two whole rows, hit all banks once.  Rows 32 apart are a constant apart.
+__device__ __forceinline__ int lds_at(int row, int block) { return row * 128 + (block ^ (row >> 1 & 7)) * 16; }
 
 // What is given by j stands by j, 64 rows of R values: a transposing read gives a lane 4 values of j of one column.  32 lanes
 // read 64 bytes of 4 rows that follow each other, so the 64-byte parts of a row are exchanged by its number, and all banks
@@ -110,7 +105,7 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   const int64_t gi = min(i0 + piece * 8, rows - 8);  // TRANSPOSED: the first row of out that is read
   const int over = (int)min(i0 + piece * 8 - gi, (int64_t)8);
   constexpr int BLOCKS = R * 8 / NT;
-  const int block = tid % 8, row_u = swap02(tid / 8);  // by rows: block and row of each NT / 8 rows
+  const int block = tid % 8, row_u = tid / 8;  // by rows: block and row of each NT / 8 rows
   // of g: from the tile's corner, 32 bits (rows are not too far apart for that)
   constexpr int ROWS = TRANSPOSED ? 1 : BLOCKS, VECTORS = TRANSPOSED ? EACH : BLOCKS;
   uint32_t g_at[ROWS];
