@@ -34,8 +34,9 @@ __device__ __forceinline__ v4u philox(uint64_t block, uint64_t key) {
 // without gaps in memory and in numbering come as one row.  Whole blocks are read and written as vectors at
 // element-aligned addresses.
 //
-// Bound by memory: 8192 x 8192 bfloat16 with a residual (403 MB) in 70 us, 5.7 TB/s, with the generator's
-// multiplications under the loads.  Two blocks a lane, both read before either is numbered.
+// Bound by memory: 16384 x 4096 bfloat16 with a residual (403 MB) in 60 us, 6.7 TB/s, with the generator's
+// multiplications under the loads.  Two blocks a lane, both read before either is numbered.  Loads are nontemporal, stores
+// are not (us: 60; both 63, neither 71).
 constexpr int kBlocks = 2;
 
 struct RowSplit {
@@ -51,7 +52,7 @@ __device__ __forceinline__ Raw8<T> load_part(const char* p, int lo, int hi) {
   for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = v4u{0, 0, 0, 0};
   if (WHOLE || (lo == 0 && hi == 8)) {
 #pragma unroll
-    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(p + 16 * i);
+    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, true, T::kBytes>(p + 16 * i);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -8,8 +8,8 @@ namespace {
 // each other, also from row to row, is consecutive, so codes and scales leave as whole words in order.  A workgroup
 // takes 16 groups side by side and kGroups of those in turn, all read before any is written.
 //
-// Bound by memory: 8192 x 8192 bfloat16 (170 MB) in 28 us, 6.0 TB/s (36 where the input comes from HBM and the output
-// evicts it); 1001 x 1000 float32 (4.5 MB) in 3.6 us, of which 3 are a launch of anything.
+// Bound by memory: 8192 x 8192 bfloat16 (170 MB) in 27 us, 6.3 TB/s, by nontemporal loads (29 otherwise, and
+// 8192 x 8192 x 8192 with it took 12 longer); 1001 x 1000 float32 (4.5 MB) in 3.6 us, of which 3 are a launch of anything.
 constexpr int kGroups = 4;
 
 template <typename T>
@@ -23,7 +23,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(Mat x, uint32_t total, in
 #pragma unroll
       for (int u = 0; u < kGroups; ++u) {
         const uint32_t g = min(base + u * 16 + threadIdx.x / 16, total - 1), row = groups.divide(g);
-        r[u] = load_raw8<T, C>((const char*)x.p + (int64_t)row * x.stride * T::kBytes,
+        r[u] = load_raw8<T, C, true>((const char*)x.p + (int64_t)row * x.stride * T::kBytes,
                                (int64_t)(g - row * groups.d) * 128 + sub * 8, cols);
       }
 #pragma unroll

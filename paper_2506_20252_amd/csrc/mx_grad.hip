@@ -270,7 +270,8 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
           for (int e = 0; e < 16; ++e) acc[x][y][e] += at(p, x, y, e);
   }
   static_assert(W * tile_part(FB) * 4 <= 2 * sizeof(Lds), "");
-  write_tile<FA, FB, T>(acc, (float*)lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
+  // nontemporal, as the 4-bit product's, the stores cost 4 % of 8192 x 4096 x 4096
+  write_tile<FA, FB, T, false>(acc, (float*)lds, wave, wave_row, wave_col, i0, c0, rows, cols, out);
 }
 
 // The same product where the vectors of 8 above do not exist (fewer than 8 values of j, or of rows where g is given by j),

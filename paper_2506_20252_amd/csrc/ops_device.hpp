@@ -180,13 +180,13 @@ __device__ __forceinline__ void move_down(Raw8<F32>& r, int d) {
     }
   }
 }
-template <typename T, Cover C>
+template <typename T, Cover C, bool NT = false>
 __device__ __forceinline__ Raw8<T> load_raw8(const char* row, int64_t c, int64_t cols) {
   Raw8<T> r;
   if constexpr (C == kEnd) {
     const int64_t at = min(c, cols - 8);
 #pragma unroll
-    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(row + at * T::kBytes + 16 * i);
+    for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, NT, T::kBytes>(row + at * T::kBytes + 16 * i);
     return r;
   }
 #pragma unroll
@@ -194,7 +194,7 @@ __device__ __forceinline__ Raw8<T> load_raw8(const char* row, int64_t c, int64_t
   if constexpr (C == kWhole) {
     if (c < cols) {
 #pragma unroll
-      for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, false, T::kBytes>(row + c * T::kBytes + 16 * i);
+      for (int i = 0; i < T::kBytes / 2; ++i) r.w[i] = ldg<v4u, NT, T::kBytes>(row + c * T::kBytes + 16 * i);
     }
   } else {
 #pragma unroll
@@ -299,7 +299,7 @@ __device__ __forceinline__ bool tile_place(int64_t tiles_m, int64_t tiles_n, Til
 // them as vectors.  Nobody may still be reading that LDS when the last wave comes here: the barrier is in here.
 constexpr int tile_part(int fb) { return 32 * (32 * fb + 8); }  // rows 8 banks apart, for the halves' rows of 4 apart
 
-template <int FA, int FB, typename T>
+template <int FA, int FB, typename T, bool NT>
 __device__ __forceinline__ void write_tile(const v16f (&acc)[FA][FB], float* lds, int slot, int wave_row, int wave_col,
                                            int64_t i0, int64_t j0, int64_t rows, int64_t cols, MatOut out) {
   constexpr int C = 32 * FB, P = C + 8, LANES = C / 8;  // columns, their pitch, lanes a row with 8 columns each
@@ -320,8 +320,8 @@ __device__ __forceinline__ void write_tile(const v16f (&acc)[FA][FB], float* lds
       const v4f lo = *(const v4f*)(part + r * P + c), hi = *(const v4f*)(part + r * P + c + 4);
       const float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
       char* p = (char*)out.p + (i * out.stride + j) * T::kBytes;
-      if (i < rows && cols - j >= 8) store8<T, false, false, kWhole>(p, 8, 4, v);
-      else if (i < rows && cols > j) store8<T, false, false, kEnd>(p, cols - j, 4, v);
+      if (i < rows && cols - j >= 8) store8<T, false, NT, kWhole>(p, 8, 4, v);
+      else if (i < rows && cols > j) store8<T, false, NT, kEnd>(p, cols - j, 4, v);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   }
