@@ -34,10 +34,11 @@ __device__ __forceinline__ v8i frag(v4i c) { return v8i{c[0], c[1], c[2], c[3], 
 // row l mod 32 and one block, and any two blocks will do as long as both sides take the same.  Lane half h takes blocks
 // 2h and 2h + 1 of a group in turn, whose scales are two neighbouring bytes: the instruction picks the byte.
 //
-// 8192 x 8192 x 8192: 270 to 300 us, 4.1 to 3.7 PFLOP/s, where the instructions alone take 160 for these columns, the loads
-// alone 190 (45 GB/s a CU: 12 % of what is read from L2 is not there) and the reads of LDS nearly the cycles of the
+// 8192 x 8192 x 8192: 255 to 300 us by card, 4.3 to 3.7 PFLOP/s, where the instructions alone take 160 for these columns, the
+// loads alone 190 (45 GB/s a CU: 12 % of what is read from L2 is not there) and the reads of LDS nearly the cycles of the
 // instructions; 25 us are each tile's first loads and its stores.  Four waves of 128 x 128 take as long as these eight.
-// Slower: four groups of 128 columns in LDS (330: pieces of 64 bytes), a barrier of its own for the release of LDS (290).
+// Slower: four groups of 128 columns in LDS (330: pieces of 64 bytes), a barrier of its own for the release of LDS (290
+// beside 277).
 
 template <int FA, int FB, int WA, int WB>
 struct Tile {
