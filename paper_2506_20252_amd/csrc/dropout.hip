@@ -3,8 +3,6 @@
 // One Philox4x32-10 call gives the 16-bit numbers of 8 consecutive elements (numbered over the whole tensor), so a lane
 // takes the 8 elements of a generator block.  16 bits instead of 32 halve the generator's work, whose 20 wide
 // multiplications otherwise cost more than the memory; p is met to 2^-17, and the scale belongs to the p that is.
-#include <algorithm>
-
 #include "ops_device.hpp"
 
 namespace pat {
@@ -37,7 +35,7 @@ __device__ __forceinline__ v4u philox(uint64_t block, uint64_t key) {
 // Bound by memory: 16384 x 4096 bfloat16 with a residual (403 MB) in 60 us, 6.7 TB/s, with the generator's
 // multiplications under the loads.  Two blocks a lane, both read before either is numbered.  Loads are nontemporal, stores
 // are not (us: 60; both 63, neither 71).
-constexpr int kBlocks = 2;
+constexpr int kBlocks = kDropoutBlocks;
 
 struct RowSplit {
   int lanes;
@@ -125,20 +123,15 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, RowSplit sp
 
 hipError_t launch_dropout(const DropoutArgs& given, Elem dtype, hipStream_t stream) {
   DropoutArgs a = given;
-  const bool flat = a.rows > 1 && a.rows <= ((int64_t)1 << 36) / a.cols &&  // what a grid holds
-                    a.x.stride == a.cols && a.out.stride == a.cols && a.index_stride == (uint64_t)a.cols &&
-                    (!a.residual.p || a.residual.stride == a.cols);
-  if (flat) {
+  const DropoutPlan plan = dropout_plan(a.rows, a.cols,
+                                        a.x.stride == a.cols && a.out.stride == a.cols && a.index_stride == (uint64_t)a.cols &&
+                                            (!a.residual.p || a.residual.stride == a.cols));
+  if (plan.flat) {
     a.cols *= a.rows;
     a.rows = 1;
   }
-  const int64_t blocks = (a.cols + 7) / 8 + 1;  // one more where rows begin inside a block
-  RowSplit split;
-  split.lanes = row_lanes((int64_t)ceil_div(blocks, kBlocks), 256);
-  split.tiles = (uint32_t)ceil_div(blocks, (int64_t)split.lanes * kBlocks);
-  const size_t row_wgs = ceil_div(a.rows, 256 / split.lanes);
-  const size_t most = std::max<size_t>(((size_t)1 << 22) / split.tiles, 1);
-  const dim3 grid((unsigned)(std::min(row_wgs, most) * split.tiles));
+  const RowSplit split{plan.lanes, (uint32_t)plan.tiles};
+  const dim3 grid((unsigned)plan.wgs);
   const auto kernel = dtype == Elem::f32 ? (a.residual.p ? dropout_kernel<F32, true> : dropout_kernel<F32, false>)
                                          : (a.residual.p ? dropout_kernel<B16, true> : dropout_kernel<B16, false>);
   hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, split);

@@ -16,6 +16,31 @@ inline int row_lanes(int64_t vectors, int threads) {
   return lanes;
 }
 
+// ---- dropout ---------------------------------------------------------------------------------------------------
+
+// Rows without gaps in memory and in numbering (`dense`) are taken as one row where a launch holds its workgroups, which
+// have 256 lanes: fewer than 2^32 lanes.  A row takes `lanes` lanes, kDropoutBlocks generator blocks a lane in turn, and
+// `tiles` workgroups; `wgs` workgroups in all go through the rows.
+constexpr int kDropoutBlocks = 2;
+constexpr int64_t kDropoutFlat = 8 * (256 * kDropoutBlocks * (((int64_t)1 << 24) - 1) - 1);  // elements of 2^24 - 1 workgroups
+
+struct DropoutPlan {
+  bool flat;
+  int lanes;
+  int64_t tiles, wgs;
+};
+
+inline DropoutPlan dropout_plan(int64_t rows, int64_t cols, bool dense) {
+  DropoutPlan p;
+  p.flat = dense && rows > 1 && rows <= kDropoutFlat / cols;
+  const int64_t blocks = ((p.flat ? rows * cols : cols) + 7) / 8 + 1;  // one more where rows begin inside a block
+  p.lanes = row_lanes((int64_t)ceil_div(blocks, kDropoutBlocks), 256);
+  p.tiles = (int64_t)ceil_div(blocks, (int64_t)p.lanes * kDropoutBlocks);
+  const int64_t row_wgs = (int64_t)ceil_div(p.flat ? 1 : rows, 256 / p.lanes);
+  p.wgs = std::min(row_wgs, std::max(((int64_t)1 << 22) / p.tiles, (int64_t)1)) * p.tiles;
+  return p;
+}
+
 // ---- gradients of the 4-bit product ----------------------------------------------------------------------------
 
 // How a product is cut: the tile's size, and slices of j that get workgroups and a float32 matrix of their own, which

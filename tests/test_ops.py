@@ -138,6 +138,21 @@ def test_host_side_under_asan_ubsan(tmp_path):
     assert " 0 failures" in res.stdout
 
 
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir("/opt/rocm/include/hip"),
+                    reason="no g++ or no HIP headers")
+def test_launches_hold_their_lanes(tmp_path):
+    """Every size that is accepted gives a launch of fewer than 2^32 lanes that reaches all of its work."""
+    exe = tmp_path / "ops_grid_check"
+    csrc = os.path.join(ROOT, "paper_2506_20252_amd", "csrc")
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", csrc,
+           os.path.join(ROOT, "tests", "host", "ops_grid_check.cpp"), "-o", str(exe)]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, (res.stdout[-2000:], res.stderr[-2000:])
+    assert " 0 failures" in res.stdout
+
+
 @pytest.mark.parametrize("source", ["mx.hip", "mx_product.hip", "mx_grad.hip", "embedding.hip", "dropout.hip"])
 def test_kernels_as_compiled(source, tmp_path):
     """No scratch memory, no packed fp32; a workgroup of eight waves and more leaves two waves a SIMD their registers."""
