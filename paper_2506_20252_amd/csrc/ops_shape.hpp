@@ -74,6 +74,11 @@ inline GradPlan grad_plan(int64_t rows, int64_t inner, int64_t cols) {
   return p;
 }
 
+// Workgroups of narrow_kernel, 64 lanes each; tiles of 16 x 16 beyond a launch's are taken in turn.
+inline int64_t narrow_wgs(int64_t rows, int64_t cols) {
+  return std::min((int64_t)(ceil_div(rows, 16) * ceil_div(cols, 16)), (int64_t)1 << 22);
+}
+
 // ---- embedding gradient ----------------------------------------------------------------------------------------
 
 constexpr int kSortThreads = 256, kMaxBits = 10;  // of a sorting workgroup; of a pass's digit

@@ -34,6 +34,15 @@ static void check_dropout(int64_t rows, int64_t cols) {
   if (rows > 1 && rows * cols <= (int64_t)1 << 35) CHECK(dropout_plan(rows, cols, true).flat, "%lld %lld", r, c);
 }
 
+// Accepted: fewer than 2^26 rows and columns, and 2^31 tiles of 16 x 16.
+static void check_product(int64_t rows, int64_t cols) {
+  const int64_t most = ((int64_t)1 << 26) - 1;
+  if (rows < 1 || cols < 1 || rows > most || cols > most) return;
+  if ((rows + 15) / 16 * ((cols + 15) / 16) >= (int64_t)1 << 31) return;
+  const int64_t wgs = narrow_wgs(rows, cols);
+  CHECK(wgs >= 1 && wgs * 64 < kLanes, "%lld %lld: %lld workgroups", (long long)rows, (long long)cols, (long long)wgs);
+}
+
 int main() {
   unsigned long long x = 88172645463325252ull;
   auto rnd = [&](int64_t most) {  // 1 ... most, spread over the logarithm
@@ -52,6 +61,10 @@ int main() {
       }
   for (int i = 0; i < 200000; ++i) check_dropout(rnd(most), rnd(most));
   check_dropout(most, most);
+  for (int e = 0; e <= 26; ++e)
+    for (int f = 0; f <= 26; ++f)
+      for (int d = -17; d <= 17; ++d) check_product(((int64_t)1 << e) + d, ((int64_t)1 << f) + d);
+  for (int i = 0; i < 200000; ++i) check_product(rnd(most >> 5), rnd(most >> 5));
   std::printf("%d checks, %d failures\n", g_checked, g_failures);
   return g_failures != 0;
 }

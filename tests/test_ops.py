@@ -429,6 +429,21 @@ def test_matmul_grad(rows, inner, cols, transposed, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("rows,cols", [(131075, 131072), (40001, 40003)])
+def test_matmul_grad_of_more_tiles_than_workgroups(rows, cols):
+    """Outer products of more 16 x 16 tiles than one launch has workgroups, the first of 2^34 values and more: each value is
+    one product, exact in float32 and rounded once."""
+    g = values((1, rows), 1, B16)
+    q, vq = random_mx(1, cols, 2)
+    row = torch.from_numpy(vq[0]).float().cuda()
+    out = torch.full((rows, cols), 5.0, dtype=B16, device="cuda")
+    ops.mx_matmul_grad(g, q, B16, True, out)
+    for r0 in range(0, rows, 4096):
+        part = slice(r0, min(r0 + 4096, rows))
+        assert torch.equal(out[part], (g[0, part, None].float() * row).to(B16)), r0
+
+
+@gpu
 def test_matmul_gradients_against_differences():
     """The product is linear in each value of its factors, so a changed code changes sum(g * out) by the change
     times that value's gradient, up to the sums' rounding."""
