@@ -53,6 +53,7 @@ extern "C" {
  * Rows are filled up to whole groups of 128 values, codes and scales with
  * zeros, so every kernel may read whole groups, and both buffers of any number
  * of rows are whole 32-bit words: pat_allgather moves them as PAT_INT32.
+ * Fewer than 2^31 groups in all (rows * G, else PAT_ERR_UNSUPPORTED).
  */
 #define PAT_MX_GROUP 128
 #define PAT_MX_CODE_BYTES(cols) (((size_t)(cols) + 127) / 128 * 64)
@@ -74,8 +75,8 @@ pat_status_t pat_mx_dequantize(const void* codes, const void* scales, size_t row
 /*
  * out[i][j] = sum over x < k of a[i][x] * b[j][x]: a (m rows) and b (n rows) in
  * the stored form, both of k columns; out PAT_FLOAT32 or PAT_BFLOAT16.  All
- * products here: fewer than 2^26 rows and columns of the output, 2^24 terms of a
- * sum (else PAT_ERR_UNSUPPORTED).
+ * products here: fewer than 2^26 rows and columns of the output and 2^30 tiles of
+ * 16 x 16 of it, 2^24 terms of a sum (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_mx_matmul(const void* a_codes, const void* a_scales, const void* b_codes, const void* b_scales, size_t m,
                            size_t n, size_t k, void* out, int64_t out_stride, pat_dtype_t dtype, hipStream_t stream);

@@ -334,7 +334,6 @@ template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED>
 hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, const GradPlan& p,
                     void* workspace, hipStream_t stream) {
   constexpr int R = GradTile<FA, FB, WA, WB>::R;
-  const size_t tiles = ceil_div(rows, R) * ceil_div(cols, R);
   const bool sliced = p.slices > 1, f32 = dtype == Elem::f32;
   const MatOut to = sliced ? MatOut{workspace, slice_pitch(cols)} : out;
   auto kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, false, F32>
@@ -342,7 +341,7 @@ hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, M
   if (TRANSPOSED && rows % 8)
     kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, F32>
                            : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, B16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8), (unsigned)p.slices), dim3(64 * WA * WB * PARTS), 0,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tile_wgs(rows, cols, R), (unsigned)p.slices), dim3(64 * WA * WB * PARTS), 0,
                      stream, g, q, rows, inner, cols, to, p.slice);
   if (sliced) {
     const int lanes = row_lanes((int64_t)ceil_div(cols, 8), 256);

@@ -216,9 +216,6 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b,
 // Bound by the reading of b: one row of 8192 columns by 8192 rows of b (36 MB) in 9.6 us, of which 3 are a launch of
 // anything; 24 quantised rows of 4001 by 5000 (11 MB) in 7.
 
-constexpr int kSplitWaves = 8;
-constexpr int kSplitRows = 48;
-
 template <int MT, int NT, bool FUSED, typename X, typename T>
 __global__ __launch_bounds__(64 * kSplitWaves) void split_kernel(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k,
                                                                   int groups, Divisor per_row, MatOut out) {
@@ -343,36 +340,36 @@ template <int MT, int NT, bool FUSED, typename X>
 hipError_t run_split(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
   const int groups = (int)groups_of(k);
   const size_t sums = (size_t)kSplitWaves * MT * NT * 1024, rows = FUSED ? (size_t)m * (groups * 68 + 16) : 0;
-  const dim3 grid((unsigned)(ceil_div(m, 16 * MT) * ceil_div(n, 16 * NT))), block(64 * kSplitWaves);
+  const dim3 grid((unsigned)split_wgs(m, n)), block(64 * kSplitWaves);
   const auto kernel = dtype == Elem::f32 ? split_kernel<MT, NT, FUSED, X, F32> : split_kernel<MT, NT, FUSED, X, B16>;
   hipLaunchKernelGGL(kernel, grid, block, std::max(sums, rows), stream, a, x, b, m, n, k, groups,
-                     Divisor((uint32_t)std::max(groups, 1) * 16), out);
+                     Divisor((uint32_t)groups * 16), out);
   return hipGetLastError();
 }
 
 template <int MT, bool FUSED, typename X>
 hipError_t pick_columns(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
-  // As many columns a workgroup as leave one for each of the 256 CUs: the rows of a are read and quantised once per
-  // workgroup.  us at 24 rows with 16, 32, 64 columns: 8.2, 9.2, 11.9 (n = k = 4096), 18, 14.6, 19 (8192), 18, 14.5, 13
-  // (n = 16384, k = 4096).
-  if (n <= 16 * 256) return run_split<MT, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  if (n <= 32 * 256) return run_split<MT, 2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  return run_split<MT, 4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  switch (split_columns(n)) {
+    case 1: return run_split<MT, 1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+    case 2: return run_split<MT, 2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+    default: return run_split<MT, 4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  }
 }
 
 template <bool FUSED, typename X>
 hipError_t pick_split(MxMat a, Mat x, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
-  if (m <= 16) return pick_columns<1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  if (m <= 32) return pick_columns<2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
-  return pick_columns<4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  switch (split_rows(m)) {
+    case 1: return pick_columns<1, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+    case 2: return pick_columns<2, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+    default: return pick_columns<4, FUSED, X>(a, x, b, m, n, k, out, dtype, stream);
+  }
 }
 
 template <int FA, int FB, int WA, int WB>
 hipError_t run_tile(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
   constexpr int R = Tile<FA, FB, WA, WB>::R;
-  const size_t tiles = ceil_div(m, R) * ceil_div(n, R);
   const auto kernel = dtype == Elem::f32 ? tile_kernel<FA, FB, WA, WB, F32> : tile_kernel<FA, FB, WA, WB, B16>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(ceil_div(tiles, 8) * 8)), dim3(64 * WA * WB), 0, stream, a, b, m, n,
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tile_wgs(m, n, R)), dim3(64 * WA * WB), 0, stream, a, b, m, n,
                      (int)groups_of(k), out);
   return hipGetLastError();
 }
@@ -381,20 +378,17 @@ hipError_t run_tile(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut ou
 // k = 4096: 4.5 and 5.8 for one row, 5.1 and 6.6 for 4, 8.6 and 7.3 for 16; k = 8192: 8.1 and 10.7, 10.4 and 11.6,
 // none and 12.6).  What they take in LDS stays below 32 KB.  No more rows than the split takes of a product whose rows
 // are quantised before: the sums are then the same either way.
-bool fused(int64_t m, int64_t k) { return m <= kSplitRows && m * k <= 32768; }
+bool fused(int64_t m, int64_t k) { return k > 0 && m <= kSplitRows && m * k <= 32768; }
 
 }  // namespace
 
 hipError_t launch_mx_matmul(MxMat a, MxMat b, int64_t m, int64_t n, int64_t k, MatOut out, Elem dtype, hipStream_t stream) {
-  // The largest tile that gives more than half of the 256 CUs one.  A tile's time grows with its area only once the chip
-  // is full; us with tiles of 64, 128, 256 at n = k = 8192: 24, 30, 51 for m = 256 (512, 128, 32 tiles), 48, 32, 51 for
-  // m = 512, 85, 52, 54 for m = 1024, 161, 96, 72 for m = 2048.  Up to 48 rows or columns the split is as fast or
-  // faster (n = 8192: 19 against 20; n = k = 1024: 5 against 6).
-  auto tiles = [&](int size) { return ceil_div(m, size) * ceil_div(n, size); };
-  if (k > 0 && m > kSplitRows && n > kSplitRows) {
-    if (tiles(256) > 128) return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
-    if (tiles(128) > 128) return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
-    return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
+  // without columns all are zero: the gradient's sum of no terms, which takes outputs of any size
+  if (k == 0) return launch_mx_grad({nullptr, 0}, false, {nullptr, nullptr}, m, 0, n, out, dtype, nullptr, stream);
+  switch (product_tile(m, n)) {
+    case 256: return run_tile<4, 2, 2, 4>(a, b, m, n, k, out, dtype, stream);
+    case 128: return run_tile<2, 2, 2, 2>(a, b, m, n, k, out, dtype, stream);
+    case 64: return run_tile<1, 1, 2, 2>(a, b, m, n, k, out, dtype, stream);
   }
   return pick_split<false, F32>(a, {}, b, m, n, k, out, dtype, stream);
 }

@@ -87,10 +87,11 @@ bool grad_dims_ok(size_t ntokens, size_t rows, size_t cols) {
   return ntokens < size_t(1) << 28 && rows < size_t(1) << 28 && cols < size_t(1) << 23;
 }
 
-// Products: what a launch's grid and its kernels' 32-bit offsets inside a tile's rows hold.
+// Products: what a launch's grid and its kernels' 32-bit offsets inside a tile's rows hold; fewer than 2^38 values of the
+// output, in tiles of 16 x 16, which are more than the card's memory.
 bool product_ok(size_t rows, size_t cols, size_t inner) {
   return rows < size_t(1) << 26 && cols < size_t(1) << 26 && inner < size_t(1) << 24 &&
-         ((rows + 15) / 16) * ((cols + 15) / 16) < kMaxDim;
+         ((rows + 15) / 16) * ((cols + 15) / 16) < size_t(1) << 30;
 }
 
 }  // namespace

@@ -41,6 +41,35 @@ inline DropoutPlan dropout_plan(int64_t rows, int64_t cols, bool dense) {
   return p;
 }
 
+// ---- 4-bit product -----------------------------------------------------------------------------------------------
+
+constexpr int kSplitWaves = 8;
+constexpr int kSplitRows = 48;
+
+// The product's tiles (256, 128 or 64 rows and columns), or 0: split_kernel.
+//
+// The largest tile that gives more than half of the 256 CUs one.  A tile's time grows with its area only once the chip is
+// full; us with tiles of 64, 128, 256 at n = k = 8192: 24, 30, 51 for m = 256 (512, 128, 32 tiles), 48, 32, 51 for
+// m = 512, 85, 52, 54 for m = 1024, 161, 96, 72 for m = 2048.  Up to 48 rows or columns the split is as fast or
+// faster (n = 8192: 19 against 20; n = k = 1024: 5 against 6).
+inline int64_t product_tiles(int64_t m, int64_t n, int size) { return (int64_t)(ceil_div(m, size) * ceil_div(n, size)); }
+inline int product_tile(int64_t m, int64_t n) {
+  if (m <= kSplitRows || n <= kSplitRows) return 0;
+  return product_tiles(m, n, 256) > 128 ? 256 : product_tiles(m, n, 128) > 128 ? 128 : 64;
+}
+// Workgroups of such tiles: the same for each XCD.
+inline int64_t tile_wgs(int64_t m, int64_t n, int size) { return (int64_t)ceil_div(product_tiles(m, n, size), 8) * 8; }
+
+// Rows and columns of split_kernel's workgroups, in sixteens.
+inline int split_rows(int64_t m) { return m <= 16 ? 1 : m <= 32 ? 2 : 4; }
+// As many columns a workgroup as leave one for each of the 256 CUs: the rows of a are read and quantised once per
+// workgroup.  us at 24 rows with 16, 32, 64 columns: 8.2, 9.2, 11.9 (n = k = 4096), 18, 14.6, 19 (8192), 18, 14.5, 13
+// (n = 16384, k = 4096).
+inline int split_columns(int64_t n) { return n <= 16 * 256 ? 1 : n <= 32 * 256 ? 2 : 4; }
+inline int64_t split_wgs(int64_t m, int64_t n) {
+  return (int64_t)(ceil_div(m, 16 * split_rows(m)) * ceil_div(n, 16 * split_columns(n)));
+}
+
 // ---- gradients of the 4-bit product ----------------------------------------------------------------------------
 
 // How a product is cut: the tile's size, and slices of j that get workgroups and a float32 matrix of their own, which

@@ -2,6 +2,7 @@
 #include <cstdio>
 #include <cstdlib>
 
+#include "../../include/pat_ops.h"
 #include "ops_shape.hpp"
 
 using namespace pat;
@@ -34,13 +35,59 @@ static void check_dropout(int64_t rows, int64_t cols) {
   if (rows > 1 && rows * cols <= (int64_t)1 << 35) CHECK(dropout_plan(rows, cols, true).flat, "%lld %lld", r, c);
 }
 
-// Accepted: fewer than 2^26 rows and columns, and 2^31 tiles of 16 x 16.
+// What the C entry points of the products and their gradient hand to a launch: of accepted sizes it holds the lanes.
+namespace pat {
+static int64_t g_lanes = -1;
+void record_hip_error(hipError_t) {}
+hipError_t launch_mx_quantize(Mat, Elem, int64_t, int64_t, uint8_t*, uint8_t*, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_dequantize(MxMat, int64_t, int64_t, MatOut, Elem, hipStream_t) { return hipSuccess; }
+hipError_t launch_mx_matmul(MxMat, MxMat, int64_t m, int64_t n, int64_t k, MatOut, Elem, hipStream_t) {
+  const int tile = product_tile(m, n);
+  g_lanes = k == 0 ? narrow_wgs(m, n) * 64 : tile ? tile_wgs(m, n, tile) * (tile == 256 ? 512 : 256) : split_wgs(m, n) * 64 * kSplitWaves;
+  return hipSuccess;
+}
+size_t mx_linear_workspace(int64_t, int64_t, int64_t) { return 0; }
+hipError_t launch_mx_linear(Mat, Elem, MxMat, int64_t, int64_t, int64_t, MatOut, Elem, void*, hipStream_t) {
+  return hipSuccess;
+}
+size_t mx_grad_workspace(int64_t, int64_t, int64_t) { return 0; }
+hipError_t launch_mx_grad(Mat, bool, MxMat, int64_t rows, int64_t inner, int64_t cols, MatOut, Elem, void*, hipStream_t) {
+  const GradPlan p = grad_plan(rows, inner, cols);
+  g_lanes = std::max(narrow_wgs(rows, cols) * 64, tile_wgs(rows, cols, p.tile) * 512);
+  return hipSuccess;
+}
+hipError_t launch_embedding(const void*, int, int64_t, Mat, Elem, int64_t, int64_t, int64_t, float, MatOut, Elem,
+                            hipStream_t) {
+  return hipSuccess;
+}
+size_t embedding_grad_workspace(int64_t, int64_t, int64_t) { return 0; }
+hipError_t launch_embedding_grad(const void*, int, int64_t, Mat, Elem, int64_t, int64_t, int64_t, float, MatOut, Elem, void*,
+                                 hipStream_t) {
+  return hipSuccess;
+}
+hipError_t launch_dropout(const DropoutArgs&, Elem, hipStream_t) { return hipSuccess; }
+}  // namespace pat
+
 static void check_product(int64_t rows, int64_t cols) {
-  const int64_t most = ((int64_t)1 << 26) - 1;
-  if (rows < 1 || cols < 1 || rows > most || cols > most) return;
-  if ((rows + 15) / 16 * ((cols + 15) / 16) >= (int64_t)1 << 31) return;
-  const int64_t wgs = narrow_wgs(rows, cols);
-  CHECK(wgs >= 1 && wgs * 64 < kLanes, "%lld %lld: %lld workgroups", (long long)rows, (long long)cols, (long long)wgs);
+  auto at = [](uint64_t off) { return (void*)(uintptr_t)off; };  // never read: launches only record
+  if (rows < 1 || cols < 1) return;
+  for (int64_t terms : {0, 1, 200}) {
+    g_lanes = 0;
+    const pat_status_t st = pat_mx_matmul(at(1ull << 60), at(1ull << 59), at(1ull << 58), at(1ull << 57), rows, cols, terms, at(4096),
+                                          cols, PAT_FLOAT32, nullptr);
+    CHECK(st == PAT_OK ? g_lanes > 0 : st == PAT_ERR_UNSUPPORTED && rows * cols >= (int64_t)1 << 26, "%lld %lld: %d", (long long)rows,
+          (long long)cols, st);
+    CHECK(g_lanes < kLanes, "%lld %lld %lld: %lld lanes", (long long)rows, (long long)cols, (long long)terms, (long long)g_lanes);
+    g_lanes = 0;
+    const pat_status_t gr = pat_mx_matmul_grad(at(1ull << 60), rows, 1, at(1ull << 58), at(1ull << 57), rows, terms, cols, at(4096),
+                                               cols, PAT_FLOAT32, nullptr, 0, nullptr);
+    CHECK(gr == PAT_OK ? g_lanes > 0 : gr == PAT_ERR_UNSUPPORTED && rows * cols >= (int64_t)1 << 26, "%lld %lld: %d", (long long)rows,
+          (long long)cols, gr);
+    CHECK(g_lanes < kLanes, "%lld %lld %lld: %lld lanes", (long long)rows, (long long)cols, (long long)terms, (long long)g_lanes);
+    // 2^37 values, 256 GiB in bfloat16, are taken
+    if (rows < 1 << 26 && cols < 1 << 26 && rows * cols <= (int64_t)1 << 37 && rows >= 256 && cols >= 256)
+      CHECK(st == PAT_OK && gr == PAT_OK, "%lld %lld: %d %d", (long long)rows, (long long)cols, st, gr);
+  }
 }
 
 int main() {
@@ -64,7 +111,7 @@ int main() {
   for (int e = 0; e <= 26; ++e)
     for (int f = 0; f <= 26; ++f)
       for (int d = -17; d <= 17; ++d) check_product(((int64_t)1 << e) + d, ((int64_t)1 << f) + d);
-  for (int i = 0; i < 200000; ++i) check_product(rnd(most >> 5), rnd(most >> 5));
+  for (int i = 0; i < 200000; ++i) check_product(rnd((1 << 26) + 100), rnd((1 << 26) + 100));
   std::printf("%d checks, %d failures\n", g_checked, g_failures);
   return g_failures != 0;
 }

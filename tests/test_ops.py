@@ -145,7 +145,7 @@ def test_launches_hold_their_lanes(tmp_path):
     exe = tmp_path / "ops_grid_check"
     csrc = os.path.join(ROOT, "paper_2506_20252_amd", "csrc")
     cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
-           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", csrc,
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", csrc, os.path.join(csrc, "ops.cpp"),
            os.path.join(ROOT, "tests", "host", "ops_grid_check.cpp"), "-o", str(exe)]
     subprocess.run(cmd, check=True, capture_output=True, text=True)
     res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
@@ -389,6 +389,15 @@ def test_products_of_no_columns_are_zero(m, n, k):
     out = torch.full((m, 40), 5.0, device="cuda")  # a gradient of no rows
     empty = torch.empty((m, 0), dtype=B16, device="cuda")
     assert bool((ops.mx_matmul_grad(empty, ops.mx_empty(0, 40), F32, out=out) == 0).all())
+
+
+@gpu
+def test_product_of_no_columns_and_many_values_is_zero():
+    """2^35 values, of more tiles than one launch has workgroups of eight waves."""
+    m = n = 1 << 17
+    out = torch.full((2 * m, n), 5.0, dtype=B16, device="cuda")
+    ops.mx_matmul(ops.mx_empty(2 * m, 0), ops.mx_empty(n, 0), B16, out)
+    assert not any(bool(part.any()) for part in out.split(8192))
 
 
 @gpu
