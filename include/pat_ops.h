@@ -26,7 +26,9 @@
  *     is needed, NULL is accepted); its contents mean nothing after the call.
  *     Calls that may overlap need one each.  Fewer bytes: PAT_ERR_TOO_LARGE.
  *   - An output that overlaps an input or the workspace is
- *     PAT_ERR_INVALID_ARGUMENT, except where in place is named.
+ *     PAT_ERR_INVALID_ARGUMENT, except where in place is named.  Columns of
+ *     one matrix beside each other do not overlap; matrices of different
+ *     strides (in bytes) whose rows alternate count as if they did.
  *   - Nothing is launched when an output has no elements.  Buffers without
  *     elements may be NULL.  Row and column counts are below 2^31.
  *   - Results are deterministic: no sum depends on the order of execution.

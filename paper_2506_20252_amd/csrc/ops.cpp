@@ -21,12 +21,22 @@ bool elem_of(pat_dtype_t dtype, Elem* e) {
 
 size_t elem_bytes(Elem e) { return e == Elem::f32 ? 4 : 2; }
 
-// The addresses [lo, hi) of a buffer; empty ones overlap nothing.
+// The addresses of a buffer: `width` bytes from lo and from every `pitch` bytes after it, the last end at hi; pitch 0: one
+// run of bytes.  Empty ones overlap nothing.
 struct Span {
   uintptr_t lo = 0, hi = 0;
+  size_t pitch = 0, width = 0;
 };
 
-bool overlap(const Span& a, const Span& b) { return a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi; }
+// Runs of bytes of the same pitch may stand between each other's, as column slices of one matrix do; of two different
+// pitches whole ranges are compared.
+bool overlap(const Span& a, const Span& b) {
+  if (!(a.lo < a.hi && b.lo < b.hi && a.lo < b.hi && b.lo < a.hi)) return false;
+  const size_t pitch = a.pitch ? a.pitch : b.pitch;
+  if (!pitch || (b.pitch && b.pitch != pitch)) return true;
+  const size_t d = b.lo >= a.lo ? (b.lo - a.lo) % pitch : (pitch - (a.lo - b.lo) % pitch) % pitch;  // b's columns in a's rows
+  return d < a.width || b.width > pitch - d;
+}
 
 // Span of `bytes` bytes at p; false where p is null, misaligned or wraps around.
 bool span_of(const void* p, size_t bytes, size_t align, Span* s) {
@@ -36,7 +46,7 @@ bool span_of(const void* p, size_t bytes, size_t align, Span* s) {
   }
   const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
   if (!lo || lo % align || bytes > UINTPTR_MAX - lo) return false;
-  *s = Span{lo, lo + bytes};
+  *s = Span{lo, lo + bytes, 0, bytes};
   return true;
 }
 
@@ -51,7 +61,9 @@ bool matrix_span(const void* p, int64_t stride, size_t rows, size_t cols, size_t
   if (rows > 1 && __builtin_mul_overflow(rows - 1, size_t(stride), &elems)) return false;
   if (__builtin_add_overflow(elems, cols, &elems) || __builtin_mul_overflow(elems, es, &bytes)) return false;
   if (bytes > size_t(INT64_MAX)) return false;
-  return span_of(p, bytes, es, s);
+  if (!span_of(p, bytes, es, s)) return false;
+  if (rows > 1) s->pitch = size_t(stride) * es, s->width = cols * es;
+  return true;
 }
 
 // Spans of a stored form's two buffers.

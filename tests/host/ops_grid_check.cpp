@@ -1,6 +1,8 @@
-// What the operators' launches ask for (ops_shape.hpp): a launch holds fewer than 2^32 lanes, and has to reach all its work.
+// What the operators' launches ask for (ops_shape.hpp): a launch holds fewer than 2^32 lanes, and has to reach all its work;
+// and which places of an output beside an input the entry points (ops.cpp) take.
 #include <cstdio>
 #include <cstdlib>
+#include <cstring>
 
 #include "../../include/pat_ops.h"
 #include "ops_shape.hpp"
@@ -90,6 +92,37 @@ static void check_product(int64_t rows, int64_t cols) {
   }
 }
 
+// An output in the columns that an input leaves free of the same rows shares no byte with it.  Matrices of the same pitch, or
+// of one row, are refused where bytes are shared and only there; of other pitches at least there.
+static void check_overlap(int64_t rows, int64_t g_rows, int64_t cols, int64_t inner, int64_t g_stride, int64_t o_stride, int64_t d) {
+  const uint64_t g0 = 1 << 20, o0 = g0 + d;
+  static char used[1 << 16];
+  std::memset(used, 0, sizeof used);
+  const int64_t lo = -(1 << 15);
+  for (int64_t r = 0; r < g_rows; ++r)
+    for (int64_t b = 0; b < 2 * inner; ++b) used[2 * r * g_stride + b - lo] = 1;
+  bool shared = false;
+  for (int64_t r = 0; r < rows; ++r)
+    for (int64_t b = 0; b < 4 * cols; ++b) shared |= used[d + 4 * r * o_stride + b - lo] != 0;
+  // the gradient's g (bfloat16) and output (float32): rows of g are rows of the output
+  auto at = [](uint64_t a) { return (void*)(uintptr_t)a; };
+  const bool exact = 2 * g_stride == 4 * o_stride || rows == 1;
+  if (g_rows == rows) {
+    const pat_status_t st = pat_mx_matmul_grad(at(g0), g_stride, 0, at(1 << 25), at(1 << 26), rows, inner, cols, at(o0), o_stride,
+                                               PAT_FLOAT32, nullptr, 0, nullptr);
+    CHECK(shared || exact ? st == (shared ? PAT_ERR_INVALID_ARGUMENT : PAT_OK) : true, "%lld %lld %lld %lld %lld %lld: %d", (long long)rows,
+          (long long)cols, (long long)inner, (long long)g_stride, (long long)o_stride, (long long)d, st);
+  }
+  // an embedding's table (bfloat16) of g_rows, and as many columns as the output
+  if (inner == cols) {
+    const pat_status_t st = pat_embedding(at(1 << 25), 4, rows, at(g0), g_stride, PAT_BFLOAT16, 0, g_rows, cols, 1.0f, at(o0), o_stride,
+                                          PAT_FLOAT32, nullptr);
+    const bool same = exact || g_rows == 1;
+    CHECK(shared || same ? st == (shared ? PAT_ERR_INVALID_ARGUMENT : PAT_OK) : true, "embedding %lld %lld %lld %lld %lld %lld: %d",
+          (long long)rows, (long long)g_rows, (long long)cols, (long long)g_stride, (long long)o_stride, (long long)d, st);
+  }
+}
+
 int main() {
   unsigned long long x = 88172645463325252ull;
   auto rnd = [&](int64_t most) {  // 1 ... most, spread over the logarithm
@@ -112,6 +145,12 @@ int main() {
     for (int f = 0; f <= 26; ++f)
       for (int d = -17; d <= 17; ++d) check_product(((int64_t)1 << e) + d, ((int64_t)1 << f) + d);
   for (int i = 0; i < 200000; ++i) check_product(rnd((1 << 26) + 100), rnd((1 << 26) + 100));
+  for (int i = 0; i < 300000; ++i) {
+    const int64_t rows = rnd(6), cols = rnd(12), inner = rnd(4) == 1 ? cols : rnd(20), o_stride = cols + rnd(30) - 1;
+    int64_t g_stride = rnd(3) == 1 ? inner + rnd(40) - 1 : 2 * o_stride;
+    if (g_stride < inner) g_stride = inner;
+    check_overlap(rows, rnd(2) == 1 ? rnd(6) : rows, cols, inner, g_stride, o_stride, 4 * (rnd(600) - rnd(600)));
+  }
   std::printf("%d checks, %d failures\n", g_checked, g_failures);
   return g_failures != 0;
 }

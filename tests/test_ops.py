@@ -743,6 +743,33 @@ def test_offsets_beyond_32_bits():
     assert bool((room[:, cols:64] == 0).all()) and bool((room[:, 200:4096] == 0).all())
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_input_and_output_in_columns_of_one_buffer(dtype):
+    """Whatever stands in the columns beside an output is read as it was and left so."""
+    x, tokens = values((40, 96), 1, dtype), torch.arange(40, device="cuda") * 7 % 40
+    q = ops.mx_quantize(values((70, 96), 3))
+    calls = {"dropout": lambda a, out: ops.dropout(a, 0.3, 5, out=out),
+             "residual": lambda a, out: ops.dropout(x, 0.3, 5, residual=a, out=out),
+             "embedding": lambda a, out: ops.embedding(tokens, a, 2.0, out=out),
+             "embedding_grad": lambda a, out: ops.embedding_grad(tokens, a, 40, 2.0, out=out)}
+    if dtype == B16:
+        calls["grad"] = lambda a, out: ops.mx_matmul_grad(a, ops.mx_quantize(values((96, 96), 4)), out=out)
+    calls["linear"] = lambda a, out: ops.mx_linear(a, q, out=out)
+    for name, call in calls.items():
+        want = call(x, None)
+        for left, right in ((0, 0), (3, 5)):
+            for first in (False, True):
+                room = torch.full((40, 96 + want.shape[1] + left + right), -77.0, dtype=dtype, device="cuda")
+                at = left if first else left + want.shape[1]
+                to = left + 96 if first else left
+                a, out = room[:, at:at + 96], room[:, to:to + want.shape[1]]
+                a.copy_(x)
+                call(a, out)
+                assert torch.equal(out, want) and torch.equal(a, x), name
+                assert bool((room[:, :left] == -77.0).all()) and bool((room[:, left + 96 + want.shape[1]:] == -77.0).all()), name
+
+
 # ---- the operators together, between the collectives
 
 def example():
