@@ -379,6 +379,22 @@ def test_linear(m, n, k, dtype, out_dtype):
 
 
 @gpu
+@pytest.mark.parametrize("m,n", [(1500, 1501), (2900, 2899)])  # tiles of 128 and of 256
+@pytest.mark.parametrize("k", [1030, 1160, 1290, 1420, 2430])  # 9, 10, 11, 12 and 19 groups: every rest of the loop by four
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_matmul_goes_through_many_columns_of_large_tiles(m, n, k, dtype):
+    """The reference in 64 bits by the GPU's library.  Twice: a race would hardly give the same bits."""
+    a, va = random_mx(m, k, m + k)
+    b, vb = random_mx(n, k, n + k)
+    out, untouched = guarded((m, n), dtype, pad=1)
+    ops.mx_matmul(a, b, dtype, out)
+    assert untouched()
+    ta, tb = torch.from_numpy(va).cuda(), torch.from_numpy(vb).cuda().t().contiguous()
+    within(out, f64(torch.mm(ta, tb)), f64(torch.mm(ta.abs(), tb.abs())), k, dtype)
+    assert torch.equal(out, ops.mx_matmul(a, b, dtype))
+
+
+@gpu
 @pytest.mark.parametrize("m,n,k", [(3, 20, 0), (300, 300, 0)])
 def test_products_of_no_columns_are_zero(m, n, k):
     a, b = ops.mx_empty(m, k), ops.mx_empty(n, k)
