@@ -258,6 +258,25 @@ def test_bad_arguments_are_refused_before_any_device_call(call, args, change, st
     assert call(*args(**change)) == status
 
 
+LARGE_LINEAR = dict(m=60, x=BASE + 0x100000, out=BASE + 0x200000, workspace=BASE + 0x300000)
+LARGE_GRAD = dict(rows=40, inner=8449, g=BASE + 0x1000000, g_stride=8449, q_codes=BASE + 0x2000000, q_scales=BASE + 0x3000000,
+                  out=BASE + 0x4000000, workspace=BASE + 0x5000000)
+
+
+@pytest.mark.parametrize("call,args,size,need", [
+    (ops.pat_mx_linear, lambda **kw: linear_args(**{**LARGE_LINEAR, **kw}), LARGE_LINEAR, lambda: ops.pat_mx_linear_workspace(60, 5, 200)),
+    (ops.pat_mx_matmul_grad, lambda **kw: grad_args(**{**LARGE_GRAD, **kw}), LARGE_GRAD,
+     lambda: ops.pat_mx_matmul_grad_workspace(40, 8449, 200))], ids=["linear", "grad"])
+def test_bad_workspaces_are_refused_before_any_device_call(call, args, size, need):
+    """Too small, absent, misaligned, or over the output, an input, or a stored form."""
+    need = need()
+    assert need > 0
+    assert call(*args(workspace_bytes=need - 1)) == TOO_LARGE and call(*args(workspace_bytes=0)) == TOO_LARGE
+    stored = [size.get(name, BASE + place) for name, place in (("q_codes", 0x2000), ("q_scales", 0x4000))]
+    for place in (0, size["workspace"] + 8, size["out"], size["out"] - need + 16, size.get("g", size.get("x")), *stored):
+        assert call(*args(workspace=place, workspace_bytes=need)) == INVALID, hex(place)
+
+
 def test_calls_without_elements_launch_nothing():
     none = dict(x=0, codes=0, scales=0)
     assert ops.pat_mx_quantize(*quantize_args(rows=0, **none)) == pat.PAT_OK
@@ -731,6 +750,85 @@ def test_memory_of_a_call_on_another_stream(name):
         got = call(handle)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def with_workspaces():
+    """Calls that need memory between their launches: name -> (call of an output and a stream, bytes of workspace)."""
+    x, w = values((60, 300), 1, B16), values((70, 300), 2)
+    q = ops.mx_quantize(w)
+    g, tall = values((40, 8449), 3, B16), ops.mx_quantize(values((8449, 200), 4))
+    by_terms = g.t().contiguous()
+    rows = {n: (values((n, 24), n, B16), torch.from_numpy(np.random.default_rng(n).integers(-3, 300, size=n) // 2).cuda())
+            for n in (2000, 6000)}
+    return {
+        "linear": (lambda out, s=None: ops.mx_linear(x, q, F32, out, s), ops.pat_mx_linear_workspace(60, 70, 300)),
+        "grad": (lambda out, s=None: ops.mx_matmul_grad(g, tall, F32, False, out, s),
+                 ops.pat_mx_matmul_grad_workspace(40, 8449, 200)),
+        "grad_t": (lambda out, s=None: ops.mx_matmul_grad(by_terms, tall, F32, True, out, s),
+                   ops.pat_mx_matmul_grad_workspace(40, 8449, 200)),
+        **{f"embedding_grad_{n}": (lambda out, s=None, n=n: ops.embedding_grad(rows[n][1], rows[n][0], 140, dtype=F32, out=out, stream=s),
+                                   ops.pat_embedding_grad_workspace(n, 140, 24)) for n in rows},
+    }
+
+
+WITH_WORKSPACES = ["linear", "grad", "grad_t", "embedding_grad_2000", "embedding_grad_6000"]
+
+
+@gpu
+@pytest.mark.parametrize("name", WITH_WORKSPACES)
+def test_graph_replays_of_calls_with_workspaces(name):
+    call, need = with_workspaces()[name]
+    assert need > 0
+    want = call(None)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for _ in range(4):
+        out.zero_()
+        junk = torch.full((max(need, 1 << 20),), 0x77, dtype=torch.uint8, device="cuda")  # the pool's memory is not the graph's
+        graph.replay()
+        assert torch.equal(call(None), want)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and bool((junk == 0x77).all())
+
+
+@gpu
+@pytest.mark.parametrize("name", WITH_WORKSPACES)
+def test_workspaces_belong_to_the_stream_of_the_call(name, monkeypatch):
+    """Output and workspace of a call on a given stream are that stream's memory, and the result is right while the current
+    stream writes over blocks of the same sizes that it has just freed."""
+    call, need = with_workspaces()[name]
+    assert need > 0
+    want, side, held = call(None), torch.cuda.Stream(), []
+    take = ops._work
+
+    def work(*args):
+        address, tensor = take(*args)
+        held.append((address, tensor.numel()))
+        return address, tensor
+
+    monkeypatch.setattr(ops, "_work", work)
+    torch.cuda.synchronize()
+    for handle in (side, side.cuda_stream):
+        for _ in range(20):
+            late = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in 2 * (need, want.numel() * 4)]
+            for t in late:
+                t.fill_(0x77)
+            del late, t
+            got = call(None, handle)
+            side.synchronize()
+            assert torch.equal(got, want)
+        torch.cuda.synchronize()
+        segments = torch.cuda.memory_snapshot()
+
+        def stream_of(address):
+            return [s["stream"] for s in segments if s["address"] <= address < s["address"] + s["total_size"]]
+
+        assert len(held) == 20 and all(size == need and stream_of(at) == [side.cuda_stream] for at, size in held)
+        assert stream_of(got.data_ptr()) == [side.cuda_stream]
+        held.clear()
 
 
 @gpu
