@@ -533,6 +533,22 @@ def test_embedding(ntokens, rows, cols, first, dtype, out_dtype, wide):
 
 
 @gpu
+@pytest.mark.parametrize("ntokens,rows,cols", [(2051, 37, 1031), (2047, 9, 4100), (66001, 300, 40), (524001, 50, 5)])
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (B16, B16), (B16, F32), (F32, B16)])
+def test_embedding_of_many_tokens(ntokens, rows, cols, dtype, out_dtype):
+    """Two tokens a lane in turn; a workgroup's last ones may not exist, a third of all is outside the table."""
+    tokens = np.random.default_rng(ntokens).integers(3 - rows, 3 + 2 * rows, size=ntokens)
+    table = values((rows, cols), rows, dtype)
+    inside = (tokens >= 3) & (tokens < 3 + rows)
+    want = np.where(inside[:, None], 1.75 * f64(table)[np.where(inside, tokens - 3, 0)], 0.0)
+    for token_dtype, view in ((torch.int32, table), (torch.int64, strided(table, 2, 1))):
+        out, untouched = guarded((ntokens, cols), out_dtype)
+        ops.embedding(torch.from_numpy(tokens).to(token_dtype).cuda(), view, 1.75, 3, out_dtype, out)
+        assert untouched()
+        within(out, want, 0.0, 0, out_dtype)
+
+
+@gpu
 def test_embedding_in_a_table_without_rows():
     out = torch.full((9, 40), 5.0, device="cuda")
     ops.embedding(torch.arange(9, device="cuda"), torch.empty((0, 40), device="cuda"), dtype=F32, out=out)
@@ -589,6 +605,37 @@ def test_embedding_grad_of_wide_rows_and_none(ntokens, cols):
     out = ops.embedding_grad(torch.from_numpy(tokens).cuda(), g, 41, dtype=F32)
     within(out, O.embedding_grad(tokens, f64(g), 41, 1.0, 0), O.embedding_grad(tokens, np.abs(f64(g)), 41, 1.0, 0), ntokens,
            F32)
+
+
+@gpu
+@pytest.mark.parametrize("ntokens,rows,cols,share", [
+    (9001, 500, 1030, 0.3),         # whole waves a piece, sorted by several workgroups; pieces of 16 entries
+    (70001, 3000, 1031, 0.4),       # pieces of 32
+    (140001, 3000, 1030, 0.5),      # pieces of 64, sorting workgroups of more than 1024 entries
+    (140001, 1, 260, 0.0),          # one row of all
+    (30001, 70000, 2057, 0.2),      # two column parts, most rows without an entry
+    (150001, 1100000, 5, 0.1),      # three sorting passes
+])
+@pytest.mark.parametrize("dtype,out_dtype", [(F32, F32), (B16, F32), (B16, B16)])
+def test_embedding_grad_of_many_tokens(ntokens, rows, cols, share, dtype, out_dtype):
+    """A frequent row (`share` of the tokens), rare ones, some outside; the sums in 64 bits on the GPU."""
+    r = np.random.default_rng(ntokens + cols)
+    tokens = np.where(r.random(ntokens) < share, rows // 3, r.integers(-rows // 8 - 1, rows + rows // 8 + 1, size=ntokens))
+    t = torch.from_numpy(tokens).cuda()
+    g = torch.randn((ntokens, cols), device="cuda", generator=torch.Generator("cuda").manual_seed(ntokens)).to(dtype)
+    inside = ((t >= 0) & (t < rows)).nonzero()[:, 0]
+    terms = int(torch.bincount(t[inside]).max())
+    want, size = (torch.zeros((rows, cols), dtype=torch.float64, device="cuda") for _ in range(2))
+    for part in inside.split(20000):
+        want.index_add_(0, t[part], 0.5 * g[part].double())
+        size.index_add_(0, t[part], 0.5 * g[part].double().abs())
+    out, untouched = guarded((rows, cols), out_dtype)
+    ops.embedding_grad(t, g, rows, 0.5, 0, out_dtype, out)
+    assert untouched()
+    bound = 2 * (terms + 2) * U * size + (E if out_dtype == B16 else 2 * U) * want.abs() + 1e-300  # as within()
+    assert bool(((out.double() - want).abs() <= bound).all())
+    wide = strided(g, 3, 1)
+    assert torch.equal(ops.embedding_grad(t.int(), wide, rows, 0.5, 0, out_dtype), out)
 
 
 @gpu
