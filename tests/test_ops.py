@@ -879,6 +879,49 @@ def test_workspaces_belong_to_the_stream_of_the_call(name, monkeypatch):
 
 
 @gpu
+@pytest.mark.parametrize("name", ["quantize", "dequantize", "embedding", "embedding_grad", "dropout"])
+def test_more_work_than_a_launch_has_workgroups(name):
+    """Workgroups that go round several times: every part of a large result is that of a small call on the same values."""
+    parts = 4099  # of 4096 rows each, the last one short
+    if name in ("quantize", "dequantize"):  # more than 2^26 groups of 128 values
+        x = values((4096, 600), 1, B16)
+        q = ops.mx_quantize(x)
+        if name == "quantize":
+            got = ops.mx_quantize(x.repeat(parts, 1)[:-5])
+            wanted = q[:2]
+        else:
+            got = (ops.mx_dequantize(ops.Mx(q.codes.repeat(parts, 1)[:-5], q.scales.repeat(parts, 1)[:-5], 600), B16),)
+            wanted = (ops.mx_dequantize(q, B16),)
+        assert got[0].shape[0] * 5 > 1 << 26
+        for big, small in zip(got, wanted):
+            assert all(torch.equal(part, small[:len(part)]) for part in big.split(4096))
+    elif name == "embedding":  # two tokens a lane, 256 lanes, 2^20 workgroups
+        n, table = (1 << 29) + 70001, values((1 << 20, 2), 2, B16)
+        tokens = torch.randint(-9, 1 << 20, (n,), dtype=torch.int32, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+        out = torch.full((n, 2), 5.0, dtype=B16, device="cuda")
+        ops.embedding(tokens, table, out=out)
+        for r0 in range(0, n, 1 << 24):
+            t = tokens[r0:r0 + (1 << 24)].long()
+            assert torch.equal(out[r0:r0 + (1 << 24)], torch.where((t >= 0)[:, None], table[t.clamp_min(0)], 0.0)), r0
+    elif name == "embedding_grad":  # 128 rows a workgroup
+        rows, n = (1 << 27) + 9001, 1000
+        tokens = torch.randint(0, rows, (n,), device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+        tokens[1:5], tokens[5] = tokens[0], rows - 1
+        g = torch.randint(-8, 9, (n, 3), device="cuda", generator=torch.Generator("cuda").manual_seed(3)).to(F32)  # exact sums
+        out = torch.full((rows, 3), 5.0, dtype=F32, device="cuda")
+        ops.embedding_grad(tokens, g, rows, out=out)
+        assert torch.equal(out, torch.zeros((rows, 3), device="cuda").index_add_(0, tokens, g))
+    else:  # one lane and one element a row
+        rows = (1 << 30) + 5001
+        x = torch.ones((rows, 1), dtype=B16, device="cuda")
+        out = ops.dropout(x, 0.25, 3, index=2**64 - 77, index_stride=3)
+        assert abs(float((out[:1 << 26] == 0).double().mean()) - 0.25) < 6 * math.sqrt(0.25 * 0.75 / 2**26)
+        for r0 in (0, 1 << 29, (1 << 30) - 100, 1 << 30, rows - 3000):
+            part = x[r0:r0 + 3000]
+            assert torch.equal(out[r0:r0 + 3000], ops.dropout(part, 0.25, 3, index=3 * r0 - 77, index_stride=3))
+
+
+@gpu
 def test_offsets_beyond_32_bits():
     """Tables, gradients and outputs whose byte and element offsets pass 2^32: rows spread over 10 GiB."""
     pitch, rows, cols = 1 << 30, 5, 40
