@@ -280,30 +280,28 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 // for any stride, and slow (every value is a load of its own).
 template <bool TRANSPOSED, typename T>
 __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out) {
-  const int64_t pitch = (cols + 127) / 128 * 64, tiles_c = (cols + 15) / 16, tiles = (rows + 15) / 16 * tiles_c;
+  const int64_t pitch = (cols + 127) / 128 * 64;
+  const int64_t tiles_c = (cols + 15) / 16, i0 = blockIdx.x / tiles_c * 16, c0 = blockIdx.x % tiles_c * 16;
   const int lane = threadIdx.x, part = lane / 16;
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t i0 = t / tiles_c * 16, c0 = t % tiles_c * 16;
-    const int64_t i = min(i0 + lane % 16, rows - 1), c = min(c0 + lane % 16, cols - 1);
-    v4f sum = {0, 0, 0, 0};
-    for (int64_t j0 = 0; j0 < inner; j0 += 32) {
-      v4u fg = {0, 0, 0, 0}, fq = {0, 0, 0, 0};
+  const int64_t i = min(i0 + lane % 16, rows - 1), c = min(c0 + lane % 16, cols - 1);
+  v4f sum = {0, 0, 0, 0};
+  for (int64_t j0 = 0; j0 < inner; j0 += 32) {
+    v4u fg = {0, 0, 0, 0}, fq = {0, 0, 0, 0};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int64_t j = j0 + 8 * part + e;
-        if (j >= inner) continue;
-        const int64_t at = TRANSPOSED ? j * g.stride + i : i * g.stride + j;
-        fg[e / 2] |= (uint32_t)ldg<uint16_t, false>((const char*)g.p + 2 * at) << (16 * (e & 1));
-        const uint32_t code = q.codes[j * pitch + c / 2] >> (4 * (c & 1)), s = q.scales[j * (pitch / 16) + c / 32];
-        fq[e / 2] |= (widen2<0>(code & 15u, s) & 0xFFFFu) << (16 * (e & 1));
-      }
-      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, fg), __builtin_bit_cast(v8bf, fq), sum, 0, 0, 0);
+    for (int e = 0; e < 8; ++e) {
+      const int64_t j = j0 + 8 * part + e;
+      if (j >= inner) continue;
+      const int64_t at = TRANSPOSED ? j * g.stride + i : i * g.stride + j;
+      fg[e / 2] |= (uint32_t)ldg<uint16_t, false>((const char*)g.p + 2 * at) << (16 * (e & 1));
+      const uint32_t code = q.codes[j * pitch + c / 2] >> (4 * (c & 1)), s = q.scales[j * (pitch / 16) + c / 32];
+      fq[e / 2] |= (widen2<0>(code & 15u, s) & 0xFFFFu) << (16 * (e & 1));
     }
-    if (c0 + lane % 16 >= cols) continue;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (i0 + 4 * part + r < rows) T::store((char*)out.p, (i0 + 4 * part + r) * out.stride + c, sum[r]);
+    sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, fg), __builtin_bit_cast(v8bf, fq), sum, 0, 0, 0);
   }
+  if (c0 + lane % 16 >= cols) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    if (i0 + 4 * part + r < rows) T::store((char*)out.p, (i0 + 4 * part + r) * out.stride + c, sum[r]);
 }
 
 // out = the sum of `parts` float32 matrices of rows x pitch, in order.  A row takes `lanes` lanes, 8 columns each.
@@ -361,8 +359,13 @@ hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, 
                      hipStream_t stream) {
   if (narrow(TRANSPOSED, rows, inner, g.stride)) {
     const auto kernel = dtype == Elem::f32 ? narrow_kernel<TRANSPOSED, F32> : narrow_kernel<TRANSPOSED, B16>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)narrow_wgs(rows, cols)), dim3(64), 0, stream, g, q, rows,
-                       inner, cols, out);
+    const int64_t band = narrow_band(rows, cols);
+    for (int64_t i = 0; i < rows; i += band) {  // as many rows as a launch holds
+      const int64_t here = std::min(band, rows - i);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)narrow_wgs(here, cols)), dim3(64), 0, stream,
+                         Mat{(const char*)g.p + 2 * (TRANSPOSED ? i : i * g.stride), g.stride}, q, here, inner, cols,
+                         MatOut{(char*)out.p + i * out.stride * (dtype == Elem::f32 ? 4 : 2), out.stride});
+    }
     return hipGetLastError();
   }
   const GradPlan p = grad_plan(rows, inner, cols);

@@ -103,9 +103,11 @@ inline GradPlan grad_plan(int64_t rows, int64_t inner, int64_t cols) {
   return p;
 }
 
-// Workgroups of narrow_kernel, 64 lanes each; tiles of 16 x 16 beyond a launch's are taken in turn.
-inline int64_t narrow_wgs(int64_t rows, int64_t cols) {
-  return std::min((int64_t)(ceil_div(rows, 16) * ceil_div(cols, 16)), (int64_t)1 << 22);
+// narrow_kernel: workgroups of 64 lanes for `rows` rows, 16 x 16 values each, and the rows that go into one launch, fewer
+// than 2^26 workgroups.  (Workgroups that take several tiles in turn: 147 us and not 120 for 8192 x 8192 of 4 terms.)
+inline int64_t narrow_wgs(int64_t rows, int64_t cols) { return (int64_t)(ceil_div(rows, 16) * ceil_div(cols, 16)); }
+inline int64_t narrow_band(int64_t rows, int64_t cols) {
+  return std::min(rows, (((int64_t)1 << 26) - 1) / (int64_t)ceil_div(cols, 16) * 16);
 }
 
 // ---- embedding gradient ----------------------------------------------------------------------------------------

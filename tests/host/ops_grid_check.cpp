@@ -40,12 +40,16 @@ static void check_dropout(int64_t rows, int64_t cols) {
 // What the C entry points of the products and their gradient hand to a launch: of accepted sizes it holds the lanes.
 namespace pat {
 static int64_t g_lanes = -1;
+static int64_t narrow_lanes(int64_t rows, int64_t cols) {  // of the first, largest launch; 0: it would cut a tile
+  const int64_t band = narrow_band(rows, cols);
+  return band > 0 && (band == rows || band % 16 == 0) ? narrow_wgs(band, cols) * 64 : 0;
+}
 void record_hip_error(hipError_t) {}
 hipError_t launch_mx_quantize(Mat, Elem, int64_t, int64_t, uint8_t*, uint8_t*, hipStream_t) { return hipSuccess; }
 hipError_t launch_mx_dequantize(MxMat, int64_t, int64_t, MatOut, Elem, hipStream_t) { return hipSuccess; }
 hipError_t launch_mx_matmul(MxMat, MxMat, int64_t m, int64_t n, int64_t k, MatOut, Elem, hipStream_t) {
   const int tile = product_tile(m, n);
-  g_lanes = k == 0 ? narrow_wgs(m, n) * 64 : tile ? tile_wgs(m, n, tile) * (tile == 256 ? 512 : 256) : split_wgs(m, n) * 64 * kSplitWaves;
+  g_lanes = k == 0 ? narrow_lanes(m, n) : tile ? tile_wgs(m, n, tile) * (tile == 256 ? 512 : 256) : split_wgs(m, n) * 64 * kSplitWaves;
   return hipSuccess;
 }
 size_t mx_linear_workspace(int64_t, int64_t, int64_t) { return 0; }
@@ -55,7 +59,7 @@ hipError_t launch_mx_linear(Mat, Elem, MxMat, int64_t, int64_t, int64_t, MatOut,
 size_t mx_grad_workspace(int64_t, int64_t, int64_t) { return 0; }
 hipError_t launch_mx_grad(Mat, bool, MxMat, int64_t rows, int64_t inner, int64_t cols, MatOut, Elem, void*, hipStream_t) {
   const GradPlan p = grad_plan(rows, inner, cols);
-  g_lanes = std::max(narrow_wgs(rows, cols) * 64, tile_wgs(rows, cols, p.tile) * 512);
+  g_lanes = narrow_lanes(rows, cols) ? std::max(narrow_lanes(rows, cols), tile_wgs(rows, cols, p.tile) * 512) : 0;
   return hipSuccess;
 }
 hipError_t launch_embedding(const void*, int, int64_t, Mat, Elem, int64_t, int64_t, int64_t, float, MatOut, Elem,

@@ -428,7 +428,7 @@ def test_products_of_no_columns_are_zero(m, n, k):
 
 @gpu
 def test_product_of_no_columns_and_many_values_is_zero():
-    """2^35 values, of more tiles than one launch has workgroups of eight waves."""
+    """2^35 values, of more tiles of any size than one launch holds."""
     m = n = 1 << 17
     out = torch.full((2 * m, n), 5.0, dtype=B16, device="cuda")
     ops.mx_matmul(ops.mx_empty(2 * m, 0), ops.mx_empty(n, 0), B16, out)
@@ -475,7 +475,7 @@ def test_matmul_grad(rows, inner, cols, transposed, dtype):
 @gpu
 @pytest.mark.parametrize("rows,cols", [(131075, 131072), (40001, 40003)])
 def test_matmul_grad_of_more_tiles_than_workgroups(rows, cols):
-    """Outer products of more 16 x 16 tiles than one launch has workgroups, the first of 2^34 values and more: each value is
+    """Outer products, the first of more 16 x 16 tiles than one launch holds (2^34 values and more): each value is
     one product, exact in float32 and rounded once."""
     g = values((1, rows), 1, B16)
     q, vq = random_mx(1, cols, 2)
