@@ -20,8 +20,8 @@ __device__ __forceinline__ int64_t token_row(const char* tokens, int token_bytes
 // A row is taken by `lanes` lanes, 8 columns each at a time; a workgroup holds 256 / lanes tokens side by side and
 // TOKENS of them in turn, whose table rows a lane reads before it writes any.
 //
-// Bound by memory: 65536 random tokens of 4096 bfloat16 columns, a table of 32768 rows, in 153 us: 649 MB if each row were
-// read once, 833 MB counted (a row that comes again is mostly gone from the caches), 5.4 TB/s.
+// Bound by memory: 65536 random tokens of 4096 bfloat16 columns, a table of 32768 rows, in 156 us: 649 MB if each row were
+// read once, 837 MB counted (a row that comes again is mostly gone from the caches), 5.4 TB/s.
 template <int TOKENS, typename TI, typename TO>
 __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int token_bytes, int64_t ntokens, Mat table,
                                                      int64_t first, int64_t rows, int64_t cols, float scale, MatOut out,
@@ -67,8 +67,9 @@ __global__ __launch_bounds__(256) void lookup_kernel(const char* tokens, int tok
 // are listed in order; then a wave adds up its rows one by one, or writes zeros.  A row with far more than its share of
 // the list is added up by all waves, a section of the list each, and the waves' sums in order.
 //
-// Bound by latency: a load of tokens, a load of rows of g after it, and a launch: 5 us for 1001 tokens of 333 columns and
-// 1251 rows, of which 3 are a launch of anything (sorted first, in three launches: 19).  7.7 with one of them 64 times.
+// Bound by latency: a load of tokens, a load of rows of g after it, and a launch: 5.4 us for 1001 tokens of 333 columns all
+// over 1251 rows, of which 3 are a launch of anything (sorted first, in three launches: 19).  7.4 to 7.7 where a token comes
+// more often, 64 times.
 
 constexpr int kFewWaves = 16, kFewMostEach = 8;
 static_assert(kFewTokens == 64 * kFewWaves, "a token a lane");
@@ -347,8 +348,8 @@ __global__ __launch_bounds__(kSortThreads) void scatter_kernel(SortArgs a) {
   }
 }
 
-// The whole sort in one workgroup, for so few tokens that launches are what it costs (us, 1001 tokens of 1251 rows: 14.5
-// in four launches, 6.8 in this one).  Entries stay in LDS from pass to pass; a wave takes a section of them, 64 at a time.
+// The whole sort in one workgroup, for so few tokens that launches are what it costs: 8 us for 2048 tokens of 1251 rows, 14
+// for 4096 of 50000 (both ways' times stand at the rule, with kSmallTokens).  Entries stay in LDS from pass to pass; a wave takes a section of them, 64 at a time.
 constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
 
 __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(SortArgs a, int passes) {
@@ -442,8 +443,8 @@ __device__ __forceinline__ int32_t wave_lower_bound(const int32_t* keys, int32_t
 // order.  A piece has two such rows at most: slot 0 for the row of its first entry, slot 1 for that of its last.
 // Rows without an entry are zeroed by workgroups of their own in the same launch.
 //
-// Bound by memory: 131072 tokens of 2048 bfloat16 columns into 65536 float32 rows (1.07 GB) in 210 us, 5.1 TB/s, and
-// 18 us for the rows over pieces.  1001 tokens of 333 columns: 9 and 4 us, launches and one chain of loads.
+// Bound by memory: 131072 tokens of 2048 bfloat16 columns into 65536 float32 rows (1.07 GB) in 210 to 222 us, 5.1 TB/s, and
+// 17 us for the rows over pieces.  2048 float32 tokens of 333 columns, 1251 rows: 8 and 5 us, launches and one chain of loads.
 
 struct SumArgs {
   const int32_t *keys, *pos, *nvalid;
@@ -499,7 +500,7 @@ __device__ void zero_rows(const SumArgs& a, int wg, int32_t n) {
   }
 }
 
-// UNIFORM: a piece's lanes are whole waves (rows of 505 columns and more).  A wave then holds 64 entries at a time, one
+// UNIFORM: a piece's lanes are whole waves (rows of 257 columns and more).  A wave then holds 64 entries at a time, one
 // per lane, and takes each from its lane into scalar registers: no load of a row waits for a load of its entry.
 template <bool UNIFORM, typename TI, typename TO>
 __global__ __launch_bounds__(256) void sum_kernel(SumArgs a) {

@@ -9,7 +9,7 @@ namespace {
 // takes 16 groups side by side and kGroups of those in turn, all read before any is written.
 //
 // Bound by memory: 8192 x 8192 bfloat16 (170 MB) in 27 us, 6.3 TB/s, by nontemporal loads (29 otherwise, and
-// 8192 x 8192 x 8192 with it took 12 longer); 1001 x 1000 float32 (4.5 MB) in 3.6 us, of which 3 are a launch of anything.
+// 8192 x 8192 x 8192 with it took 12 longer); 1001 x 1000 float32 (4.5 MB) in 3.4 us, of which 3 are a launch of anything.
 constexpr int kGroups = 4;
 
 template <typename T>

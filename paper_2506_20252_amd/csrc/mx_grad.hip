@@ -19,10 +19,11 @@ namespace {
 // waves on a SIMD one multiplies first and the other widens first, so that the matrix unit and the vector unit both have
 // work (229 and 226 us for the sizes below on one card, 236 and 235 with all in the same order).
 //
-// Bound by the matrix instructions: 8192 x 4096 x 4096 in 222 us (g as given) and 221 us (g by j, float32 out), 1240
-// TFLOP/s, beside 1395 of a large bfloat16 library product; turning q and g round by vector instructions on their way into
-// LDS took 228 and 240.  1001 x 1000 x 1333: 12.3 and 12.9 us (15 and 17), the latency of 8 steps in turn with one or two
-// workgroups a CU.
+// 8192 x 4096 x 4096 in 220 us (g as given) and 225 us (g by j, float32 out), 1235 TFLOP/s, beside 1622 of a large bfloat16
+// library product of rows by rows and 1398 of rows by columns; the first dozens of calls from an idle card take 240 to 300.
+// The matrix units work in 0.6 of the busy CUs' cycles; what is between is widening, and LDS's reads and barriers.  Turning q
+// and g round by vector instructions on their way into LDS took 6 and 19 longer.  1001 x 1000 x 1333: 13.1 and 13.4 us (15 and
+// 17), the latency of 8 to 11 steps in turn with one or two workgroups a CU.
 //
 // PARTS: as many such groups of waves in a workgroup, each with its own part of j and its own LDS; their sums are added
 // in order at the end.  For few tiles, whose waves would otherwise wait for one another's latencies alone.

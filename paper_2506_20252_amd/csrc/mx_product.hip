@@ -34,9 +34,9 @@ __device__ __forceinline__ v8i frag(v4i c) { return v8i{c[0], c[1], c[2], c[3], 
 // row l mod 32 and one block, and any two blocks will do as long as both sides take the same.  Lane half h takes blocks
 // 2h and 2h + 1 of a group in turn, whose scales are two neighbouring bytes: the instruction picks the byte.
 //
-// 8192 x 8192 x 8192: 255 to 300 us by card, 4.3 to 3.7 PFLOP/s, where the instructions alone take 160 for these columns, the
-// loads alone 190 (45 GB/s a CU: 12 % of what is read from L2 is not there) and the reads of LDS nearly the cycles of the
-// instructions; 25 us are each tile's first loads and its stores.  Four waves of 128 x 128 take as long as these eight.
+// 8192 x 8192 x 8192: 265 us, 4.15 PFLOP/s (the first dozens of calls from an idle card up to 345), where the instructions
+// alone take 160 for these columns, the loads alone 190 (45 GB/s a CU: 12 % of what is read from L2 is not there) and the
+// reads of LDS nearly the cycles of the instructions; 25 us are each tile's first loads and its stores.  Four waves of 128 x 128 take as long as these eight.
 // Slower: four groups of 128 columns in LDS (330: pieces of 64 bytes), a barrier of its own for the release of LDS (290
 // beside 277).
 
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void tile_kernel(MxMat a, MxMat b,
 // FUSED: the rows of a are still x, float32 or bfloat16.  The workgroup quantises all of them into LDS first; every
 // workgroup repeats that, which is little beside its part of b as long as the rows are few.
 //
-// Bound by the reading of b: one row of 8192 columns by 8192 rows of b (36 MB) in 9.6 us, of which 3 are a launch of
+// Bound by the reading of b: one row of 8192 columns by 8192 rows of b (36 MB) in 9.3 us, of which 3 are a launch of
 // anything; 24 quantised rows of 4001 by 5000 (11 MB) in 7.
 
 template <int MT, int NT, bool FUSED, typename X, typename T>

@@ -283,7 +283,8 @@ struct TilePlace {
 };
 // Workgroups go to the 8 XCDs in turn; each XCD gets consecutive tiles, in bands of 6 tile rows, so that the 32 tiles that
 // it works on together are nearly square and what they read stays in its L2 (us with bands of 4, 6, 8, 16: 297, 294, 300,
-// 300 for 8192 x 8192 x 8192 with its quantisation, 445, 447, 455, 470 for both gradients of 8192 x 4096 x 4096).
+// 300 for 8192 x 8192 x 8192 with its quantisation, 445, 447, 455, 470 for both gradients of 8192 x 4096 x 4096;
+// timed at these two sizes alone).
 __device__ __forceinline__ bool tile_place(int64_t tiles_m, int64_t tiles_n, TilePlace* p) {
   constexpr int kBand = 6;
   const int64_t total = tiles_m * tiles_n, per = (total + 7) / 8;

@@ -10,6 +10,10 @@ by the HIP kernels of ``libpat.so``, and there is no fallback.
 Tensors are 2-D with unit stride along rows; rows may be strided.  Calls run on
 `stream`, by default torch's current stream of the tensors' device; what they
 allocate belongs to that stream.
+
+Nothing here is recorded for autograd: a result carries no graph, also where an
+input requires grad.  A training step calls the gradients by name, or from an
+autograd function of its own.
 """
 
 import ctypes
