@@ -110,14 +110,14 @@ def _blocks(x):
 
 
 def _plain_eighths(x):
-    """8-bit blocks: the least power of two under which no value of the block is above 448, and the nearest multiples that
+    """8-bit blocks: the least power of two under which no value of the block is above 3.75, and the nearest multiples that
     three mantissa bits hold (ties to even, 2^-9 the smallest step).  Returns the multiples [rows, blocks, 32], float32,
     and the scale bytes [rows, blocks], int32."""
     v = _blocks(x)
     high = v.abs().amax(2).view(torch.int32)
-    field = (high >> 23) - 8 + ((high & 0x7FFFFF) > 0x600000).int()
+    field = (high >> 23) - 1 + ((high & 0x7FFFFF) > 0x700000).int()
     byte = torch.where(high >= 0x7F800000, 255, field.clamp_min(0)).to(torch.int32)
-    down = _pow2(254 - byte.clamp_max(253))  # at least 2^-126, the other way round
+    down = _pow2(254 - byte.clamp_max(254))
     v = torch.where((byte == 255)[..., None], 0.0, v * down[..., None])
     exponent = ((v.view(torch.int32) >> 23 & 255) - 127).clamp_min(-6)
     step = ((exponent - 3 + 127) << 23).view(torch.float32)
@@ -392,8 +392,8 @@ def _exact_eight(x):
     full[:, :cols] = x
     blocks = full.view(rows, -1, BLOCK)
     high = blocks.abs().amax(2, keepdim=True)
-    f, e = torch.frexp(high)  # high = f 2^e, f in [1/2, 1); 448 = 7/8 * 2^9
-    unit = torch.exp2((e - 9 + (f > 0.875)).clamp_min(-127).double())
+    f, e = torch.frexp(high)  # high = f 2^e, f in [1/2, 1); 3.75 = 15/16 * 2^2
+    unit = torch.exp2((e - 2 + (f > 0.9375)).clamp_min(-127).double())
     unit = torch.where(high == 0, 2.0**-127, unit)
     a = blocks / unit
     _, e = torch.frexp(a)
