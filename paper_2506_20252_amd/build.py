@@ -22,7 +22,8 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
 TARGETS = [
     (os.path.join(PKG, "libpat.so"),
      [os.path.join(CSRC, f) for f in ("plan.cpp", "api.cpp", "kernels.hip", "walk.hip", "noalloc.hip",
-                                      "ops.cpp", "mx.hip", "mx_product.hip", "mx_grad.hip", "embedding.hip", "dropout.hip")]),
+                                      "ops.cpp", "mx.hip", "mx_product.hip", "mx_grad.hip", "embedding.hip", "dropout.hip",
+                                      "layer.cpp", "mxb.hip", "mxb_product.hip", "gated.hip", "norm.hip")]),
     (os.path.join(ROOT, "synth", "libpatsynth.so"), [os.path.join(ROOT, "synth", "synth.hip")]),
     (os.path.join(PKG, "libpatceiling.so"), [os.path.join(CSRC, "ceiling.hip")]),
 ]

@@ -1,5 +1,5 @@
-// Products of a bfloat16 gradient with a 4-bit matrix, out[i][c] = sum over j of g[i][j] q[j][c] (or g[j][i]): both
-// gradients of the 4-bit product.
+// Products of a bfloat16 gradient with a matrix in blocks, out[i][c] = sum over j of g[i][j] q[j][c] (or g[j][i]): both
+// gradients of the 4-bit product, and the weight's gradient from an input in 8-bit blocks.
 //
 // The sum runs over rows of q, across its blocks, so q is widened to bfloat16 (exactly) and multiplied by the bfloat16
 // matrix instructions.  These want 8 consecutive j of one row of g and of one column of q in a lane, while q, and g where
@@ -7,7 +7,7 @@
 // (ds_read_b64_tr_b16) turn them round on the way to the registers.
 #include <algorithm>
 
-#include "ops_device.hpp"
+#include "layer_device.hpp"
 
 namespace pat {
 namespace {
@@ -62,14 +62,41 @@ __device__ __forceinline__ v8bf read_turned(const uint8_t* at, int j0) {
   return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Two codes of a byte (the I-th of a word) as two bfloat16.
-template <int I>
-__device__ __forceinline__ uint32_t widen2(uint32_t code, uint32_t s) {
-  const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, mx_scale_operand(s), I);
-  return __builtin_bit_cast(uint32_t, v);
-}
+// What q's codes are: how many bytes 8 columns take, and the 8 bfloat16 that they stand for under scale byte s.  Every
+// value of a 4-bit block is one exactly, and of an 8-bit block every one above 2^-127.
+struct Fours {
+  static constexpr int kBytes = 4;
+  typedef uint32_t Codes;
+  // two codes of a byte (the I-th of the word)
+  template <int I>
+  __device__ static uint32_t widen2(Codes code, uint32_t s) {
+    const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, mx_scale_operand(s), I);
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  __device__ static v4u widen(Codes c, uint32_t s) { return v4u{widen2<0>(c, s), widen2<1>(c, s), widen2<2>(c, s), widen2<3>(c, s)}; }
+  __device__ static Codes none() { return 0u; }
+  // column c's bfloat16, of a row's codes
+  __device__ static uint32_t one(const uint8_t* row, int64_t c, uint32_t s) {
+    const uint32_t code = row[c / 2] >> (4 * (c & 1));
+    return widen2<0>(code & 15u, s) & 0xFFFFu;
+  }
+};
+struct Eights {
+  static constexpr int kBytes = 8;
+  typedef v2u Codes;
+  template <bool HIGH>
+  __device__ static uint32_t widen2(uint32_t code, uint32_t s) {
+    const v2bf v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, mx_scale_operand(s), HIGH);
+    return __builtin_bit_cast(uint32_t, v);
+  }
+  __device__ static v4u widen(Codes c, uint32_t s) {
+    return v4u{widen2<false>(c[0], s), widen2<true>(c[0], s), widen2<false>(c[1], s), widen2<true>(c[1], s)};
+  }
+  __device__ static Codes none() { return v2u{0, 0}; }
+  __device__ static uint32_t one(const uint8_t* row, int64_t c, uint32_t s) { return widen2<false>(row[c], s) & 0xFFFFu; }
+};
 
-template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED, bool EDGE, typename T>
+template <typename Q, int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED, bool EDGE, typename T>
 __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, MxMat q, int64_t rows, int64_t inner,
                                                                        int64_t cols, MatOut out, int64_t slice) {
   typedef GradTile<FA, FB, WA, WB> S;
@@ -79,12 +106,12 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   TilePlace place;
   if (!tile_place((rows + R - 1) / R, (cols + R - 1) / R, &place)) return;
   const int64_t i0 = place.i * R, c0 = place.j * R;
-  const int64_t pitch = (cols + 127) / 128 * 64;
+  const int64_t pitch = (cols + 127) / 128 * (16 * Q::kBytes), spitch = pitch / (4 * Q::kBytes);  // of codes, of scales
   if (gridDim.y > 1) {  // this launch row's slice of j, into its own matrix
     const int64_t j = blockIdx.y * slice;
     g.p = (const char*)g.p + 2 * (TRANSPOSED ? j * g.stride : j);
     q.codes += j * pitch;
-    q.scales += j * (pitch / 16);
+    q.scales += j * spitch;
     out.p = (char*)out.p + (int64_t)blockIdx.y * rows * out.stride * T::kBytes;
     inner = min(slice, inner - j);
   }
@@ -101,8 +128,8 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
   constexpr int GROUPS = R / 32;
   const int scale_j = wave * (64 / PIECES) + lane % 16 / GROUPS + min(lane / 16, EACH - 1) * SIDE;
   const int scale_of = 4 * (lane / PIECES * GROUPS + piece / 4);  // the lane that has this lane's, 16 lanes further for each row
-  const uint32_t q_at = (uint32_t)(first * pitch + min(c0 / 2 + piece * 4, pitch - 4));
-  const uint32_t q_scale_at = (uint32_t)(scale_j * (pitch / 16) + min(c0 / 32 + lane % GROUPS, pitch / 16 - 1));
+  const uint32_t q_at = (uint32_t)(first * pitch + min(c0 * Q::kBytes / 8 + piece * Q::kBytes, pitch - Q::kBytes));
+  const uint32_t q_scale_at = (uint32_t)(scale_j * spitch + min(c0 / 32 + lane % GROUPS, spitch - 1));
   const int64_t gi = min(i0 + piece * 8, rows - 8);  // TRANSPOSED: the first row of out that is read
   const int over = (int)min(i0 + piece * 8 - gi, (int64_t)8);
   constexpr int BLOCKS = R * 8 / NT;
@@ -116,7 +143,8 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
                                         : (min(i0 + u * (NT / 8) + row_u, rows - 1) - i0) * g.stride + block * 8);
   const char* g_base = (const char*)g.p + (TRANSPOSED ? 0 : 2 * i0 * g.stride);
 
-  uint32_t codes[EACH], scales;
+  typename Q::Codes codes[EACH];
+  uint32_t scales;
   Raw8<B16> raw[VECTORS];
 
   // TAIL: perhaps fewer than 64 values of j are left.
@@ -127,14 +155,13 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
       const int64_t j = j0 + u * SIDE, back = TAIL ? max(first + u * SIDE - (left - 1), 0) : 0;
-      codes[u] = ldg<uint32_t, false>((const char*)q.codes + j * pitch + (TAIL ? q_at - back * pitch : q_at));
+      codes[u] = ldg<typename Q::Codes, false>((const char*)q.codes + j * pitch + (TAIL ? q_at - back * pitch : q_at));
       if constexpr (TRANSPOSED)
         raw[u].w[0] = ldg<v4u, false, 2>(g_base + 2 * j * g.stride + (TAIL ? g_at[0] - 2 * back * g.stride : g_at[0]));
     }
     {
       const int64_t back = TAIL ? max(scale_j - (left - 1), 0) : 0;
-      scales = ldg<uint8_t, false>((const char*)q.scales + j0 * (pitch / 16) +
-                                   (TAIL ? q_scale_at - back * (pitch / 16) : q_scale_at));
+      scales = ldg<uint8_t, false>((const char*)q.scales + j0 * spitch + (TAIL ? q_scale_at - back * spitch : q_scale_at));
     }
     if constexpr (!TRANSPOSED) {
       const int64_t back = TAIL ? max(j0 + block * 8 - (inner - 8), (int64_t)0) : 0;
@@ -148,10 +175,11 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
     const int left = TAIL ? (int)min(inner - j0, (int64_t)64) : 64;
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
-      uint32_t code = codes[u], s = __builtin_amdgcn_ds_bpermute(scale_of + 64 * u, scales);
+      typename Q::Codes code = codes[u];
+      uint32_t s = __builtin_amdgcn_ds_bpermute(scale_of + 64 * u, scales);
       const bool in = !TAIL || first + u * SIDE < left;
-      if (TAIL) code = in ? code : 0u, s = in ? s : 0u;
-      *(v4u*)(l.q + put + u * SIDE * 2 * R) = v4u{widen2<0>(code, s), widen2<1>(code, s), widen2<2>(code, s), widen2<3>(code, s)};
+      if (TAIL) code = in ? code : Q::none(), s = in ? s : 0u;
+      *(v4u*)(l.q + put + u * SIDE * 2 * R) = Q::widen(code, s);
       if constexpr (TRANSPOSED) {
         if constexpr (EDGE) move_down(raw[u], over);
         if (TAIL && !in) raw[u].w[0] = v4u{0, 0, 0, 0};
@@ -279,9 +307,9 @@ __global__ __launch_bounds__(64 * WA * WB * PARTS, 2) void grad_kernel(Mat g, Mx
 // or where a tile's rows of g are so far apart that their offsets need more than 32 bits.  One wave per 16 x 16 of out; an
 // instruction of 16 x 16 x 32 takes j = 8 * (l / 16) ... + 7 of row and column l mod 16 in lane l, read one by one: right
 // for any stride, and slow (every value is a load of its own).
-template <bool TRANSPOSED, typename T>
+template <typename Q, bool TRANSPOSED, typename T>
 __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out) {
-  const int64_t pitch = (cols + 127) / 128 * 64;
+  const int64_t pitch = (cols + 127) / 128 * (16 * Q::kBytes), spitch = pitch / (4 * Q::kBytes);  // of codes, of scales
   const int64_t tiles_c = (cols + 15) / 16, i0 = blockIdx.x / tiles_c * 16, c0 = blockIdx.x % tiles_c * 16;
   const int lane = threadIdx.x, part = lane / 16;
   const int64_t i = min(i0 + lane % 16, rows - 1), c = min(c0 + lane % 16, cols - 1);
@@ -294,8 +322,7 @@ __global__ __launch_bounds__(64) void narrow_kernel(Mat g, MxMat q, int64_t rows
       if (j >= inner) continue;
       const int64_t at = TRANSPOSED ? j * g.stride + i : i * g.stride + j;
       fg[e / 2] |= (uint32_t)ldg<uint16_t, false>((const char*)g.p + 2 * at) << (16 * (e & 1));
-      const uint32_t code = q.codes[j * pitch + c / 2] >> (4 * (c & 1)), s = q.scales[j * (pitch / 16) + c / 32];
-      fq[e / 2] |= (widen2<0>(code & 15u, s) & 0xFFFFu) << (16 * (e & 1));
+      fq[e / 2] |= Q::one(q.codes + j * pitch, c, q.scales[j * spitch + c / 32]) << (16 * (e & 1));
     }
     sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, fg), __builtin_bit_cast(v8bf, fq), sum, 0, 0, 0);
   }
@@ -329,17 +356,17 @@ __global__ __launch_bounds__(256) void add_kernel(const float* sums, int parts, 
 
 int64_t slice_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
 
-template <int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED>
+template <typename Q, int FA, int FB, int WA, int WB, int PARTS, bool TRANSPOSED>
 hipError_t run_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, const GradPlan& p,
                     void* workspace, hipStream_t stream) {
   constexpr int R = GradTile<FA, FB, WA, WB>::R;
   const bool sliced = p.slices > 1, f32 = dtype == Elem::f32;
   const MatOut to = sliced ? MatOut{workspace, slice_pitch(cols)} : out;
-  auto kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, false, F32>
-                              : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, false, B16>;
+  auto kernel = f32 || sliced ? grad_kernel<Q, FA, FB, WA, WB, PARTS, TRANSPOSED, false, F32>
+                              : grad_kernel<Q, FA, FB, WA, WB, PARTS, TRANSPOSED, false, B16>;
   if (TRANSPOSED && rows % 8)
-    kernel = f32 || sliced ? grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, F32>
-                           : grad_kernel<FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, B16>;
+    kernel = f32 || sliced ? grad_kernel<Q, FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, F32>
+                           : grad_kernel<Q, FA, FB, WA, WB, PARTS, TRANSPOSED, TRANSPOSED, B16>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)tile_wgs(rows, cols, R), (unsigned)p.slices), dim3(64 * WA * WB * PARTS), 0,
                      stream, g, q, rows, inner, cols, to, p.slice);
   if (sliced) {
@@ -355,11 +382,11 @@ bool narrow(bool transposed, int64_t rows, int64_t inner, int64_t stride) {
   return inner < 8 || (transposed && rows < 8) || stride > 1 << 22;  // 256 rows of 2 bytes: below 2^31
 }
 
-template <bool TRANSPOSED>
+template <typename Q, bool TRANSPOSED>
 hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype, void* workspace,
                      hipStream_t stream) {
   if (narrow(TRANSPOSED, rows, inner, g.stride)) {
-    const auto kernel = dtype == Elem::f32 ? narrow_kernel<TRANSPOSED, F32> : narrow_kernel<TRANSPOSED, B16>;
+    const auto kernel = dtype == Elem::f32 ? narrow_kernel<Q, TRANSPOSED, F32> : narrow_kernel<Q, TRANSPOSED, B16>;
     const int64_t band = narrow_band(rows, cols);
     for (int64_t i = 0; i < rows; i += band) {  // as many rows as a launch holds
       const int64_t here = std::min(band, rows - i);
@@ -370,9 +397,9 @@ hipError_t pick_grad(Mat g, MxMat q, int64_t rows, int64_t inner, int64_t cols, 
     return hipGetLastError();
   }
   const GradPlan p = grad_plan(rows, inner, cols);
-  if (p.tile == 256) return run_grad<4, 2, 2, 4, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
-  if (p.tile == 128) return run_grad<2, 2, 2, 2, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
-  return run_grad<1, 1, 2, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
+  if (p.tile == 256) return run_grad<Q, 4, 2, 2, 4, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
+  if (p.tile == 128) return run_grad<Q, 2, 2, 2, 2, 1, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
+  return run_grad<Q, 1, 1, 2, 2, 2, TRANSPOSED>(g, q, rows, inner, cols, out, dtype, p, workspace, stream);
 }
 
 }  // namespace
@@ -384,8 +411,13 @@ size_t mx_grad_workspace(int64_t rows, int64_t inner, int64_t cols) {
 
 hipError_t launch_mx_grad(Mat g, bool transposed, MxMat q, int64_t rows, int64_t inner, int64_t cols, MatOut out,
                           Elem dtype, void* workspace, hipStream_t stream) {
-  return transposed ? pick_grad<true>(g, q, rows, inner, cols, out, dtype, workspace, stream)
-                    : pick_grad<false>(g, q, rows, inner, cols, out, dtype, workspace, stream);
+  return transposed ? pick_grad<Fours, true>(g, q, rows, inner, cols, out, dtype, workspace, stream)
+                    : pick_grad<Fours, false>(g, q, rows, inner, cols, out, dtype, workspace, stream);
+}
+
+hipError_t launch_mxb_weight_grad(Mat g, MxbMat x, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype,
+                                  void* workspace, hipStream_t stream) {
+  return pick_grad<Eights, true>(g, {x.codes, x.scales}, rows, inner, cols, out, dtype, workspace, stream);
 }
 
 }  // namespace pat

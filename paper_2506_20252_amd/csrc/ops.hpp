@@ -66,4 +66,62 @@ struct DropoutArgs {
 };
 hipError_t launch_dropout(const DropoutArgs& a, Elem dtype, hipStream_t stream);
 
+// ---- layer.cpp -----------------------------------------------------------------------------------------------------
+
+// 8-bit blocks in the stored form, groups as above; MxbOut with codes == nullptr: not wanted.
+struct MxbMat {
+  const uint8_t* codes;
+  const uint8_t* scales;
+};
+struct MxbOut {
+  uint8_t* codes;
+  uint8_t* scales;
+};
+
+hipError_t launch_mxb_quantize(Mat x, Elem dtype, int64_t rows, int64_t cols, MxbOut q, hipStream_t stream);
+hipError_t launch_mxb_dequantize(MxbMat q, int64_t rows, int64_t cols, MatOut out, Elem dtype, hipStream_t stream);
+
+// What is done with x w^T before it is stored.  Not gated: plus `residual` (p == nullptr: none), to `out`.  Gated: to `out`
+// or, where its p is nullptr, to `blocks`; what a checkpoint keeps to saved_a and saved_b.
+enum class Act : int { silu, gelu };
+struct Epilogue {
+  bool gated;
+  Act act;
+  Mat residual;
+  MatOut out;
+  Elem dtype;
+  MxbOut blocks, saved_a, saved_b;
+};
+// w has n rows, 2 n where gated; k > 0 or not.
+hipError_t launch_mxb_product(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream);
+
+hipError_t launch_mxb_weight_grad(Mat g, MxbMat x, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype,
+                                  void* workspace, hipStream_t stream);
+
+hipError_t launch_gated_grad(Mat g, Elem dtype, MxbMat a, MxbMat b, int64_t m, int64_t n, Act act, MatOut out,
+                             hipStream_t stream);
+
+struct NormArgs {
+  Mat x, residual;  // residual.p == nullptr: none
+  const void* weight;
+  int64_t rows, cols;
+  float eps;
+  MatOut total, out;  // p == nullptr: not wanted
+  MxbOut blocks;
+  Elem dtype, weight_dtype, out_dtype;
+};
+hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream);
+
+struct NormGradArgs {
+  Mat g, x, total_grad;  // total_grad.p == nullptr: none
+  const void* weight;
+  int64_t rows, cols;
+  float eps;
+  MatOut out;
+  float* dweight;
+  Elem dtype, x_dtype, weight_dtype;
+};
+size_t rms_norm_grad_workspace(int64_t rows, int64_t cols);
+hipError_t launch_rms_norm_grad(const NormGradArgs& a, void* workspace, hipStream_t stream);
+
 }  // namespace pat
