@@ -55,6 +55,13 @@ inline NormGradPlan norm_grad_plan(int64_t rows, int64_t cols) {
 
 // ---- products of 8-bit with 4-bit blocks ------------------------------------------------------------------------
 
+// Tiles of m tokens by n rows of the weight: 256 (256 x 256), 128 (128 x 128) or 64 (64 tokens x 128 rows).  The largest that
+// gives more than half of the 256 CUs one.
+inline int layer_tile(int64_t m, int64_t n) {
+  auto tiles = [&](int rows_x, int rows_w) { return (int64_t)(ceil_div(m, rows_x) * ceil_div(n, rows_w)); };
+  return tiles(256, 256) > 128 ? 256 : tiles(128, 128) > 128 ? 128 : 64;
+}
+
 // few_kernel: tokens and columns of the output of a workgroup, in sixteens (a gated column is two rows of the weight), and
 // the tokens that go into one launch of fewer than 2^22 workgroups.
 constexpr int kFewMost = 48;

@@ -52,6 +52,304 @@ __device__ __forceinline__ void store4(char* p, int64_t left, const v4f& f) {
       if (i < left) T::store(p, i, v[i]);
 }
 
+// ---- tiles through LDS ---------------------------------------------------------------------------------------
+//
+// A workgroup of WN x WM waves computes a tile of N rows of the weight by M tokens, a wave FN x FM blocks of 32 x 32; of a
+// gated tile's rows every wave has as many of either half, so that a and b of a value are the same lane's.  It goes through
+// the terms 128 at a time.  What the step after the next multiplies is on its way into LDS, written there by the loads
+// themselves: the tokens' 128 bytes a row, and with every other step the 128 bytes that hold 256 terms of the weight's rows
+// (half lines would take twice the requests), and both sides' scales of 256 terms.
+//
+// LDS holds a row's eight 16-byte pieces at place piece ^ (row / 2 mod 8): a row is half of the 64 banks, so 16 lanes that
+// read one piece of consecutive rows hit all banks once.  The loads write lane after lane, so each lane fetches the piece
+// that belongs at its place.  An instruction of 32 x 32 x 64 takes two blocks of 32 terms: of the weight lane l has row
+// l mod 32 and all of block l / 32, of the activations 16 terms of each.  Any two blocks will do as long as both sides
+// take the same; the J-th instruction of a step takes the J-th and the J + 2-nd of its four, so that a lane's scales
+// are two neighbouring bytes, of which the instruction picks the J-th.
+typedef __attribute__((address_space(1))) const uint32_t* GlobalWords;
+typedef __attribute__((address_space(3))) uint32_t* LdsWords;
+
+template <int FN, int FM, int WN, int WM>
+struct Tile {
+  static constexpr int kWaves = WN * WM, N = 32 * FN * WN, M = 32 * FM * WM;
+  struct Pair {  // 256 terms
+    uint8_t codes[N * 128];
+    uint8_t w_scales[N * 8], x_scales[M * 8];
+  };
+  struct Step {  // 128 terms
+    uint8_t codes[M * 128];
+  };
+};
+
+// Writes NB blocks of 32 columns, of one token a lane as the instructions leave them (lane l: token l mod 32, columns
+// 8 * (c / 4) + 4 * (l / 32) + c mod 4), to columns j ... of tokens i ...: the wave turns them round in `part`, LDS of its own.
+constexpr int turn_floats(int nb) { return 32 * (32 * nb + 4); }
+
+template <int NB, typename T, bool NT>
+__device__ __forceinline__ void store_turned(const float (&v)[NB][16], float* part, int64_t i, int64_t j, int64_t m, int64_t n,
+                                             Mat residual, MatOut out) {
+  constexpr int P = 32 * NB + 4, LANES = 4 * NB, ROWS = 64 / LANES;  // floats a token; lanes and tokens of an access
+  const int lane = threadIdx.x % 64, half = lane / 32, c = lane % LANES * 8;
+  const int64_t left = n - j - c;
+  float r[32 / ROWS][8];
+#pragma unroll
+  for (int u = 0; u < 32 / ROWS; ++u) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[u][e] = 0.0f;
+    const int64_t row = i + u * ROWS + lane / LANES;
+    if (residual.p && row < m && left > 0) {
+      const char* p = (const char*)residual.p + (row * residual.stride + j + c) * T::kBytes;
+      if (left >= 8) load8<T, false, false, kWhole>(p, 8, 4, r[u]);
+      else load8<T, false, false, kFew>(p, left, 4, r[u]);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < NB; ++x)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *(v4f*)(part + lane % 32 * P + 32 * x + 8 * e + 4 * half) = v4f{v[x][4 * e], v[x][4 * e + 1], v[x][4 * e + 2], v[x][4 * e + 3]};
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int u = 0; u < 32 / ROWS; ++u) {
+    const int token = u * ROWS + lane / LANES;
+    const v4f lo = *(const v4f*)(part + token * P + c), hi = *(const v4f*)(part + token * P + c + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[u][e] += lo[e], r[u][4 + e] += hi[e];
+    char* p = (char*)out.p + ((i + token) * out.stride + j + c) * T::kBytes;
+    if (i + token < m && left >= 8) store8<T, false, NT, kWhole>(p, 8, 4, r[u]);
+    else if (i + token < m && left > 0) store8<T, false, NT, kEnd>(p, left, 4, r[u]);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+}
+
+// One block of 32 columns from column j, of one token a lane, as above, in 8 bits: 16 bytes of codes a lane.
+__device__ __forceinline__ void store_block(const float (&f)[16], int64_t i, int64_t j, int64_t m, int64_t n, MxbOut to) {
+  const int half = threadIdx.x % 64 / 32;
+  float v[16];
+  uint32_t high = 0;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    v[e] = j + 8 * (e / 4) + 4 * half + e % 4 < n ? f[e] : 0.0f;
+    high = max(high, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  }
+  const auto other = __builtin_amdgcn_permlane32_swap(high, high, false, false);
+  const uint32_t s = mxb_scale_byte(max(other[0], other[1]));
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = mxb_codes(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3], s);
+  // the halves have every other word of the block: the first two and the last two change hands
+  const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+  const int64_t groups = (n + 127) / 128;
+  if (i >= m || j >= groups * 128) return;
+  stg<false>((char*)to.codes + i * groups * 128 + j + 16 * half, v4u{a[0], a[1], b[0], b[1]});
+  if (half == 0) stg<false>((char*)to.scales + i * groups * 4 + j / 32, (uint8_t)s);
+}
+
+template <int FN, int FM, int WN, int WM, bool GATED, typename O>
+__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w, int64_t m, int64_t n, int groups, int64_t tiles_n,
+                                                               Epilogue ep) {
+  typedef Tile<FN, FM, WN, WM> S;
+  typedef typename S::Pair Pair;
+  typedef typename S::Step Step;
+  constexpr int N = S::N, M = S::M, W = S::kWaves, COLS = GATED ? N / 2 : N;
+  // Objects of their own, and not arrays: the compiler then knows that the loads into one do not touch the others.
+  __shared__ __attribute__((aligned(16))) Pair pair0;
+  __shared__ __attribute__((aligned(16))) Pair pair1;
+  __shared__ __attribute__((aligned(16))) Step step0;
+  __shared__ __attribute__((aligned(16))) Step step1;
+  TilePlace place;
+  if (!tile_place((m + M - 1) / M, tiles_n, &place)) return;
+  const int64_t i0 = place.i * M, j0 = place.j * COLS;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  const uint32_t w_pitch = groups * 64, x_pitch = groups * 128, s_pitch = groups * 4;
+
+  // Rows beyond a matrix are its last row again; what they give is not stored.
+  const int64_t jb = min(j0, n - 1);
+  const int rows_w = (int)min((int64_t)COLS, n - jb), rows_x = (int)min((int64_t)M, m - i0);
+  // Of a gated tile's row: its column, and (the same for 32 rows) whether it is of the second half.
+  auto column = [&](int row) { return GATED ? row / (32 * FN) * (16 * FN) + row / 32 % (FN / 2) * 32 + row % 32 : row; };
+  auto second = [&](int row) { return GATED && row / 32 % FN >= FN / 2; };
+  constexpr int LOADS_W = N / 8 / W, LOADS_X = M / 8 / W;  // of codes, 8 rows each, a wave
+  static_assert(LOADS_W * 8 * W == N && LOADS_X * 8 * W == M && W % 2 == 0, "");
+  uint32_t at_w[LOADS_W], at_x[LOADS_X];  // of this lane's piece, in the rows' codes
+  const int piece = (lane ^ (wave * 8 + lane / 8) / 2) % 8;
+#pragma unroll
+  for (int u = 0; u < LOADS_W; ++u) at_w[u] = (uint32_t)min(column((u * W + wave) * 8 + lane / 8), rows_w - 1) * w_pitch + piece * 16;
+#pragma unroll
+  for (int u = 0; u < LOADS_X; ++u) at_x[u] = (uint32_t)min((u * W + wave) * 8 + lane / 8, rows_x - 1) * x_pitch + piece * 16;
+  // a wave loads the scales of 32 rows, two words each
+  const int s_row = wave * 32 + lane / 2;
+  static_assert(N / 32 <= W && M / 32 <= W, "");
+  const uint32_t sat_w = (uint32_t)min(column(s_row), rows_w - 1) * s_pitch + lane % 2 * 4;
+  const uint32_t sat_x = (uint32_t)min(s_row, rows_x - 1) * s_pitch + lane % 2 * 4;
+  const uint8_t *codes_w = w.codes + jb * w_pitch, *scales_w = w.scales + jb * s_pitch;
+  const uint8_t *codes_x = x.codes + i0 * x_pitch, *scales_x = x.scales + i0 * s_pitch;
+
+  auto fetch_pair = [&](Pair& l, int g) {
+    // the second group of the last 256 terms may not exist: the first again, not multiplied
+    const uint32_t back = g + 1 < groups ? 0 : (piece >= 4 ? 64 : 0), sback = g + 1 < groups ? 0 : lane % 2 * 4;
+#pragma unroll
+    for (int u = 0; u < LOADS_W; ++u) {
+      const uint8_t* p = codes_w + (int64_t)g * 64 + (second((u * W + wave) * 8) ? n * w_pitch : 0);
+      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (at_w[u] - back)), (LdsWords)(l.codes + (u * W + wave) * 1024), 16, 0, 0);
+    }
+    if (N / 32 == W || wave < N / 32) {
+      const uint8_t* p = scales_w + (int64_t)g * 4 + (second(wave * 32) ? n * s_pitch : 0);
+      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (sat_w - sback)), (LdsWords)(l.w_scales + wave * 256), 4, 0, 0);
+    }
+    if (M / 32 == W || wave < M / 32) {
+      const uint8_t* p = scales_x + (int64_t)g * 4;
+      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (sat_x - sback)), (LdsWords)(l.x_scales + wave * 256), 4, 0, 0);
+    }
+  };
+  auto fetch_step = [&](Step& l, int g) {
+#pragma unroll
+    for (int u = 0; u < LOADS_X; ++u)
+      __builtin_amdgcn_global_load_lds((GlobalWords)(codes_x + (int64_t)g * 128 + at_x[u]), (LdsWords)(l.codes + (u * W + wave) * 1024),
+                                       16, 0, 0);
+  };
+
+  const int half = lane / 32, wave_n = wave / WM * 32 * FN, wave_m = wave % WM * 32 * FM;
+  const int row_w = wave_n + lane % 32, row_x = wave_m + lane % 32;
+  v16f acc[FN][FM];
+#pragma unroll
+  for (int a = 0; a < FN; ++a)
+#pragma unroll
+    for (int b = 0; b < FM; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+
+  // What the next instructions multiply is read from LDS while these run, from one register set into the other.
+  struct Blocks {
+    v4i w[FN], x[FM][2];
+  };
+  struct Scales {
+    int w[FN], x[FM];
+  };
+  auto read_scales = [&](const Pair& l, int h, Scales& s) {  // of the h-th group of the pair
+#pragma unroll
+    for (int a = 0; a < FN; ++a) s.w[a] = *(const uint16_t*)(l.w_scales + (row_w + 32 * a) * 8 + 4 * h + 2 * half);
+#pragma unroll
+    for (int b = 0; b < FM; ++b) s.x[b] = *(const uint16_t*)(l.x_scales + (row_x + 32 * b) * 8 + 4 * h + 2 * half);
+  };
+  auto read = [&](const Pair& p, const Step& l, int h, int j, Blocks& c) {
+    auto at = [&](int piece) { return (piece ^ (lane >> 1 & 7)) * 16; };
+#pragma unroll
+    for (int a = 0; a < FN; ++a) c.w[a] = *(const v4i*)(p.codes + (row_w + 32 * a) * 128 + at(4 * h + 2 * half + j));
+#pragma unroll
+    for (int b = 0; b < FM; ++b) {
+      c.x[b][0] = *(const v4i*)(l.codes + (row_x + 32 * b) * 128 + at(2 * j + half));
+      c.x[b][1] = *(const v4i*)(l.codes + (row_x + 32 * b) * 128 + at(4 + 2 * j + half));
+    }
+  };
+  auto multiply = [&](const Blocks& c, const Scales& s, auto which) {
+    constexpr int J = decltype(which)::value;
+#pragma unroll
+    for (int a = 0; a < FN; ++a)
+#pragma unroll
+      for (int b = 0; b < FM; ++b)
+        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(c.w[a]), frag(c.x[b][0], c.x[b][1]), acc[a][b], 4, 0, J, s.w[a],
+                                                                   J, s.x[b]);
+    // these stay together: moved over each other, all steps' blocks would be in registers at once
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  Blocks c0, c1;
+  Scales s0, s1;
+  // Step g, the h-th of pair `p`, out of `l`; the first instructions' blocks are in c0 and the scales in `s`.  Before the second
+  // ones the next step has arrived and this step's LDS has been read by all, so both the next first blocks and what
+  // comes two steps (or pairs) later come in under them.  No branch: beyond the last it is fetched again.
+  auto step = [&](Pair& p, Step& l, const Pair& next_p, const Step& next_l, auto which, const Scales& s, Scales& next_s, int g) {
+    constexpr int H = decltype(which)::value;
+    read(p, l, H, 1, c1);
+    multiply(c0, s, Int<0>{});
+    __syncthreads();
+    read_scales(next_p, 1 - H, next_s);
+    read(next_p, next_l, 1 - H, 0, c0);
+    fetch_step(l, min(g + 2, groups - 1));
+    if constexpr (H == 1) fetch_pair(p, min(g + 3, (groups - 1) / 2 * 2));
+    multiply(c1, s, Int<1>{});
+  };
+  fetch_pair(pair0, 0);
+  fetch_step(step0, 0);
+  __syncthreads();
+  fetch_pair(pair1, min(2, (groups - 1) / 2 * 2));
+  fetch_step(step1, min(1, groups - 1));
+  read_scales(pair0, 0, s0);
+  read(pair0, step0, 0, 0, c0);
+  int g = 0;
+  for (; g + 4 <= groups; g += 4) {
+    step(pair0, step0, pair0, step1, Int<0>{}, s0, s1, g);
+    step(pair0, step1, pair1, step0, Int<1>{}, s1, s0, g + 1);
+    step(pair1, step0, pair1, step1, Int<0>{}, s0, s1, g + 2);
+    step(pair1, step1, pair0, step0, Int<1>{}, s1, s0, g + 3);
+  }
+  if (g < groups) step(pair0, step0, pair0, step1, Int<0>{}, s0, s1, g);
+  if (g + 1 < groups) step(pair0, step1, pair1, step0, Int<1>{}, s1, s0, g + 1);
+  if (g + 2 < groups) step(pair1, step0, pair1, step1, Int<0>{}, s0, s1, g + 2);
+
+  // Results leave through LDS, whose last loads have to have come first.
+  __syncthreads();
+  static_assert(sizeof(Pair) >= W / 2 * turn_floats(2) * 4, "");
+  float* part = (wave < W / 2 ? (float*)&pair0 : (float*)&pair1) + wave % (W / 2) * turn_floats(2);
+  constexpr bool NONTEMPORAL = N * M >= 256 * 256;
+#pragma unroll
+  for (int b = 0; b < FM; ++b) {
+    const int64_t i = i0 + wave_m + 32 * b;
+    if constexpr (!GATED) {
+      static_assert(FN % 2 == 0, "");
+#pragma unroll
+      for (int a = 0; a < FN; a += 2) {
+        float v[2][16];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[y][e] = acc[a + y][b][e];
+        store_turned<2, O, NONTEMPORAL>(v, part, i, j0 + wave_n + 32 * a, m, n, ep.residual, ep.out);
+      }
+    } else {
+      constexpr int H = FN / 2;
+      const int64_t j = j0 + wave_n / 2;
+      float v[H][16];
+#pragma unroll
+      for (int a = 0; a < H; ++a) {
+        float va[16], vb[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          va[e] = acc[a][b][e], vb[e] = acc[H + a][b][e];
+          v[a][e] = activate(ep.act, va[e]) * vb[e];
+        }
+        if (ep.saved_a.codes) {
+          store_block(va, i + lane % 32, j + 32 * a, m, n, ep.saved_a);
+          store_block(vb, i + lane % 32, j + 32 * a, m, n, ep.saved_b);
+        }
+        if constexpr (O::kBytes == 1) store_block(v[a], i + lane % 32, j + 32 * a, m, n, ep.blocks);
+      }
+      if constexpr (O::kBytes > 1) store_turned<H, O, NONTEMPORAL>(v, part, i, j, m, n, {nullptr, 0}, ep.out);
+    }
+  }
+}
+
+template <int FN, int FM, int WN, int WM, bool GATED, typename O>
+hipError_t run_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  typedef Tile<FN, FM, WN, WM> S;
+  const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);
+  const int64_t tiles_n = (int64_t)ceil_div(blocks ? groups_of(n) * 128 : n, GATED ? S::N / 2 : S::N);
+  const int64_t wgs = (int64_t)ceil_div(ceil_div(m, S::M) * tiles_n, 8) * 8;
+  hipLaunchKernelGGL((tile_kernel<FN, FM, WN, WM, GATED, O>), dim3((unsigned)wgs), dim3(64 * WN * WM), 0, stream, x, w, m, n,
+                     (int)groups_of(k), tiles_n, e);
+  return hipGetLastError();
+}
+
+template <bool GATED, typename O>
+hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  switch (layer_tile(m, GATED ? 2 * n : n)) {
+    case 256: return run_tile<4, 2, 2, 4, GATED, O>(x, w, m, n, k, e, stream);
+    case 128: return run_tile<2, 2, 2, 2, GATED, O>(x, w, m, n, k, e, stream);
+    default: return run_tile<2, 1, 2, 2, GATED, O>(x, w, m, n, k, e, stream);
+  }
+}
+
 // ---- few tokens ----------------------------------------------------------------------------------------------
 //
 // A workgroup computes 16 * MT tokens by 16 * H columns (gated: 16 * 2 H rows of the weight); its waves take 512 terms (four
@@ -204,6 +502,10 @@ hipError_t pick_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Ep
 
 template <typename O>
 hipError_t pick(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  if (m > kFewMost && k > 0) {
+    if (e.gated) return pick_tile<true, O>(x, w, m, n, k, e, stream);
+    if constexpr (O::kBytes > 1) return pick_tile<false, O>(x, w, m, n, k, e, stream);
+  }
   switch (few_tokens_sixteens(m)) {
     case 1: return pick_few<1, O>(x, w, m, n, k, e, stream);
     case 2: return pick_few<2, O>(x, w, m, n, k, e, stream);
