@@ -16,20 +16,15 @@ struct NormPlan {
   int64_t wgs;
 };
 
-// Vectors a lane for a row of `units` times 8 columns: 1, 2, 4, or 0 where that is too few.
-inline int norm_vectors(int64_t units, int lanes) {
-  return units <= lanes ? 1 : units <= 2 * lanes ? 2 : units <= 4 * lanes ? 4 : 0;
-}
-
 inline NormPlan norm_plan(int64_t rows, int64_t cols, bool blocks) {
   const int64_t units = blocks ? groups_of(cols) * 16 : (int64_t)ceil_div(cols, 8);  // blocks are filled up to 128 columns
   NormPlan p;
-  p.lanes = row_lanes(units, units <= 4 * kNormThreads ? kNormThreads : kNormMost);
-  while (p.lanes > kNormThreads && units <= 2 * p.lanes) p.lanes /= 2;
+  p.lanes = row_lanes(units, kNormThreads);
+  while (p.lanes < kNormMost && units > 2 * p.lanes) p.lanes *= 2;
   // many rows: a wave each, whose sum needs no LDS
-  if (rows >= 2048 && p.lanes > 64 && units <= 64 * 4) p.lanes = 64;
+  if (rows >= 2048 && p.lanes > 64 && units <= 64 * 2) p.lanes = 64;
   if (blocks && p.lanes < 16) p.lanes = 16;
-  p.vectors = norm_vectors(units, p.lanes);
+  p.vectors = units <= p.lanes ? 1 : units <= 2 * p.lanes ? 2 : 0;
   p.wgs = std::min((int64_t)ceil_div(rows, std::max(kNormThreads, p.lanes) / p.lanes), (int64_t)1 << 20);
   return p;
 }
@@ -44,8 +39,9 @@ struct NormGradPlan {
 inline NormGradPlan norm_grad_plan(int64_t rows, int64_t cols) {
   NormGradPlan p;
   const int64_t units = (int64_t)ceil_div(cols, 8);
-  p.lanes = row_lanes(units, units <= 4 * kNormThreads ? kNormThreads : kNormGradMost);
-  p.vectors = norm_vectors(units, p.lanes);
+  p.lanes = row_lanes(units, kNormThreads);
+  while (p.lanes < kNormGradMost && units > 2 * p.lanes) p.lanes *= 2;
+  p.vectors = units <= p.lanes ? 1 : units <= 2 * p.lanes ? 2 : units <= 4 * p.lanes ? 4 : 0;
   p.pitch = units * 8;
   p.strips = (int64_t)ceil_div(units, kNormThreads);
   const int64_t most = p.vectors ? 512 : std::max<int64_t>(1, 1024 / p.strips);

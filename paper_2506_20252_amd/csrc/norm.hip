@@ -7,19 +7,62 @@
 namespace pat {
 namespace {
 
-// A lane's columns from `col` of a row, those behind the row's end zero, as load8 takes them; `left` columns are there.
-template <typename T, bool SPLIT, Cover C>
-__device__ __forceinline__ void load_cols(const void* row, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
-  load8<T, SPLIT, false, C>((const char*)row + col * T::kBytes, cols - col, gap, v);
+// A lane's 8 columns of a row as they are in memory, as load8 takes them (the second four `gap` columns after the first, those
+// behind the row's end zero once they are widened); nothing is done with what is loaded, so that a row's loads are on their
+// way together.
+template <typename T>
+struct Raw {
+  typename T::vec4 lo, hi;
+};
+template <typename T, bool SPLIT, Cover C, bool NT = false>
+__device__ __forceinline__ Raw<T> load_raw(const void* row, int64_t col, int64_t cols, int64_t gap) {
+  typedef typename T::vec4 V;
+  const int64_t n = cols - col;
+  const char* p = (const char*)row + col * T::kBytes;
+  if constexpr (C == kWhole && !SPLIT && T::kBytes == 2) {
+    const v4u a = ldg<v4u, NT, 2>(p);
+    return {{a[0], a[1]}, {a[2], a[3]}};
+  } else if constexpr (C == kWhole) {
+    return {ldg<V, NT, T::kBytes>(p), ldg<V, NT, T::kBytes>(p + gap * T::kBytes)};
+  } else if constexpr (C == kEnd) {
+    return {ldg<V, NT, T::kBytes>(p + min((int64_t)0, n - 4) * T::kBytes), ldg<V, NT, T::kBytes>(p + min(gap, n - 4) * T::kBytes)};
+  } else {
+    float v[8];
+    load8<T, SPLIT, false, kFew>(p, n, gap, v);
+    return {T::narrow(v), T::narrow(v + 4)};
+  }
 }
+template <typename T, Cover C>
+__device__ __forceinline__ void widen(const Raw<T>& r, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
+  T::widen(r.lo, v);
+  T::widen(r.hi, v + 4);
+  if constexpr (C == kEnd) {
+    const int64_t n = cols - col;
+    move_down(v, max((int64_t)0, 4 - n));
+    move_down(v + 4, max((int64_t)0, gap + 4 - n));
+  }
+}
+// The same of a vector whose type is known at the launch alone.
+struct RawWeight {
+  v4u lo, hi;
+};
 template <bool SPLIT, Cover C>
-__device__ __forceinline__ void load_cols(Elem e, const void* row, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
-  if (e == Elem::f32) load_cols<F32, SPLIT, C>(row, col, cols, gap, v);
-  else load_cols<B16, SPLIT, C>(row, col, cols, gap, v);
+__device__ __forceinline__ RawWeight load_raw(Elem e, const void* weight, int64_t col, int64_t cols, int64_t gap) {
+  if (e == Elem::f32) {
+    const Raw<F32> r = load_raw<F32, SPLIT, C>(weight, col, cols, gap);
+    return {__builtin_bit_cast(v4u, r.lo), __builtin_bit_cast(v4u, r.hi)};
+  }
+  const Raw<B16> r = load_raw<B16, SPLIT, C>(weight, col, cols, gap);
+  return {v4u{r.lo[0], r.lo[1], r.hi[0], r.hi[1]}, v4u{0, 0, 0, 0}};
 }
-template <typename T, bool SPLIT, Cover C>
+template <Cover C>
+__device__ __forceinline__ void widen(Elem e, const RawWeight& r, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
+  if (e == Elem::f32) widen<F32, C>({__builtin_bit_cast(v4f, r.lo), __builtin_bit_cast(v4f, r.hi)}, col, cols, gap, v);
+  else widen<B16, C>({{r.lo[0], r.lo[1]}, {r.lo[2], r.lo[3]}}, col, cols, gap, v);
+}
+template <typename T, bool SPLIT, Cover C, bool NT = false>
 __device__ __forceinline__ void store_cols(void* row, int64_t col, int64_t cols, int64_t gap, const float (&v)[8]) {
-  store8<T, SPLIT, false, C>((char*)row + col * T::kBytes, cols - col, gap, v);
+  store8<T, SPLIT, NT, C>((char*)row + col * T::kBytes, cols - col, gap, v);
 }
 template <typename T>
 __device__ __forceinline__ const char* row_of(Mat m, int64_t r) {
@@ -75,21 +118,10 @@ __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) 
     const bool real = base + threadIdx.x / lanes < a.rows;
     const int64_t first = again((int)lane_column<SPLIT>(lane));
     const void* weight = again(a.weight);
-    auto load = [&](int64_t col, auto cover, float (&t)[8], bool again) {
-      constexpr Cover C = decltype(cover)::value;
-      if (again && a.total.p) return load_cols<X, SPLIT, C>(row_of<X>(a.total, row), col, a.cols, gap, t);
-      load_cols<X, SPLIT, C>(row_of<X>(a.x, row), col, a.cols, gap, t);
-      if (a.residual.p) {
-        float r[8];
-        load_cols<X, SPLIT, C>(row_of<X>(a.residual, row), col, a.cols, gap, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = round_to(X{}, t[i] + r[i]);
-      }
-    };
-    auto finish = [&](int64_t col, auto cover, const float (&t)[8], float r) {
+    auto finish = [&](int64_t col, auto cover, const float (&t)[8], const RawWeight& raw, float r) {
       constexpr Cover C = decltype(cover)::value;
       float w[8], y[8];
-      load_cols<SPLIT, C>(a.weight_dtype, weight, col, a.cols, gap, w);
+      widen<C>(a.weight_dtype, raw, col, a.cols, gap, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) y[i] = t[i] * r * w[i];
       if constexpr (BLOCKS) {
@@ -111,29 +143,62 @@ __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) 
     };
     auto go = [&](auto cover) {
       constexpr Cover C = decltype(cover)::value;
+      const bool residual = a.residual.p != nullptr;
+      const char* x_row = row_of<X>(a.x, row);
+      const char* res_row = residual ? row_of<X>(a.residual, row) : x_row;
       float t[V][8], sum[1] = {0.0f};
-      auto take = [&](int64_t col, float (&t)[8]) {
-        if (a.total.p && real) store_cols<X, SPLIT, C>(row_of<X>(a.total, row), col, a.cols, gap, t);
-        float eight = 0.0f;  // added up apart, so that long rows' sums have an eighth of the terms
+      RawWeight w[V];
+      auto at = [&](int64_t u) { return first + u * 8 * lanes; };
+      // V vectors from column `at(u)`: t, its part of the sum, the total where that is wanted
+      auto take = [&](int64_t u0) {
+        Raw<X> x[V], r[V];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) eight = fmaf(t[i], t[i], eight);
-        sum[0] += eight;
+        for (int u = 0; u < V; ++u) x[u] = load_raw<X, SPLIT, C, true>(x_row, at(u0 + u), a.cols, gap);
+        if (residual) {
+#pragma unroll
+          for (int u = 0; u < V; ++u) r[u] = load_raw<X, SPLIT, C, true>(res_row, at(u0 + u), a.cols, gap);
+        }
+        if constexpr (U > 0) {
+#pragma unroll
+          for (int u = 0; u < V; ++u) w[u] = load_raw<SPLIT, C>(a.weight_dtype, weight, at(u), a.cols, gap);
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+          widen<X, C>(x[u], at(u0 + u), a.cols, gap, t[u]);
+          if (residual) {
+            float v[8];
+            widen<X, C>(r[u], at(u0 + u), a.cols, gap, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[u][i] = round_to(X{}, t[u][i] + v[i]);
+            if (a.total.p && real) store_cols<X, SPLIT, C, true>(row_of<X>(a.total, row), at(u0 + u), a.cols, gap, t[u]);
+          }
+          float eight = 0.0f;  // added up apart, so that long rows' sums have an eighth of the terms
+#pragma unroll
+          for (int i = 0; i < 8; ++i) eight = fmaf(t[u][i], t[u][i], eight);
+          sum[0] += eight;
+        }
       };
-      if constexpr (U > 0) {
-#pragma unroll
-        for (int u = 0; u < V; ++u) load(first + u * 8 * lanes, cover, t[u], false);
-#pragma unroll
-        for (int u = 0; u < V; ++u) take(first + u * 8 * lanes, t[u]);
-      } else {
-        for (int64_t u = 0; u < turns; ++u) load(first + u * 8 * lanes, cover, t[0], false), take(first + u * 8 * lanes, t[0]);
-      }
+      if constexpr (U > 0) take(0);
+      else
+        for (int64_t u = 0; u < turns; ++u) take(u);
       sum_of_row(sum, lanes, part[turn]);
       const float r = rsqrtf(sum[0] / (float)a.cols + a.eps);
       if constexpr (U > 0) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) finish(first + u * 8 * lanes, cover, t[u], r);
+        for (int u = 0; u < V; ++u) finish(at(u), cover, t[u], w[u], r);
       } else {
-        for (int64_t u = 0; u < turns; ++u) load(first + u * 8 * lanes, cover, t[0], true), finish(first + u * 8 * lanes, cover, t[0], r);
+        for (int64_t u = 0; u < turns; ++u) {  // again, out of the total where there is one
+          const bool total = a.total.p != nullptr;
+          const Raw<X> x = load_raw<X, SPLIT, C>(total ? (const char*)row_of<X>(a.total, row) : x_row, at(u), a.cols, gap);
+          widen<X, C>(x, at(u), a.cols, gap, t[0]);
+          if (residual && !total) {
+            float v[8];
+            widen<X, C>(load_raw<X, SPLIT, C>(res_row, at(u), a.cols, gap), at(u), a.cols, gap, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[0][i] = round_to(X{}, t[0][i] + v[i]);
+          }
+          finish(at(u), cover, t[0], load_raw<SPLIT, C>(a.weight_dtype, weight, at(u), a.cols, gap), r);
+        }
       }
     };
     if (a.cols == (U ? U : turns) * 8 * lanes) go(CoverOf<kWhole>{});
@@ -144,13 +209,16 @@ __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) 
 
 // ---- gradients
 
+// A row's loads are all on their way before its sums, and, where the registers suffice (up to 16 columns a lane), the next
+// row's before this row's results; the weight stays in registers then too.  Wider lanes load it, and the total's gradient, where
+// they use them.
 template <typename X, typename G, int U>
-__global__ __launch_bounds__(U == 4 ? kNormGradMost : kNormThreads, U == 1 ? 4 : U == 2 ? 3 : 2) void norm_grad_kernel(NormGradArgs a, int lanes, float* sums, int64_t pitch) {
-  constexpr bool SPLIT = Split<X, G>::value;
+__global__ __launch_bounds__(U == 1 ? kNormThreads : kNormGradMost) void norm_grad_kernel(NormGradArgs a, int lanes, float* sums, int64_t pitch) {
+  constexpr bool SPLIT = Split<X, G>::value, AHEAD = X::kBytes + G::kBytes == 4 && U <= 2, KEEP = U <= 2;
   __shared__ float part[2][2 * kNormGradMost / 64];
   __shared__ float joined[U == 1 ? 8 * kNormThreads : 1];
   const int lane = threadIdx.x % lanes, side = blockDim.x / lanes;
-  const int64_t gap = lane_gap<SPLIT>(lanes);
+  const int64_t gap = lane_gap<SPLIT>(lanes), step = (int64_t)gridDim.x * side;
   float dw[U][8];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -158,45 +226,67 @@ __global__ __launch_bounds__(U == 4 ? kNormGradMost : kNormThreads, U == 1 ? 4 :
     for (int i = 0; i < 8; ++i) dw[u][i] = 0.0f;
   auto all = [&](auto cover) {
     constexpr Cover C = decltype(cover)::value;
-    int turn = 0;
-    for (int64_t base = (int64_t)blockIdx.x * side; base < a.rows; base += (int64_t)gridDim.x * side, turn ^= 1) {
+    auto at = [&](int u) { return lane_column<SPLIT>(lane) + u * 8 * lanes; };
+    RawWeight weight[U];
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), a.cols, gap);
+    }
+    Raw<X> x_raw[U];
+    Raw<G> g_raw[U];
+    auto fetch = [&](int64_t base) {
       const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
-      const bool real = base + threadIdx.x / lanes < a.rows;
-      const int64_t first = again((int)lane_column<SPLIT>(lane));
-      const void* weight = again(a.weight);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        x_raw[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), a.cols, gap);
+        g_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.g, row), at(u), a.cols, gap);
+      }
+    };
+    int turn = 0;
+    int64_t base = (int64_t)blockIdx.x * side;
+    if (base < a.rows) fetch(base);
+    for (; base < a.rows; base += step, turn ^= 1) {
+      const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
+      const bool real = base + threadIdx.x / lanes < a.rows, more = a.total_grad.p != nullptr;
+      Raw<G> t_raw[U];
+      if (KEEP && more) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), a.cols, gap);
+      }
       float x[U][8], g[U][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        load_cols<X, SPLIT, C>(row_of<X>(a.x, row), first + u * 8 * lanes, a.cols, gap, x[u]);
-        load_cols<G, SPLIT, C>(row_of<G>(a.g, row), first + u * 8 * lanes, a.cols, gap, g[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
         float w[8];
-        load_cols<SPLIT, C>(a.weight_dtype, weight, first + u * 8 * lanes, a.cols, gap, w);
+        widen<X, C>(x_raw[u], at(u), a.cols, gap, x[u]);
+        widen<G, C>(g_raw[u], at(u), a.cols, gap, g[u]);
+        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), a.cols, gap);
+        widen<C>(a.weight_dtype, weight[u], at(u), a.cols, gap, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] = fmaf(x[u][i], x[u][i], s[0]), s[1] = fmaf(g[u][i] * w[i], x[u][i], s[1]);
       }
+      if (AHEAD && base + step < a.rows) fetch(base + step);
       sum_of_row(s, lanes, part[turn]);
       const float n = (float)a.cols, r = rsqrtf(s[0] / n + a.eps), k = r * r * (s[1] / n);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int64_t col = first + u * 8 * lanes;
         float w[8], d[8];
-        load_cols<SPLIT, C>(a.weight_dtype, weight, col, a.cols, gap, w);
+        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), a.cols, gap);
+        widen<C>(a.weight_dtype, weight[u], at(u), a.cols, gap, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           d[i] = r * (g[u][i] * w[i] - x[u][i] * k);
           dw[u][i] += real ? g[u][i] * (x[u][i] * r) : 0.0f;
         }
-        if (a.total_grad.p) {
+        if (more) {
+          if (!KEEP) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), a.cols, gap);
           float t[8];
-          load_cols<G, SPLIT, C>(row_of<G>(a.total_grad, row), col, a.cols, gap, t);
+          widen<G, C>(t_raw[u], at(u), a.cols, gap, t);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
-        if (real) store_cols<G, SPLIT, C>(row_of<G>(a.out, row), col, a.cols, gap, d);
+        if (real) store_cols<G, SPLIT, C, true>(row_of<G>(a.out, row), at(u), a.cols, gap, d);
       }
+      if (!AHEAD && base + step < a.rows) fetch(base + step);
     }
   };
   if (a.cols == U * 8 * lanes) all(CoverOf<kWhole>{});
@@ -237,9 +327,12 @@ __global__ __launch_bounds__(kNormThreads) void norm_sums_kernel(NormGradArgs a,
       float x[8], g[8], w[8];
       auto take = [&](auto cover) {
         constexpr Cover C = decltype(cover)::value;
-        load_cols<X, SPLIT, C>(row_of<X>(a.x, row), col, a.cols, gap, x);
-        load_cols<G, SPLIT, C>(row_of<G>(a.g, row), col, a.cols, gap, g);
-        load_cols<SPLIT, C>(a.weight_dtype, a.weight, col, a.cols, gap, w);
+        const Raw<X> x_raw = load_raw<X, SPLIT, C>(row_of<X>(a.x, row), col, a.cols, gap);
+        const Raw<G> g_raw = load_raw<G, SPLIT, C>(row_of<G>(a.g, row), col, a.cols, gap);
+        const RawWeight w_raw = load_raw<SPLIT, C>(a.weight_dtype, a.weight, col, a.cols, gap);
+        widen<X, C>(x_raw, col, a.cols, gap, x);
+        widen<G, C>(g_raw, col, a.cols, gap, g);
+        widen<C>(a.weight_dtype, w_raw, col, a.cols, gap, w);
       };
       if (c + 8 * kNormThreads <= a.cols) take(CoverOf<kWhole>{});
       else take(CoverOf<kEnd>{});
@@ -263,11 +356,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_strip_kernel(NormGradArgs a
   float w[8], dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   auto all = [&](auto cover) {
     constexpr Cover C = decltype(cover)::value;
-    load_cols<SPLIT, C>(a.weight_dtype, a.weight, col, a.cols, gap, w);
+    widen<C>(a.weight_dtype, load_raw<SPLIT, C>(a.weight_dtype, a.weight, col, a.cols, gap), col, a.cols, gap, w);
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
       float x[8], g[8], d[8];
-      load_cols<X, SPLIT, C>(row_of<X>(a.x, row), col, a.cols, gap, x);
-      load_cols<G, SPLIT, C>(row_of<G>(a.g, row), col, a.cols, gap, g);
+      const Raw<X> x_raw = load_raw<X, SPLIT, C>(row_of<X>(a.x, row), col, a.cols, gap);
+      const Raw<G> g_raw = load_raw<G, SPLIT, C>(row_of<G>(a.g, row), col, a.cols, gap);
+      widen<X, C>(x_raw, col, a.cols, gap, x);
+      widen<G, C>(g_raw, col, a.cols, gap, g);
       const v2f rk = rows[row];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -276,7 +371,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_strip_kernel(NormGradArgs a
       }
       if (a.total_grad.p) {
         float t[8];
-        load_cols<G, SPLIT, C>(row_of<G>(a.total_grad, row), col, a.cols, gap, t);
+        widen<G, C>(load_raw<G, SPLIT, C>(row_of<G>(a.total_grad, row), col, a.cols, gap), col, a.cols, gap, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] += t[i];
       }
@@ -314,10 +409,7 @@ __global__ __launch_bounds__(256) void norm_zero_kernel(float* out, int64_t cols
 template <typename X, typename O>
 hipError_t run_norm(const NormArgs& a, hipStream_t stream) {
   const NormPlan p = norm_plan(a.rows, a.cols, O::kBytes == 1);
-  const auto kernel = p.vectors == 1   ? norm_kernel<X, O, 1>
-                      : p.vectors == 2 ? norm_kernel<X, O, 2>
-                      : p.vectors == 4 ? norm_kernel<X, O, 4>
-                                       : norm_kernel<X, O, 0>;
+  const auto kernel = p.vectors == 1 ? norm_kernel<X, O, 1> : p.vectors == 2 ? norm_kernel<X, O, 2> : norm_kernel<X, O, 0>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)p.wgs), dim3(std::max(kNormThreads, p.lanes)), 0, stream, a, p.lanes);
   return hipGetLastError();
 }
