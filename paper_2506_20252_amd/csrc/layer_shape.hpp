@@ -64,17 +64,24 @@ inline NormGradPlan norm_grad_plan(int64_t rows, int64_t cols) {
 
 // ---- products of 8-bit with 4-bit blocks ------------------------------------------------------------------------
 
-// Tiles of m tokens by n rows of the weight: 256 (256 x 256), 128 (128 x 128) or 64 (64 tokens x 128 rows).  The largest that
-// gives more than half of the 256 CUs one.
+// Tiles of m tokens by n rows of the weight: 256 (256 x 256), 128 (128 x 128), 64 (64 tokens by 128 rows), or 32 (64 x 64, in two
+// parts of the terms).
+//
+// The largest of the first two that gives more than half of the 256 CUs one; else 64 x 64 as long as each CU has at most one.
+// us with 64 x 64, 64 x 128, 128 x 128: 9.1, 11.1, 14.8 (64 tokens, 4096 rows and terms: 64, 32, 32 tiles), 13.4, 16.8, 20.5 (256 tokens: 256,
+// 128, 64), 21.6, 20.2, 21.9 (512: 512, 256, 128), 10.1, 7.1, 8.1 (1001 tokens, 2000 rows, 1333 terms: 512, 256, 128).
+inline int64_t layer_tiles(int64_t m, int64_t n, int rows_x, int rows_w) { return (int64_t)(ceil_div(m, rows_x) * ceil_div(n, rows_w)); }
 inline int layer_tile(int64_t m, int64_t n) {
-  auto tiles = [&](int rows_x, int rows_w) { return (int64_t)(ceil_div(m, rows_x) * ceil_div(n, rows_w)); };
-  return tiles(256, 256) > 128 ? 256 : tiles(128, 128) > 128 ? 128 : 64;
+  if (layer_tiles(m, n, 256, 256) > 128) return 256;
+  if (layer_tiles(m, n, 128, 128) > 128) return 128;
+  return layer_tiles(m, n, 64, 64) > 256 ? 64 : 32;
 }
 
-// few_kernel: tokens and columns of the output of a workgroup, in sixteens (a gated column is two rows of the weight), and
-// the tokens that go into one launch of fewer than 2^22 workgroups.
-constexpr int kFewMost = 48;
-inline int few_tokens_sixteens(int64_t m) { return m <= 16 ? 1 : m <= 32 ? 2 : 3; }
+// few_kernel: up to so many tokens.  us, and by tiles: 7.8 and 8.5, gated 12.5 and 11.8 (32 tokens, 4096 columns and terms), 10.3 and
+// 11.4, 14.9 and 14.7 (33, 8192, 4096), 18.1 and 19.6, 25.3 and 22.3 (48, 4096, 8192), gated 11.0 and 10.8 (17, 4096, 4096).
+constexpr int kFewLinear = 48, kFewGated = 32;
+// Its columns of the output, in sixteens (two where gated, each two rows of the weight): as many as leave a workgroup for each of
+// the 256 CUs, since every workgroup reads the tokens.  And the tokens that go into one launch of fewer than 2^22 workgroups.
 inline int few_columns_sixteens(int64_t n) { return n <= 16 * 256 ? 1 : n <= 32 * 256 ? 2 : 4; }
 inline int64_t few_band(int64_t m, int64_t tiles_n, int64_t tokens) {
   return std::min(m, std::max<int64_t>(1, (((int64_t)1 << 22) - 1) / tiles_n) * tokens);

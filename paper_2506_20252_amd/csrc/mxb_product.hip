@@ -145,6 +145,45 @@ __device__ __forceinline__ void store_block(const float (&f)[16], int64_t i, int
   if (half == 0) stg<false>((char*)to.scales + i * groups * 4 + j / 32, (uint8_t)s);
 }
 
+// What a wave leaves of its FN x FM blocks: tokens i ... and columns j ... of the output.
+template <int FN, int FM, bool GATED, typename O, bool NT>
+__device__ __forceinline__ void leave(const v16f (&acc)[FN][FM], float* part, int64_t i, int64_t j, int64_t m, int64_t n, const Epilogue& ep) {
+  static_assert(FN % 2 == 0, "");
+  const int lane = threadIdx.x % 64;
+#pragma unroll
+  for (int b = 0; b < FM; ++b, i += 32) {
+    if constexpr (!GATED) {
+#pragma unroll
+      for (int a = 0; a < FN; a += 2) {
+        float v[2][16];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[y][e] = acc[a + y][b][e];
+        store_turned<2, O, NT>(v, part, i, j + 32 * a, m, n, ep.residual, ep.out);
+      }
+    } else {
+      constexpr int H = FN / 2;
+      float v[H][16];
+#pragma unroll
+      for (int a = 0; a < H; ++a) {
+        float va[16], vb[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          va[e] = acc[a][b][e], vb[e] = acc[H + a][b][e];
+          v[a][e] = activate(ep.act, va[e]) * vb[e];
+        }
+        if (ep.saved_a.codes) {
+          store_block(va, i + lane % 32, j + 32 * a, m, n, ep.saved_a);
+          store_block(vb, i + lane % 32, j + 32 * a, m, n, ep.saved_b);
+        }
+        if constexpr (O::kBytes == 1) store_block(v[a], i + lane % 32, j + 32 * a, m, n, ep.blocks);
+      }
+      if constexpr (O::kBytes > 1) store_turned<H, O, NT>(v, part, i, j, m, n, {nullptr, 0}, ep.out);
+    }
+  }
+}
+
 template <int FN, int FM, int WN, int WM, bool GATED, typename O>
 __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w, int64_t m, int64_t n, int groups, int64_t tiles_n,
                                                                Epilogue ep) {
@@ -292,61 +331,217 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
   __syncthreads();
   static_assert(sizeof(Pair) >= W / 2 * turn_floats(2) * 4, "");
   float* part = (wave < W / 2 ? (float*)&pair0 : (float*)&pair1) + wave % (W / 2) * turn_floats(2);
-  constexpr bool NONTEMPORAL = N * M >= 256 * 256;
-#pragma unroll
-  for (int b = 0; b < FM; ++b) {
-    const int64_t i = i0 + wave_m + 32 * b;
-    if constexpr (!GATED) {
-      static_assert(FN % 2 == 0, "");
-#pragma unroll
-      for (int a = 0; a < FN; a += 2) {
-        float v[2][16];
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) v[y][e] = acc[a + y][b][e];
-        store_turned<2, O, NONTEMPORAL>(v, part, i, j0 + wave_n + 32 * a, m, n, ep.residual, ep.out);
-      }
-    } else {
-      constexpr int H = FN / 2;
-      const int64_t j = j0 + wave_n / 2;
-      float v[H][16];
-#pragma unroll
-      for (int a = 0; a < H; ++a) {
-        float va[16], vb[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          va[e] = acc[a][b][e], vb[e] = acc[H + a][b][e];
-          v[a][e] = activate(ep.act, va[e]) * vb[e];
-        }
-        if (ep.saved_a.codes) {
-          store_block(va, i + lane % 32, j + 32 * a, m, n, ep.saved_a);
-          store_block(vb, i + lane % 32, j + 32 * a, m, n, ep.saved_b);
-        }
-        if constexpr (O::kBytes == 1) store_block(v[a], i + lane % 32, j + 32 * a, m, n, ep.blocks);
-      }
-      if constexpr (O::kBytes > 1) store_turned<H, O, NONTEMPORAL>(v, part, i, j, m, n, {nullptr, 0}, ep.out);
-    }
-  }
+  leave<FN, FM, GATED, O, (N * M >= 256 * 256)>(acc, part, i0 + wave_m, j0 + (GATED ? wave_n / 2 : wave_n), m, n, ep);
 }
 
-template <int FN, int FM, int WN, int WM, bool GATED, typename O>
-hipError_t run_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  typedef Tile<FN, FM, WN, WM> S;
+// ---- small tiles -------------------------------------------------------------------------------------------------
+//
+// Where a tile is small its steps are latencies one after the other.  PARTS groups of WN x WM waves in a workgroup take a part of
+// the terms each, in LDS of their own, and their sums are added in order at the end; D steps are in LDS or on their way
+// at once.  The weight's rows come as half lines then, 64 bytes a step, at place piece ^ (row / 4 mod 4) of a row's four (a
+// row is a quarter of the banks).  Every wave has the same number of loads a step, and waits for those of the next step alone.
+template <int FN, int FM, int WN, int WM>
+struct Stage {
+  static constexpr int kWaves = WN * WM, N = 32 * FN * WN, M = 32 * FM * WM;
+  uint8_t w[N * 64], x[M * 128];
+  uint8_t scales[N * 4 + M * 4];  // the weight's, the tokens'
+};
+
+// Waits until at most LATER of this wave's loads are on their way and all its reads of LDS are done, then for the other waves.
+template <int LATER>
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+}
+
+// Loads of 16 bytes a lane from base + at, and of 4 bytes from p, into LDS, lane after lane from `to` on.  Written out: the
+// compiler's own ones make it wait for all of them before LDS is read, in every turn of the loop.
+__device__ __forceinline__ uint32_t lds_place(const uint8_t* to) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to);
+}
+__device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t at, const uint8_t* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(const uint8_t* p, const uint8_t* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_place(to)), "v"(p) : "memory");
+}
+
+template <int FN, int FM, int WN, int WM, int PARTS, int D, bool GATED, typename O>
+__global__ __launch_bounds__(64 * WN * WM * PARTS, WN * WM * PARTS == 8 ? 2 : 1) void deep_kernel(MxbMat x, MxMat w, int64_t m, int64_t n, int groups, int64_t tiles_n,
+                                                            Epilogue ep) {
+  typedef Stage<FN, FM, WN, WM> S;
+  constexpr int N = S::N, M = S::M, W = S::kWaves, COLS = GATED ? N / 2 : N;
+  __shared__ __attribute__((aligned(16))) S all_lds[PARTS][D];
+  TilePlace place;
+  if (!tile_place((m + M - 1) / M, tiles_n, &place)) return;
+  const int64_t i0 = place.i * M, j0 = place.j * COLS;
+  const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64 % W);
+  const int part = __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * W));
+  S* lds = all_lds[part];
+  const uint32_t w_pitch = groups * 64, x_pitch = groups * 128, s_pitch = groups * 4;
+
+  // Rows as tile_kernel has them.
+  const int64_t jb = min(j0, n - 1);
+  const int rows_w = (int)min((int64_t)COLS, n - jb), rows_x = (int)min((int64_t)M, m - i0);
+  auto column = [&](int row) { return GATED ? row / (32 * FN) * (16 * FN) + row / 32 % (FN / 2) * 32 + row % 32 : row; };
+  auto second = [&](int row) { return GATED && row / 32 % FN >= FN / 2; };
+  constexpr int LOADS_W = N / 16 / W, LOADS_X = M / 8 / W;  // of codes, 16 and 8 rows each, a wave
+  static_assert(LOADS_W * 16 * W == N && LOADS_X * 8 * W == M && W % 2 == 0, "");
+  uint32_t at_w[LOADS_W], at_x[LOADS_X];  // of this lane's piece, in the rows' codes
+  const int piece = (lane ^ (wave * 8 + lane / 8) / 2) % 8, piece_w = (lane ^ lane / 16) % 4;
+#pragma unroll
+  for (int u = 0; u < LOADS_W; ++u) at_w[u] = (uint32_t)min(column((u * W + wave) * 16 + lane / 4), rows_w - 1) * w_pitch + piece_w * 16;
+#pragma unroll
+  for (int u = 0; u < LOADS_X; ++u) at_x[u] = (uint32_t)min((u * W + wave) * 8 + lane / 8, rows_x - 1) * x_pitch + piece * 16;
+  // a wave loads the scales of 64 rows of either side, or those of others again
+  const int s_wave = wave % (N / 64 + M / 64);
+  const bool s_of_w = s_wave < N / 64;
+  const int s_row = (s_of_w ? s_wave : s_wave - N / 64) * 64 + lane;
+  static_assert(N / 64 + M / 64 <= W, "");
+  const uint8_t *codes_w = w.codes + jb * w_pitch, *codes_x = x.codes + i0 * x_pitch;
+  const uint8_t* scales = s_of_w ? w.scales + (jb + (second(s_row) ? n : 0) + min(column(s_row), rows_w - 1)) * s_pitch
+                                 : x.scales + (i0 + min(s_row, rows_x - 1)) * s_pitch;
+
+  auto fetch = [&](S& l, int g) {
+    load_to_lds4(scales + (int64_t)g * 4, l.scales + s_wave * 256);
+#pragma unroll
+    for (int u = 0; u < LOADS_W; ++u)
+      load_to_lds16(codes_w + (int64_t)g * 64 + (second((u * W + wave) * 16) ? n * w_pitch : 0), at_w[u], l.w + (u * W + wave) * 1024);
+#pragma unroll
+    for (int u = 0; u < LOADS_X; ++u) load_to_lds16(codes_x + (int64_t)g * 128, at_x[u], l.x + (u * W + wave) * 1024);
+  };
+  constexpr int LOADS = 1 + LOADS_W + LOADS_X;
+
+  const int half = lane / 32, wave_n = wave / WM * 32 * FN, wave_m = wave % WM * 32 * FM;
+  const int row_w = wave_n + lane % 32, row_x = wave_m + lane % 32;
+  v16f acc[FN][FM];
+#pragma unroll
+  for (int a = 0; a < FN; ++a)
+#pragma unroll
+    for (int b = 0; b < FM; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[a][b][e] = 0.0f;
+
+  struct Blocks {
+    v4i w[FN], x[FM][2];
+  };
+  struct Scales {
+    int w[FN], x[FM];
+  };
+  auto read_scales = [&](const S& l, Scales& s) {
+#pragma unroll
+    for (int a = 0; a < FN; ++a) s.w[a] = *(const uint16_t*)(l.scales + (row_w + 32 * a) * 4 + 2 * half);
+#pragma unroll
+    for (int b = 0; b < FM; ++b) s.x[b] = *(const uint16_t*)(l.scales + (N + row_x + 32 * b) * 4 + 2 * half);
+  };
+  auto read = [&](const S& l, int j, Blocks& c) {
+    auto at = [&](int piece) { return (piece ^ (lane >> 1 & 7)) * 16; };
+#pragma unroll
+    for (int a = 0; a < FN; ++a) c.w[a] = *(const v4i*)(l.w + (row_w + 32 * a) * 64 + ((2 * half + j) ^ (lane >> 2 & 3)) * 16);
+#pragma unroll
+    for (int b = 0; b < FM; ++b) {
+      c.x[b][0] = *(const v4i*)(l.x + (row_x + 32 * b) * 128 + at(2 * j + half));
+      c.x[b][1] = *(const v4i*)(l.x + (row_x + 32 * b) * 128 + at(4 + 2 * j + half));
+    }
+  };
+  auto multiply = [&](const Blocks& c, const Scales& s, auto which) {
+    constexpr int J = decltype(which)::value;
+#pragma unroll
+    for (int a = 0; a < FN; ++a)
+#pragma unroll
+      for (int b = 0; b < FM; ++b)
+        acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(c.w[a]), frag(c.x[b][0], c.x[b][1]), acc[a][b], 4, 0, J, s.w[a],
+                                                                   J, s.x[b]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // This part's steps; all parts go through as many turns as the longest has.
+  const int begin = (int)((int64_t)groups * part / PARTS), count = (int)((int64_t)groups * (part + 1) / PARTS) - begin;
+  const int most = (groups + PARTS - 1) / PARTS, last = groups - 1;
+  Blocks c0, c1;
+  Scales s, next_s;
+  // Step g out of `l`, its first instructions' blocks in c0 and its scales in s; beyond the last step it is fetched again.
+  auto step = [&](S& l, const S& next, int g, bool mine) {
+    read(l, 1, c1);
+    if (mine) multiply(c0, s, Int<0>{});
+    meet<(D - 2) * LOADS>();
+    read_scales(next, next_s);
+    read(next, 0, c0);
+    fetch(l, min(begin + g + D, last));
+    if (mine) multiply(c1, s, Int<1>{});
+    s = next_s;
+  };
+#pragma unroll
+  for (int d = 0; d < D; ++d) fetch(lds[d], min(begin + d, last));
+  meet<(D - 1) * LOADS>();
+  read_scales(lds[0], s);
+  read(lds[0], 0, c0);
+  int g = 0;
+  for (; g + D <= groups / PARTS; g += D) {
+#pragma unroll
+    for (int d = 0; d < D; ++d) step(lds[d], lds[(d + 1) % D], g + d, true);
+  }
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (g + d < most) step(lds[d], lds[(d + 1) % D], g + d, g + d < count);
+
+  // Results leave through LDS, whose last loads have to have come first.
+  meet<0>();
+  float* room = (float*)all_lds;
+  if constexpr (PARTS > 1) {
+    constexpr int SIZE = FN * FM * 16 * 64;  // floats of a wave's sums
+    static_assert(sizeof(all_lds) >= (PARTS - 1) * W * SIZE * 4, "");
+    auto sums = [&](int p, int a, int b, int e) -> v4f& { return *(v4f*)(room + ((p - 1) * W + wave) * SIZE + (((a * FM + b) * 4 + e) * 64 + lane) * 4); };
+    if (part) {
+#pragma unroll
+      for (int a = 0; a < FN; ++a)
+#pragma unroll
+        for (int b = 0; b < FM; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sums(part, a, b, e) = v4f{acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2], acc[a][b][4 * e + 3]};
+    }
+    __syncthreads();
+    if (part) {
+      __syncthreads();
+      return;
+    }
+#pragma unroll
+    for (int p = 1; p < PARTS; ++p)
+#pragma unroll
+      for (int a = 0; a < FN; ++a)
+#pragma unroll
+        for (int b = 0; b < FM; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const v4f v = sums(p, a, b, e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[a][b][4 * e + i] += v[i];
+          }
+    __syncthreads();  // nobody reads the sums any more
+  }
+  static_assert(sizeof(all_lds) >= W * turn_floats(2) * 4, "");
+  leave<FN, FM, GATED, O, false>(acc, room + wave * turn_floats(2), i0 + wave_m, j0 + (GATED ? wave_n / 2 : wave_n), m, n, ep);
+}
+
+typedef void (*Product)(MxbMat, MxMat, int64_t, int64_t, int, int64_t, Epilogue);
+
+// `kernel` has tiles of M tokens by N rows of the weight, a workgroup of `threads` each.
+template <bool GATED, typename O>
+hipError_t run_tiles(Product kernel, int M, int N, int threads, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e,
+                     hipStream_t stream) {
   const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);
-  const int64_t tiles_n = (int64_t)ceil_div(blocks ? groups_of(n) * 128 : n, GATED ? S::N / 2 : S::N);
-  const int64_t wgs = (int64_t)ceil_div(ceil_div(m, S::M) * tiles_n, 8) * 8;
-  hipLaunchKernelGGL((tile_kernel<FN, FM, WN, WM, GATED, O>), dim3((unsigned)wgs), dim3(64 * WN * WM), 0, stream, x, w, m, n,
-                     (int)groups_of(k), tiles_n, e);
+  const int64_t tiles_n = (int64_t)ceil_div(blocks ? groups_of(n) * 128 : n, GATED ? N / 2 : N);
+  const int64_t wgs = (int64_t)ceil_div(ceil_div(m, M) * tiles_n, 8) * 8;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, stream, x, w, m, n, (int)groups_of(k), tiles_n, e);
   return hipGetLastError();
 }
 
 template <bool GATED, typename O>
 hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
   switch (layer_tile(m, GATED ? 2 * n : n)) {
-    case 256: return run_tile<4, 2, 2, 4, GATED, O>(x, w, m, n, k, e, stream);
-    case 128: return run_tile<2, 2, 2, 2, GATED, O>(x, w, m, n, k, e, stream);
-    default: return run_tile<2, 1, 2, 2, GATED, O>(x, w, m, n, k, e, stream);
+    case 256: return run_tiles<GATED, O>(tile_kernel<4, 2, 2, 4, GATED, O>, 256, 256, 512, x, w, m, n, k, e, stream);
+    case 128: return run_tiles<GATED, O>(tile_kernel<2, 2, 2, 2, GATED, O>, 128, 128, 256, x, w, m, n, k, e, stream);
+    case 64: return run_tiles<GATED, O>(deep_kernel<2, 1, 2, 2, 1, 3, GATED, O>, 64, 128, 256, x, w, m, n, k, e, stream);
+    default: return run_tiles<GATED, O>(deep_kernel<2, 1, 1, 2, 2, 3, GATED, O>, 64, 64, 256, x, w, m, n, k, e, stream);
   }
 }
 
@@ -494,7 +689,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
 
 template <int MT, int H, bool GATED, typename O>
 hipError_t run_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, Epilogue e, hipStream_t stream) {
-  const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);
+  const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);  // filled up to 128 columns
   const int64_t groups = groups_of(k), out_groups = groups_of(n);
   const int64_t tiles_n = (int64_t)ceil_div(blocks ? out_groups * 128 : n, 16 * H);
   const int64_t band = few_band(m, tiles_n, 16 * MT);
@@ -513,34 +708,35 @@ hipError_t run_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, Epilogue 
 
 template <int MT, typename O>
 hipError_t pick_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  if (e.gated) return run_few<MT, 2, true, O>(x, w, m, n, k, e, stream);
-  if constexpr (O::kBytes == 1) return hipErrorInvalidValue;
-  else
-    switch (few_columns_sixteens(n)) {
-      case 1: return run_few<MT, 1, false, O>(x, w, m, n, k, e, stream);
-      case 2: return run_few<MT, 2, false, O>(x, w, m, n, k, e, stream);
-      default: return run_few<MT, 4, false, O>(x, w, m, n, k, e, stream);
-    }
+  switch (few_columns_sixteens(n)) {
+    case 1: return run_few<MT, 1, false, O>(x, w, m, n, k, e, stream);
+    case 2: return run_few<MT, 2, false, O>(x, w, m, n, k, e, stream);
+    default: return run_few<MT, 4, false, O>(x, w, m, n, k, e, stream);
+  }
 }
 
 template <typename O>
-hipError_t pick(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  if (m > kFewMost && k > 0) {
-    if (e.gated) return pick_tile<true, O>(x, w, m, n, k, e, stream);
-    if constexpr (O::kBytes > 1) return pick_tile<false, O>(x, w, m, n, k, e, stream);
-  }
-  switch (few_tokens_sixteens(m)) {
-    case 1: return pick_few<1, O>(x, w, m, n, k, e, stream);
-    case 2: return pick_few<2, O>(x, w, m, n, k, e, stream);
-    default: return pick_few<3, O>(x, w, m, n, k, e, stream);
-  }
+hipError_t linear(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  if (m > kFewLinear && k > 0) return pick_tile<false, O>(x, w, m, n, k, e, stream);
+  if (m <= 16) return pick_few<1, O>(x, w, m, n, k, e, stream);
+  if (m <= 32) return pick_few<2, O>(x, w, m, n, k, e, stream);
+  return pick_few<3, O>(x, w, m, n, k, e, stream);
+}
+
+template <typename O>
+hipError_t gated(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  if (m > kFewGated && k > 0) return pick_tile<true, O>(x, w, m, n, k, e, stream);
+  if (m <= 16) return run_few<1, 2, true, O>(x, w, m, n, k, e, stream);
+  return run_few<2, 2, true, O>(x, w, m, n, k, e, stream);
 }
 
 }  // namespace
 
 hipError_t launch_mxb_product(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  if (e.gated && !e.out.p) return pick<Q8>(x, w, m, n, k, e, stream);
-  return e.dtype == Elem::f32 ? pick<F32>(x, w, m, n, k, e, stream) : pick<B16>(x, w, m, n, k, e, stream);
+  const bool f32 = e.dtype == Elem::f32;
+  if (!e.gated) return f32 ? linear<F32>(x, w, m, n, k, e, stream) : linear<B16>(x, w, m, n, k, e, stream);
+  if (!e.out.p) return gated<Q8>(x, w, m, n, k, e, stream);
+  return f32 ? gated<F32>(x, w, m, n, k, e, stream) : gated<B16>(x, w, m, n, k, e, stream);
 }
 
 }  // namespace pat

@@ -110,6 +110,21 @@ def test_oracle_gradients_against_differences():
         assert np.allclose(d[:, 50:], dy * (L.gated(a, b + h, name) - L.gated(a, b - h, name)) / (2 * h), atol=1e-8)
 
 
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir("/opt/rocm/include/hip"),
+                    reason="no g++ or no HIP headers")
+def test_host_side_under_asan_ubsan(tmp_path):
+    """How sizes are cut into workgroups, what the entry points take and hand on."""
+    exe = tmp_path / "layer_check"
+    csrc = os.path.join(ROOT, "paper_2506_20252_amd", "csrc")
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", csrc, os.path.join(csrc, "layer.cpp"),
+           os.path.join(ROOT, "tests", "host", "layer_check.cpp"), "-o", str(exe)]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, (res.stdout[-2000:], res.stderr[-2000:])
+    assert " 0 failures" in res.stdout
+
+
 @pytest.mark.parametrize("source", ["mxb.hip", "mxb_product.hip", "gated.hip", "norm.hip"])
 def test_kernels_as_compiled(source, tmp_path):
     """No scratch memory, no packed fp32; a workgroup of eight waves leaves two waves a SIMD their registers."""
