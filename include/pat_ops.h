@@ -177,8 +177,8 @@ pat_status_t pat_dropout(const void* x, int64_t x_stride, const void* residual, 
  * Quantises x[rows][cols] (PAT_FLOAT32 or PAT_BFLOAT16).  Per block: s = the least,
  * from 0, for which no magnitude is above 3.75 * 2^(s - 127); code = the nearest value
  * of x * 2^(127 - s), ties to the even code: half a step, 2^-4 of the value at most, down
- * to 2^-8 of the block's largest, and 2^-10 of the scale below.  A block that holds an infinity or a NaN gets s = 255 and stands for
- * NaN in whole.
+ * to 2^-8 of the block's largest, and 2^-10 of the scale below.  A block that holds an
+ * infinity or a NaN gets s = 255 and stands for NaN in whole.
  */
 pat_status_t pat_mxb_quantize(const void* x, int64_t x_stride, size_t rows, size_t cols, pat_dtype_t dtype, void* codes,
                               void* scales, hipStream_t stream);

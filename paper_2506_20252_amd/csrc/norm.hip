@@ -7,20 +7,23 @@
 namespace pat {
 namespace {
 
-// How a row of `cols` columns is cut into lanes' eights (fours, with the second four `gap` columns after the first, where a type
-// has 4 bytes), the same for a whole launch:
+// How a wave's part of a row of `cols` columns is cut into lanes' eights (fours, with the second four `gap` columns after the
+// first, where a type has 4 bytes):
 //   kAll   every vector exists;
 //   kSome  a vector exists or does not;
 //   kEnds  one that would go over the row's end ends there and is moved down (rows of 4 columns and more);
 //   kOne   columns one by one.
+// I: the type of places in a row, int where rows are short enough.
 enum Cut { kAll, kSome, kEnds, kOne };
 template <Cut C>
 struct CutOf {
   static constexpr Cut value = C;
 };
-template <bool SPLIT, typename F>
-__device__ __forceinline__ void cut(int64_t cols, int64_t all, F f) {
-  if (cols == all) f(CutOf<kAll>{});
+// f by what this wave has; `last`: the lane's columns from the first of its last vector to the row's end.  Waves of one
+// workgroup may go different ways, through as many barriers.
+template <bool SPLIT, typename I, typename F>
+__device__ __forceinline__ void cut(I cols, I last, I gap, F f) {
+  if (__all(last >= gap + 4)) f(CutOf<kAll>{});
   else if (cols % (SPLIT ? 4 : 8) == 0) f(CutOf<kSome>{});
   else if (cols >= 4) f(CutOf<kEnds>{});
   else f(CutOf<kOne>{});
@@ -32,42 +35,42 @@ template <typename T>
 struct Raw {
   typename T::vec4 lo, hi;
 };
-template <typename T, bool SPLIT, Cut C, bool NT = false>
-__device__ __forceinline__ Raw<T> load_raw(const void* row, int64_t col, int64_t cols, int64_t gap) {
+template <typename T, bool SPLIT, Cut C, bool NT = false, typename I>
+__device__ __forceinline__ Raw<T> load_raw(const void* row, I col, I cols, I gap) {
   typedef typename T::vec4 V;
-  const int64_t n = cols - col;
+  const I n = cols - col;
   const char* p = (const char*)row + col * T::kBytes;
   if constexpr (C == kOne) {
     float v[8];
     load8<T, SPLIT, false, kFew>(p, n, gap, v);
     return {T::narrow(v), T::narrow(v + 4)};
   } else if constexpr (C <= kSome && !SPLIT && T::kBytes == 2) {
-    const v4u a = ldg<v4u, NT, 2>(C == kAll ? p : p + min((int64_t)0, n - 8) * 2);
+    const v4u a = ldg<v4u, NT, 2>(C == kAll ? p : p + min((I)0, n - 8) * 2);
     return {{a[0], a[1]}, {a[2], a[3]}};
   } else {
-    const int64_t at = C == kAll ? 0 : min((int64_t)0, n - 4), to = C == kAll ? gap : min(gap, n - 4);
+    const I at = C == kAll ? 0 : min((I)0, n - 4), to = C == kAll ? gap : min(gap, n - 4);
     return {ldg<V, NT, T::kBytes>(p + at * T::kBytes), ldg<V, NT, T::kBytes>(p + to * T::kBytes)};
   }
 }
-template <typename T, bool SPLIT, Cut C>
-__device__ __forceinline__ void widen(const Raw<T>& r, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
-  const int64_t n = cols - col;
+template <typename T, bool SPLIT, Cut C, typename I>
+__device__ __forceinline__ void widen(const Raw<T>& r, I col, I cols, I gap, float (&v)[8]) {
+  const I n = cols - col;
   T::widen(r.lo, v);
   T::widen(r.hi, v + 4);
   if constexpr (C == kSome) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = n > (SPLIT && i >= 4 ? gap : 0) ? v[i] : 0.0f;
   } else if constexpr (C == kEnds) {
-    move_down(v, max((int64_t)0, 4 - n));
-    move_down(v + 4, max((int64_t)0, gap + 4 - n));
+    move_down(v, max((I)0, 4 - n));
+    move_down(v + 4, max((I)0, gap + 4 - n));
   }
 }
 // The same of a vector whose type is known at the launch alone.
 struct RawWeight {
   v4u lo, hi;
 };
-template <bool SPLIT, Cut C>
-__device__ __forceinline__ RawWeight load_raw(Elem e, const void* weight, int64_t col, int64_t cols, int64_t gap) {
+template <bool SPLIT, Cut C, typename I>
+__device__ __forceinline__ RawWeight load_raw(Elem e, const void* weight, I col, I cols, I gap) {
   if (e == Elem::f32) {
     const Raw<F32> r = load_raw<F32, SPLIT, C>(weight, col, cols, gap);
     return {__builtin_bit_cast(v4u, r.lo), __builtin_bit_cast(v4u, r.hi)};
@@ -75,15 +78,15 @@ __device__ __forceinline__ RawWeight load_raw(Elem e, const void* weight, int64_
   const Raw<B16> r = load_raw<B16, SPLIT, C>(weight, col, cols, gap);
   return {v4u{r.lo[0], r.lo[1], r.hi[0], r.hi[1]}, v4u{0, 0, 0, 0}};
 }
-template <bool SPLIT, Cut C>
-__device__ __forceinline__ void widen(Elem e, const RawWeight& r, int64_t col, int64_t cols, int64_t gap, float (&v)[8]) {
+template <bool SPLIT, Cut C, typename I>
+__device__ __forceinline__ void widen(Elem e, const RawWeight& r, I col, I cols, I gap, float (&v)[8]) {
   if (e == Elem::f32) widen<F32, SPLIT, C>({__builtin_bit_cast(v4f, r.lo), __builtin_bit_cast(v4f, r.hi)}, col, cols, gap, v);
   else widen<B16, SPLIT, C>({{r.lo[0], r.lo[1]}, {r.lo[2], r.lo[3]}}, col, cols, gap, v);
 }
-template <typename T, bool SPLIT, Cut C, bool NT = false>
-__device__ __forceinline__ void store_cols(void* row, int64_t col, int64_t cols, int64_t gap, const float (&v)[8]) {
+template <typename T, bool SPLIT, Cut C, bool NT = false, typename I>
+__device__ __forceinline__ void store_cols(void* row, I col, I cols, I gap, const float (&v)[8]) {
   char* p = (char*)row + col * T::kBytes;
-  const int64_t n = cols - col;
+  const I n = cols - col;
   if constexpr (C == kAll) store8<T, SPLIT, NT, kWhole>(p, n, gap, v);
   else if constexpr (C == kSome && !SPLIT) {
     if (n > 0) store8<T, SPLIT, NT, kWhole>(p, n, gap, v);
@@ -123,120 +126,168 @@ __device__ __forceinline__ void sum_of_row(float (&v)[N], int lanes, float* part
     for (int i = 0; i < N; ++i) v[i] += part[(first + w) * N + i];
 }
 
-// U > 0: a workgroup goes through rows gridDim.x apart; a row's values stay in registers, the weight too, and the next row's
-// loads are on their way before this row's sum.  0: a row's values are read again.
+// The first of a lane's columns in its u-th of U vectors: a wave's are beside each other, so that the last wave of a row alone
+// meets its end.
+template <bool SPLIT, int U>
+struct Place {
+  int lane, width;
+  __device__ __forceinline__ Place(int lanes) : lane(threadIdx.x % lanes), width(min(lanes, 64)) {}
+  __device__ __forceinline__ int operator()(int u) const { return (lane / width * U + u) * 8 * width + (int)lane_column<SPLIT>(lane % width); }
+  __device__ __forceinline__ int gap() const { return (int)lane_gap<SPLIT>(width); }
+};
+
+// What leaves of a lane's 8 columns: t * scale * weight.
+template <typename O, bool SPLIT, Cut C, typename I>
+__device__ __forceinline__ void finish(const NormArgs& a, int64_t row, bool real, I col, I cols, I gap, const float (&t)[8], const RawWeight& raw,
+                                       float scale) {
+  float w[8], y[8];
+  widen<SPLIT, C>(a.weight_dtype, raw, col, cols, gap, w);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = t[i] * scale * w[i];
+  if constexpr (O::kBytes == 1) {
+    const int64_t groups = (a.cols + 127) / 128;
+    uint32_t high = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (C != kAll) y[i] = col + i < cols ? y[i] : 0.0f;
+      high = max(high, __float_as_uint(y[i]) & 0x7FFFFFFFu);
+    }
+    const uint32_t s = mxb_scale_byte(max_of_4(high)), sub = threadIdx.x % 16;
+    const uint32_t four = or_of_16_by_4(s << (sub / 4 * 8));
+    if (!real || col >= groups * 128) return;
+    const int64_t g = row * groups + col / 128;
+    stg<false>((char*)a.blocks.codes + g * 128 + sub * 8, v2u{mxb_codes(y[0], y[1], y[2], y[3], s), mxb_codes(y[4], y[5], y[6], y[7], s)});
+    if (sub == 0) stg<false>((char*)a.blocks.scales + g * 4, four);
+  } else {
+    if (real) store_cols<O, SPLIT, C>(row_of<O>(a.out, row), col, cols, gap, y);
+  }
+}
+
+// The sum of eight squares, added up apart, so that long rows' sums have an eighth of the terms.
+__device__ __forceinline__ float squares(const float (&t)[8]) {
+  float eight = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) eight = fmaf(t[i], t[i], eight);
+  return eight;
+}
+
+// t of a lane's columns: x, or x + residual as its type holds it.
+template <typename X, bool SPLIT, Cut C, typename I>
+__device__ __forceinline__ void total_of(const Raw<X>& x, const Raw<X>& r, bool residual, I col, I cols, I gap, float (&t)[8]) {
+  widen<X, SPLIT, C>(x, col, cols, gap, t);
+  if (residual) {
+    float v[8];
+    widen<X, SPLIT, C>(r, col, cols, gap, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = round_to(X{}, t[i] + v[i]);
+  }
+}
+
+// Workgroups go through rows gridDim.x apart; a row's values stay in registers, the weight too, and the next row's loads are on
+// their way before this row's sum.  Bound by memory: 8192 x 8192 bfloat16 with a residual (537 MB) in 81 us, 6.6 TB/s (94 with
+// a workgroup for every row); loads and the total's stores are nontemporal, the output's, which are read next, are not.
 template <typename X, typename O, int U>
 __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) {
-  constexpr bool BLOCKS = O::kBytes == 1, SPLIT = !BLOCKS && Split<X, O>::value;
-  constexpr int V = U ? U : 1;
+  constexpr bool SPLIT = O::kBytes > 1 && Split<X, O>::value;
   __shared__ float part[2][kNormMost / 64];
-  const int lane = threadIdx.x % lanes, side = blockDim.x / lanes;
-  const int64_t groups = (a.cols + 127) / 128, gap = lane_gap<SPLIT>(lanes), step = (int64_t)gridDim.x * side;
-  const int64_t turns = U ? U : ((BLOCKS ? groups * 128 : a.cols) + 8 * lanes - 1) / (8 * lanes);
-  auto at = [&](int64_t u) { return lane_column<SPLIT>(lane) + u * 8 * lanes; };
+  const int side = blockDim.x / lanes, cols = (int)a.cols;
+  const int64_t step = (int64_t)gridDim.x * side;
+  const Place<SPLIT, U> at(lanes);
+  const int gap = at.gap();
+  const bool residual = a.residual.p != nullptr;
   auto all = [&](auto how) {
     constexpr Cut C = decltype(how)::value;
-    const bool residual = a.residual.p != nullptr;
-    Raw<X> x[V], r[V];
-    RawWeight weight[V];
-    auto fetch = [&](int64_t base, int64_t u0) {
+    Raw<X> x[U], r[U];
+    RawWeight weight[U];
+    auto fetch = [&](int64_t base) {
       const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
 #pragma unroll
-      for (int u = 0; u < V; ++u) x[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u0 + u), a.cols, gap);
+      for (int u = 0; u < U; ++u) x[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), cols, gap);
       if (residual) {
 #pragma unroll
-        for (int u = 0; u < V; ++u) r[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.residual, row), at(u0 + u), a.cols, gap);
-      }
-    };
-    auto sum_up = [&](int64_t u, const Raw<X>& x, const Raw<X>& r, float (&t)[8]) {
-      widen<X, SPLIT, C>(x, at(u), a.cols, gap, t);
-      if (residual) {
-        float v[8];
-        widen<X, SPLIT, C>(r, at(u), a.cols, gap, v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) t[i] = round_to(X{}, t[i] + v[i]);
+        for (int u = 0; u < U; ++u) r[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.residual, row), at(u), cols, gap);
       }
     };
     int turn = 0;
     int64_t base = (int64_t)blockIdx.x * side;
-    if (base >= a.rows) return;
-    if constexpr (U > 0) {
-      fetch(base, 0);
+    fetch(base);
 #pragma unroll
-      for (int u = 0; u < V; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), a.cols, gap);
-    }
+    for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), cols, gap);
     for (; base < a.rows; base += step, turn ^= 1) {
       const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
       const bool real = base + threadIdx.x / lanes < a.rows;
-      float t[V][8], sum[1] = {0.0f};
-      auto take = [&](int64_t u0) {
+      float t[U][8], sum[1] = {0.0f};
 #pragma unroll
-        for (int u = 0; u < V; ++u) {
-          sum_up(u0 + u, x[u], r[u], t[u]);
-          if (a.total.p && real) store_cols<X, SPLIT, C, (U > 0)>(row_of<X>(a.total, row), at(u0 + u), a.cols, gap, t[u]);
-          float eight = 0.0f;  // added up apart, so that long rows' sums have an eighth of the terms
-#pragma unroll
-          for (int i = 0; i < 8; ++i) eight = fmaf(t[u][i], t[u][i], eight);
-          sum[0] += eight;
-        }
-      };
-      auto finish = [&](int64_t col, const float (&t)[8], const RawWeight& raw, float r) {
-        float w[8], y[8];
-        widen<SPLIT, C>(a.weight_dtype, raw, col, a.cols, gap, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y[i] = t[i] * r * w[i];
-        if constexpr (BLOCKS) {
-          uint32_t high = 0;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            if (C != kAll) y[i] = col + i < a.cols ? y[i] : 0.0f;
-            high = max(high, __float_as_uint(y[i]) & 0x7FFFFFFFu);
-          }
-          const uint32_t s = mxb_scale_byte(max_of_4(high)), sub = lane % 16;
-          const uint32_t four = or_of_16_by_4(s << (sub / 4 * 8));
-          if (!real || col >= groups * 128) return;
-          const int64_t g = row * groups + col / 128;
-          stg<false>((char*)a.blocks.codes + g * 128 + sub * 8, v2u{mxb_codes(y[0], y[1], y[2], y[3], s), mxb_codes(y[4], y[5], y[6], y[7], s)});
-          if (sub == 0) stg<false>((char*)a.blocks.scales + g * 4, four);
-        } else {
-          if (real) store_cols<O, SPLIT, C>(row_of<O>(a.out, row), col, a.cols, gap, y);
-        }
-      };
-      if constexpr (U > 0) {
-        take(0);
-        if (base + step < a.rows) fetch(base + step, 0);
-      } else {
-        for (int64_t u = 0; u < turns; ++u) fetch(base, u), take(u);
+      for (int u = 0; u < U; ++u) {
+        total_of<X, SPLIT, C>(x[u], r[u], residual, at(u), cols, gap, t[u]);
+        if (a.total.p && real) store_cols<X, SPLIT, C, true>(row_of<X>(a.total, row), at(u), cols, gap, t[u]);
+        sum[0] += squares(t[u]);
       }
+      if (base + step < a.rows) fetch(base + step);
       sum_of_row(sum, lanes, part[turn]);
-      const float scale = rsqrtf(sum[0] / (float)a.cols + a.eps);
-      if constexpr (U > 0) {
+      const float scale = rsqrtf(sum[0] / (float)cols + a.eps);
 #pragma unroll
-        for (int u = 0; u < V; ++u) finish(at(u), t[u], weight[u], scale);
-      } else {
-        for (int64_t u = 0; u < turns; ++u) {  // again, out of the total where there is one
-          if (a.total.p) widen<X, SPLIT, C>(load_raw<X, SPLIT, C>(row_of<X>(a.total, row), at(u), a.cols, gap), at(u), a.cols, gap, t[0]);
-          else fetch(base, u), sum_up(u, x[0], r[0], t[0]);
-          finish(at(u), t[0], load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), a.cols, gap), scale);
-        }
-      }
+      for (int u = 0; u < U; ++u) finish<O, SPLIT, C>(a, row, real, at(u), cols, gap, t[u], weight[u], scale);
     }
   };
-  cut<SPLIT>(a.cols, turns * 8 * lanes, all);
+  cut<SPLIT>(cols, cols - at(U - 1), gap, all);
+}
+
+// Rows that are too long for registers are read again, out of the total where there is one.  2048 x 20000 bfloat16 with a
+// residual: 90 us, 5.4 TB/s without what is read again.
+template <typename X, typename O>
+__global__ __launch_bounds__(kNormMost) void norm_long_kernel(NormArgs a) {
+  constexpr bool SPLIT = O::kBytes > 1 && Split<X, O>::value;
+  __shared__ float part[2][kNormMost / 64];
+  const int64_t gap = lane_gap<SPLIT>(kNormMost), first = lane_column<SPLIT>(threadIdx.x);
+  const int64_t width = O::kBytes == 1 ? (a.cols + 127) / 128 * 128 : a.cols;  // blocks are filled up
+  const bool residual = a.residual.p != nullptr, total = a.total.p != nullptr;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
+    const char *x_row = row_of<X>(a.x, row), *r_row = residual ? row_of<X>(a.residual, row) : x_row;
+    float sum[1] = {0.0f};
+    for (int64_t col = first; col - first < width; col += 8 * kNormMost)
+      cut<SPLIT>(a.cols, a.cols - col, gap, [&](auto how) {
+        constexpr Cut C = decltype(how)::value;
+        float t[8];
+        const Raw<X> x = load_raw<X, SPLIT, C>(x_row, col, a.cols, gap), r = load_raw<X, SPLIT, C>(r_row, col, a.cols, gap);
+        total_of<X, SPLIT, C>(x, r, residual, col, a.cols, gap, t);
+        if (total) store_cols<X, SPLIT, C>(row_of<X>(a.total, row), col, a.cols, gap, t);
+        sum[0] += squares(t);
+      });
+    sum_of_row(sum, kNormMost, part[turn]);
+    const float scale = rsqrtf(sum[0] / (float)a.cols + a.eps);
+    for (int64_t col = first; col - first < width; col += 8 * kNormMost)
+      cut<SPLIT>(a.cols, a.cols - col, gap, [&](auto how) {
+        constexpr Cut C = decltype(how)::value;
+        float t[8];
+        const Raw<X> x = load_raw<X, SPLIT, C>(total ? row_of<X>(a.total, row) : x_row, col, a.cols, gap);
+        const Raw<X> r = load_raw<X, SPLIT, C>(total ? row_of<X>(a.total, row) : r_row, col, a.cols, gap);
+        const RawWeight weight = load_raw<SPLIT, C>(a.weight_dtype, a.weight, col, a.cols, gap);
+        total_of<X, SPLIT, C>(x, r, residual && !total, col, a.cols, gap, t);
+        finish<O, SPLIT, C>(a, row, true, col, a.cols, gap, t, weight, scale);
+      });
+  }
 }
 
 // ---- gradients
 
-// A row's loads are all on their way before its sums, and, where the registers suffice (up to 16 columns a lane), the next
-// row's before this row's results; the weight stays in registers then too.  Wider lanes load it, and the total's gradient, where
-// they use them.
+// With r = 1 / sqrt(mean(x^2) + eps):  out = total_grad + r (g w - x r^2 mean(g w x)),  dweight = the rows' sum of g x r.
+//
+// Bound by memory.  A row's loads are all on their way before its sums, and, where the registers suffice (up to 16 columns a
+// lane), the next row's before this row's results; the weight stays in registers then too.  Wider lanes load it, and the total's
+// gradient, where they use them.  8192 x 8192 bfloat16 with a total's gradient (537 MB) in 89 us with the parts' sum, 6.0 TB/s (97
+// without the total's gradient ahead), 16384 x 4096 in 97, 8192 x 2560 in 40, 10513 x 2129 in 59.
 template <typename X, typename G, int U>
-__global__ __launch_bounds__(U == 1 ? kStripThreads : kNormGradMost) void norm_grad_kernel(NormGradArgs a, int lanes, float* sums, int64_t pitch) {
+__global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= G::kBytes ? 3 : 2) void norm_grad_kernel(
+    NormGradArgs a, int lanes, float* sums, int64_t pitch) {
   constexpr bool SPLIT = Split<X, G>::value, AHEAD = X::kBytes + G::kBytes == 4 && U <= 2, KEEP = U <= 2;
   __shared__ float part[2][2 * kNormGradMost / 64];
   __shared__ float joined[U == 1 ? 8 * kStripThreads : 1];
-  const int lane = threadIdx.x % lanes, side = blockDim.x / lanes;
-  const int64_t gap = lane_gap<SPLIT>(lanes), step = (int64_t)gridDim.x * side;
+  const int side = blockDim.x / lanes, cols = (int)a.cols;
+  const int64_t step = (int64_t)gridDim.x * side;
+  const Place<SPLIT, U> at(lanes);
+  const int gap = at.gap();
   float dw[U][8];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -244,70 +295,72 @@ __global__ __launch_bounds__(U == 1 ? kStripThreads : kNormGradMost) void norm_g
     for (int i = 0; i < 8; ++i) dw[u][i] = 0.0f;
   auto all = [&](auto how) {
     constexpr Cut C = decltype(how)::value;
-    auto at = [&](int u) { return lane_column<SPLIT>(lane) + u * 8 * lanes; };
     RawWeight weight[U];
     if constexpr (KEEP) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), a.cols, gap);
+      for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), cols, gap);
     }
+    const bool more = a.total_grad.p != nullptr;
     Raw<X> x_raw[U];
-    Raw<G> g_raw[U];
+    Raw<G> g_raw[U], t_raw[U];
     auto fetch = [&](int64_t base) {
       const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        x_raw[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), a.cols, gap);
-        g_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.g, row), at(u), a.cols, gap);
+        x_raw[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), cols, gap);
+        g_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.g, row), at(u), cols, gap);
+      }
+      if (KEEP && more) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), cols, gap);
       }
     };
     int turn = 0;
     int64_t base = (int64_t)blockIdx.x * side;
-    if (base < a.rows) fetch(base);
+    fetch(base);
     for (; base < a.rows; base += step, turn ^= 1) {
       const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
-      const bool real = base + threadIdx.x / lanes < a.rows, more = a.total_grad.p != nullptr;
-      Raw<G> t_raw[U];
-      if (KEEP && more) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), a.cols, gap);
-      }
+      const bool real = base + threadIdx.x / lanes < a.rows;
       float x[U][8], g[U][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float w[8];
-        widen<X, SPLIT, C>(x_raw[u], at(u), a.cols, gap, x[u]);
-        widen<G, SPLIT, C>(g_raw[u], at(u), a.cols, gap, g[u]);
-        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), a.cols, gap);
-        widen<SPLIT, C>(a.weight_dtype, weight[u], at(u), a.cols, gap, w);
+        widen<X, SPLIT, C>(x_raw[u], at(u), cols, gap, x[u]);
+        widen<G, SPLIT, C>(g_raw[u], at(u), cols, gap, g[u]);
+        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), cols, gap);
+        widen<SPLIT, C>(a.weight_dtype, weight[u], at(u), cols, gap, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[0] = fmaf(x[u][i], x[u][i], s[0]), s[1] = fmaf(g[u][i] * w[i], x[u][i], s[1]);
       }
+      Raw<G> t_now[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) t_now[u] = t_raw[u];
       if (AHEAD && base + step < a.rows) fetch(base + step);
       sum_of_row(s, lanes, part[turn]);
-      const float n = (float)a.cols, r = rsqrtf(s[0] / n + a.eps), k = r * r * (s[1] / n);
+      const float n = (float)cols, r = rsqrtf(s[0] / n + a.eps), k = r * r * (s[1] / n);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float w[8], d[8];
-        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), a.cols, gap);
-        widen<SPLIT, C>(a.weight_dtype, weight[u], at(u), a.cols, gap, w);
+        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), cols, gap);
+        widen<SPLIT, C>(a.weight_dtype, weight[u], at(u), cols, gap, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           d[i] = r * (g[u][i] * w[i] - x[u][i] * k);
           dw[u][i] += real ? g[u][i] * (x[u][i] * r) : 0.0f;
         }
         if (more) {
-          if (!KEEP) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), a.cols, gap);
+          if (!KEEP) t_now[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), cols, gap);
           float t[8];
-          widen<G, SPLIT, C>(t_raw[u], at(u), a.cols, gap, t);
+          widen<G, SPLIT, C>(t_now[u], at(u), cols, gap, t);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] += t[i];
         }
-        if (real) store_cols<G, SPLIT, C>(row_of<G>(a.out, row), at(u), a.cols, gap, d);
+        if (real) store_cols<G, SPLIT, C>(row_of<G>(a.out, row), at(u), cols, gap, d);
       }
       if (!AHEAD && base + step < a.rows) fetch(base + step);
     }
   };
-  cut<SPLIT>(a.cols, U * 8 * lanes, all);
+  cut<SPLIT>(cols, cols - at(U - 1), gap, all);
 
   // The groups' parts in order.
   if constexpr (U == 1) {
@@ -324,7 +377,7 @@ __global__ __launch_bounds__(U == 1 ? kStripThreads : kNormGradMost) void norm_g
   char* to = (char*)(sums + blockIdx.x * pitch);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t col = lane_column<SPLIT>(lane) + u * 8 * lanes;
+    const int64_t col = at(u);
     store8<F32, true, false, kFew>(to + col * 4, a.cols - col, gap, dw[u]);
   }
 }
@@ -350,8 +403,7 @@ __global__ __launch_bounds__(kStripThreads) void norm_sums_kernel(NormGradArgs a
         widen<G, SPLIT, C>(g_raw, col, a.cols, gap, g);
         widen<SPLIT, C>(a.weight_dtype, w_raw, col, a.cols, gap, w);
       };
-      if (c + 8 * kStripThreads <= a.cols) take(CutOf<kAll>{});
-      else take(CutOf<kEnds>{});
+      cut<SPLIT>(a.cols, a.cols - col, gap, take);
       float e[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int i = 0; i < 8; ++i) e[0] = fmaf(x[i], x[i], e[0]), e[1] = fmaf(g[i] * w[i], x[i], e[1]);
@@ -363,7 +415,8 @@ __global__ __launch_bounds__(kStripThreads) void norm_sums_kernel(NormGradArgs a
   }
 }
 
-// Then a strip of columns a workgroup, every gridDim.y-th row.
+// Then a strip of columns a workgroup, every gridDim.y-th row.  Both: 2048 x 20000 bfloat16 with a total's gradient in 95 us (328 MB, and g and x
+// once more).
 template <typename X, typename G>
 __global__ __launch_bounds__(kStripThreads) void norm_strip_kernel(NormGradArgs a, const v2f* rows, float* sums, int64_t pitch) {
   constexpr bool SPLIT = Split<X, G>::value;
@@ -394,8 +447,7 @@ __global__ __launch_bounds__(kStripThreads) void norm_strip_kernel(NormGradArgs 
       store_cols<G, SPLIT, C>(row_of<G>(a.out, row), col, a.cols, gap, d);
     }
   };
-  if (c0 + 8 * kStripThreads <= a.cols) all(CutOf<kAll>{});
-  else all(CutOf<kEnds>{});
+  cut<SPLIT>(a.cols, a.cols - col, gap, all);
   store8<F32, true, false, kFew>((char*)(sums + blockIdx.y * pitch + col), a.cols - col, gap, dw);
 }
 
@@ -432,8 +484,11 @@ __global__ __launch_bounds__(256) void norm_zero_kernel(float* out, int64_t cols
 template <typename X, typename O>
 hipError_t run_norm(const NormArgs& a, hipStream_t stream) {
   const NormPlan p = norm_plan(a.rows, a.cols, O::kBytes == 1);
-  const auto kernel = p.vectors == 1 ? norm_kernel<X, O, 1> : p.vectors == 2 ? norm_kernel<X, O, 2> : norm_kernel<X, O, 0>;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)p.wgs), dim3(p.threads), 0, stream, a, p.lanes);
+  if (p.vectors)
+    hipLaunchKernelGGL((p.vectors == 1 ? norm_kernel<X, O, 1> : norm_kernel<X, O, 2>), dim3((unsigned)p.wgs), dim3(p.threads), 0, stream, a,
+                       p.lanes);
+  else
+    hipLaunchKernelGGL((norm_long_kernel<X, O>), dim3((unsigned)p.wgs), dim3(kNormMost), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -86,8 +86,8 @@ static void check_norm(int64_t rows, int64_t cols) {
   if (rows >= (int64_t)1 << 28 || cols >= (int64_t)1 << 26) return;
   const NormGradPlan g = norm_grad_plan(rows, cols);
   check_plan(g, rows, units, kNormGradMost, 4);
-  CHECK(g.vectors != 1 || g.threads <= kStripThreads, "%lld %lld: %d", (long long)rows, (long long)cols, g.threads);  // LDS of the groups' join
-  CHECK(g.vectors == 1 || g.vectors == 0 || g.threads == g.lanes, "%lld %lld", (long long)rows, (long long)cols);     // which others do not have
+  // rows beside each other in a workgroup are joined in LDS for 256 lanes of one vector
+  CHECK(g.threads == g.lanes || (g.vectors == 1 && g.threads <= kStripThreads), "%lld %lld: %d", (long long)rows, (long long)cols, g.threads);
   CHECK(g.pitch >= cols && g.pitch % 8 == 0 && g.strips * 8 * kStripThreads >= cols, "%lld", (long long)cols);
   CHECK(g.wgs <= rows && g.wgs < 65536 && g.strips * g.wgs * kStripThreads < kLanes, "%lld %lld: %lld", (long long)rows, (long long)cols, (long long)g.wgs);
 }
