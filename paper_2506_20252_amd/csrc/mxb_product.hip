@@ -52,6 +52,27 @@ __device__ __forceinline__ void store4(char* p, int64_t left, const v4f& f) {
       if (i < left) T::store(p, i, v[i]);
 }
 
+// Waits until at most LATER of this wave's loads are on their way and all its reads of LDS are done, then for the other waves.
+template <int LATER>
+__device__ __forceinline__ void meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
+}
+
+// Loads of 16 bytes a lane from base + at, and of 4 bytes from p, into LDS, lane after lane from `to` on.  Written out: the
+// compiler's own ones make it wait for all of them before LDS is read, in every turn of the loop.
+__device__ __forceinline__ uint32_t lds_place(const uint8_t* to) {
+  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to);
+}
+__device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t at, const uint8_t* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(const uint8_t* base, uint32_t at, const uint8_t* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(const uint8_t* p, const uint8_t* to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_place(to)), "v"(p) : "memory");
+}
+
 // ---- tiles through LDS ---------------------------------------------------------------------------------------
 //
 // A workgroup of WN x WM waves computes a tile of N rows of the weight by M tokens, a wave FN x FM blocks of 32 x 32; of a
@@ -66,9 +87,13 @@ __device__ __forceinline__ void store4(char* p, int64_t left, const v4f& f) {
 // l mod 32 and all of block l / 32, of the activations 16 terms of each.  Any two blocks will do as long as both sides
 // take the same; the J-th instruction of a step takes the J-th and the J + 2-nd of its four, so that a lane's scales
 // are two neighbouring bytes, of which the instruction picks the J-th.
-typedef __attribute__((address_space(1))) const uint32_t* GlobalWords;
-typedef __attribute__((address_space(3))) uint32_t* LdsWords;
-
+//
+// Bound by the matrix instructions' rate, of which the loads into LDS take a part.  8192 tokens, 2 x 8192 rows, 4096 terms in
+// 381 us, 2.9 PFLOP/s, 8192^3 with a residual in 406, 2.7: the instructions out of registers alone give 4.5 at the clock
+// of short runs.  Measured for the former (418 us then): a wave of higher priority 540, scales packed 458, three steps on their way, the
+// weight by half lines, 455, bands of 3, 4 or 8 tiles of tokens no faster, no loads at all 340.  Each instruction followed by
+// its share of the reads and loads, and the loads' waits counted, gave the last 8 %: issued together after the barrier they
+// kept the instructions behind them waiting.  Two workgroups of 128 tokens a CU, the weight by half lines: 532.
 template <int FN, int FM, int WN, int WM>
 struct Tile {
   static constexpr int kWaves = WN * WM, N = 32 * FN * WN, M = 32 * FM * WM;
@@ -85,24 +110,26 @@ struct Tile {
 // 8 * (c / 4) + 4 * (l / 32) + c mod 4), to columns j ... of tokens i ...: the wave turns them round in `part`, LDS of its own.
 constexpr int turn_floats(int nb) { return 32 * (32 * nb + 4); }
 
-template <int NB, typename T, bool NT>
-__device__ __forceinline__ void store_turned(const float (&v)[NB][16], float* part, int64_t i, int64_t j, int64_t m, int64_t n,
-                                             Mat residual, MatOut out) {
-  constexpr int P = 32 * NB + 4, LANES = 4 * NB, ROWS = 64 / LANES;  // floats a token; lanes and tokens of an access
+template <int NB>
+struct Turn {
+  static constexpr int LANES = 4 * NB, ROWS = 64 / LANES, N = 32 / ROWS;  // lanes and tokens of an access, accesses
+};
+template <typename T>
+__device__ __forceinline__ void add8(const Raw8<T>& r, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t w = r.w[i * T::kBytes / 16][i * T::kBytes / 4 % 4];
+    v[i] += T::kBytes == 4 ? __uint_as_float(w) : i & 1 ? bf16_hi(w) : bf16_lo(w);
+  }
+}
+
+// INSIDE: all tokens and columns are there, and `added`, where it is not null, is what the residual has for them.
+template <int NB, bool INSIDE, typename T, bool NT>
+__device__ __forceinline__ void store_turned(const float (&v)[NB][16], const Raw8<T>* added, float* part, int64_t i, int64_t j, int64_t m,
+                                             int64_t n, Mat residual, MatOut out) {
+  constexpr int P = 32 * NB + 4, LANES = Turn<NB>::LANES, ROWS = Turn<NB>::ROWS;  // P: floats a token
   const int lane = threadIdx.x % 64, half = lane / 32, c = lane % LANES * 8;
   const int64_t left = n - j - c;
-  float r[32 / ROWS][8];
-#pragma unroll
-  for (int u = 0; u < 32 / ROWS; ++u) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[u][e] = 0.0f;
-    const int64_t row = i + u * ROWS + lane / LANES;
-    if (residual.p && row < m && left > 0) {
-      const char* p = (const char*)residual.p + (row * residual.stride + j + c) * T::kBytes;
-      if (left >= 8) load8<T, false, false, kWhole>(p, 8, 4, r[u]);
-      else load8<T, false, false, kFew>(p, left, 4, r[u]);
-    }
-  }
 #pragma unroll
   for (int x = 0; x < NB; ++x)
 #pragma unroll
@@ -110,14 +137,22 @@ __device__ __forceinline__ void store_turned(const float (&v)[NB][16], float* pa
       *(v4f*)(part + lane % 32 * P + 32 * x + 8 * e + 4 * half) = v4f{v[x][4 * e], v[x][4 * e + 1], v[x][4 * e + 2], v[x][4 * e + 3]};
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-  for (int u = 0; u < 32 / ROWS; ++u) {
+  for (int u = 0; u < Turn<NB>::N; ++u) {
     const int token = u * ROWS + lane / LANES;
     const v4f lo = *(const v4f*)(part + token * P + c), hi = *(const v4f*)(part + token * P + c + 4);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[u][e] += lo[e], r[u][4 + e] += hi[e];
+    float r[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
     char* p = (char*)out.p + ((i + token) * out.stride + j + c) * T::kBytes;
-    if (i + token < m && left >= 8) store8<T, false, NT, kWhole>(p, 8, 4, r[u]);
-    else if (i + token < m && left > 0) store8<T, false, NT, kEnd>(p, left, 4, r[u]);
+    if constexpr (INSIDE) {
+      if (added) add8<T>(added[u], r);
+      store8<T, false, NT, kWhole>(p, 8, 4, r);
+    } else if (i + token < m && left > 0) {
+      if (residual.p) {
+        const char* q = (const char*)residual.p + ((i + token) * residual.stride + j + c) * T::kBytes;
+        add8<T>(left >= 8 ? load_raw8<T, kWhole>(q, 0, 8) : load_raw8<T, kFew>(q, 0, left), r);
+      }
+      if (left >= 8) store8<T, false, NT, kWhole>(p, 8, 4, r);
+      else store8<T, false, NT, kEnd>(p, left, 4, r);
+    }
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
@@ -150,19 +185,47 @@ template <int FN, int FM, bool GATED, typename O, bool NT>
 __device__ __forceinline__ void leave(const v16f (&acc)[FN][FM], float* part, int64_t i, int64_t j, int64_t m, int64_t n, const Epilogue& ep) {
   static_assert(FN % 2 == 0, "");
   const int lane = threadIdx.x % 64;
+  if constexpr (!GATED) {
+    // Two blocks at a time, and the residual of as many twos at once as there are registers for.
+    constexpr int TWOS = FN / 2 * FM, MOST = O::kBytes == 4 ? 2 : 4, ONCE = TWOS < MOST ? TWOS : MOST;
+    static_assert(TWOS % ONCE == 0, "");
+    auto put = [&](auto inside, const Raw8<O>* added, int two) {
+      const int b = two / (FN / 2), a = two % (FN / 2) * 2;
+      float v[2][16];
 #pragma unroll
-  for (int b = 0; b < FM; ++b, i += 32) {
-    if constexpr (!GATED) {
+      for (int y = 0; y < 2; ++y)
 #pragma unroll
-      for (int a = 0; a < FN; a += 2) {
-        float v[2][16];
+        for (int e = 0; e < 16; ++e) v[y][e] = acc[a + y][b][e];
+      store_turned<2, decltype(inside)::value == 1, O, NT>(v, added, part, i + 32 * b, j + 32 * a, m, n, ep.residual, ep.out);
+    };
+    if (i + 32 * FM <= m && j + 32 * FN <= n) {
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+      for (int first = 0; first < TWOS; first += ONCE) {
+        Raw8<O> added[ONCE][Turn<2>::N];
+        if (ep.residual.p) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[y][e] = acc[a + y][b][e];
-        store_turned<2, O, NT>(v, part, i, j + 32 * a, m, n, ep.residual, ep.out);
+          for (int u = 0; u < ONCE * Turn<2>::N; ++u) {
+            const int two = first + u / Turn<2>::N;
+            const int64_t row = i + two / (FN / 2) * 32 + u % Turn<2>::N * Turn<2>::ROWS + lane / Turn<2>::LANES;
+            const int64_t col = j + two % (FN / 2) * 64 + lane % Turn<2>::LANES * 8;
+            added[u / Turn<2>::N][u % Turn<2>::N] =
+                load_raw8<O, kWhole>((const char*)ep.residual.p + (row * ep.residual.stride + col) * O::kBytes, 0, 8);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int u = 0; u < ONCE; ++u) put(Int<1>{}, added[u], first + u);
+        } else {
+#pragma unroll
+          for (int u = 0; u < ONCE; ++u) put(Int<1>{}, nullptr, first + u);
+        }
       }
     } else {
+#pragma unroll
+      for (int two = 0; two < TWOS; ++two) put(Int<0>{}, nullptr, two);
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < FM; ++b, i += 32) {
       constexpr int H = FN / 2;
       float v[H][16];
 #pragma unroll
@@ -179,7 +242,7 @@ __device__ __forceinline__ void leave(const v16f (&acc)[FN][FM], float* part, in
         }
         if constexpr (O::kBytes == 1) store_block(v[a], i + lane % 32, j + 32 * a, m, n, ep.blocks);
       }
-      if constexpr (O::kBytes > 1) store_turned<H, O, NT>(v, part, i, j, m, n, {nullptr, 0}, ep.out);
+      if constexpr (O::kBytes > 1) store_turned<H, false, O, NT>(v, nullptr, part, i, j, m, n, {nullptr, 0}, ep.out);
     }
   }
 }
@@ -191,7 +254,6 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
   typedef typename S::Pair Pair;
   typedef typename S::Step Step;
   constexpr int N = S::N, M = S::M, W = S::kWaves, COLS = GATED ? N / 2 : N;
-  // Objects of their own, and not arrays: the compiler then knows that the loads into one do not touch the others.
   __shared__ __attribute__((aligned(16))) Pair pair0;
   __shared__ __attribute__((aligned(16))) Pair pair1;
   __shared__ __attribute__((aligned(16))) Step step0;
@@ -218,34 +280,25 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
   for (int u = 0; u < LOADS_X; ++u) at_x[u] = (uint32_t)min((u * W + wave) * 8 + lane / 8, rows_x - 1) * x_pitch + piece * 16;
   // a wave loads the scales of 32 rows, two words each
   const int s_row = wave * 32 + lane / 2;
-  static_assert(N / 32 <= W && M / 32 <= W, "");
+  static_assert(N / 32 == W && M / 32 == W, "");
   const uint32_t sat_w = (uint32_t)min(column(s_row), rows_w - 1) * s_pitch + lane % 2 * 4;
   const uint32_t sat_x = (uint32_t)min(s_row, rows_x - 1) * s_pitch + lane % 2 * 4;
   const uint8_t *codes_w = w.codes + jb * w_pitch, *scales_w = w.scales + jb * s_pitch;
   const uint8_t *codes_x = x.codes + i0 * x_pitch, *scales_x = x.scales + i0 * s_pitch;
 
-  auto fetch_pair = [&](Pair& l, int g) {
-    // the second group of the last 256 terms may not exist: the first again, not multiplied
-    const uint32_t back = g + 1 < groups ? 0 : (piece >= 4 ? 64 : 0), sback = g + 1 < groups ? 0 : lane % 2 * 4;
-#pragma unroll
-    for (int u = 0; u < LOADS_W; ++u) {
-      const uint8_t* p = codes_w + (int64_t)g * 64 + (second((u * W + wave) * 8) ? n * w_pitch : 0);
-      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (at_w[u] - back)), (LdsWords)(l.codes + (u * W + wave) * 1024), 16, 0, 0);
+  // A step's loads in the order in which they are given out: the tokens' codes, then half of what the pair needs.
+  constexpr int HALF = LOADS_W / 2 + 1;
+  auto fetch_x = [&](Step& l, int g, int u) { load_to_lds16(codes_x + (int64_t)g * 128, at_x[u], l.codes + (u * W + wave) * 1024); };
+  auto fetch_w = [&](Pair& l, int g, int u, uint32_t back, uint32_t sback) {
+    if (u % HALF < LOADS_W / 2) {
+      const int v = u / HALF * (LOADS_W / 2) + u % HALF;
+      const uint8_t* p = codes_w + (int64_t)g * 64 + (second((v * W + wave) * 8) ? n * w_pitch : 0);
+      load_to_lds16(p, at_w[v] - back, l.codes + (v * W + wave) * 1024);
+    } else if (u < HALF) {
+      load_to_lds4(scales_w + (int64_t)g * 4 + (second(wave * 32) ? n * s_pitch : 0), sat_w - sback, l.w_scales + wave * 256);
+    } else {
+      load_to_lds4(scales_x + (int64_t)g * 4, sat_x - sback, l.x_scales + wave * 256);
     }
-    if (N / 32 == W || wave < N / 32) {
-      const uint8_t* p = scales_w + (int64_t)g * 4 + (second(wave * 32) ? n * s_pitch : 0);
-      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (sat_w - sback)), (LdsWords)(l.w_scales + wave * 256), 4, 0, 0);
-    }
-    if (M / 32 == W || wave < M / 32) {
-      const uint8_t* p = scales_x + (int64_t)g * 4;
-      __builtin_amdgcn_global_load_lds((GlobalWords)(p + (sat_x - sback)), (LdsWords)(l.x_scales + wave * 256), 4, 0, 0);
-    }
-  };
-  auto fetch_step = [&](Step& l, int g) {
-#pragma unroll
-    for (int u = 0; u < LOADS_X; ++u)
-      __builtin_amdgcn_global_load_lds((GlobalWords)(codes_x + (int64_t)g * 128 + at_x[u]), (LdsWords)(l.codes + (u * W + wave) * 1024),
-                                       16, 0, 0);
   };
 
   const int half = lane / 32, wave_n = wave / WM * 32 * FN, wave_m = wave % WM * 32 * FM;
@@ -271,64 +324,96 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
 #pragma unroll
     for (int b = 0; b < FM; ++b) s.x[b] = *(const uint16_t*)(l.x_scales + (row_x + 32 * b) * 8 + 4 * h + 2 * half);
   };
-  auto read = [&](const Pair& p, const Step& l, int h, int j, Blocks& c) {
-    auto at = [&](int piece) { return (piece ^ (lane >> 1 & 7)) * 16; };
-#pragma unroll
-    for (int a = 0; a < FN; ++a) c.w[a] = *(const v4i*)(p.codes + (row_w + 32 * a) * 128 + at(4 * h + 2 * half + j));
-#pragma unroll
-    for (int b = 0; b < FM; ++b) {
-      c.x[b][0] = *(const v4i*)(l.codes + (row_x + 32 * b) * 128 + at(2 * j + half));
-      c.x[b][1] = *(const v4i*)(l.codes + (row_x + 32 * b) * 128 + at(4 + 2 * j + half));
+  // The i-th of the reads of what the j-th instructions multiply.  Places are formed anew in every step: kept for all pieces
+  // they would take more registers than there are.
+  constexpr int READS = FN + 2 * FM;
+  const int swap = lane >> 1 & 7;
+  int from_w = row_w * 128 + (2 * half ^ swap) * 16, from_x = row_x * 128 + (half ^ swap) * 16;
+  auto read = [&](const Pair& p, const Step& l, int h, int j, int i, Blocks& c) {
+    if (i < FN) c.w[i] = *(const v4i*)(p.codes + (from_w ^ (4 * h + j) * 16) + 32 * i * 128);
+    else {
+      const int b = (i - FN) / 2, k = (i - FN) % 2;
+      c.x[b][k] = *(const v4i*)(l.codes + (from_x ^ (4 * k + 2 * j) * 16) + 32 * b * 128);
     }
   };
-  auto multiply = [&](const Blocks& c, const Scales& s, auto which) {
+  // After each instruction comes its share of the loads.
+  auto multiply = [&](const Blocks& c, const Scales& s, auto which, auto between) {
     constexpr int J = decltype(which)::value;
 #pragma unroll
     for (int a = 0; a < FN; ++a)
 #pragma unroll
-      for (int b = 0; b < FM; ++b)
+      for (int b = 0; b < FM; ++b) {
         acc[a][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(frag(c.w[a]), frag(c.x[b][0], c.x[b][1]), acc[a][b], 4, 0, J, s.w[a],
                                                                    J, s.x[b]);
-    // these stay together: moved over each other, all steps' blocks would be in registers at once
-    __builtin_amdgcn_sched_barrier(0);
+        between(a * FM + b);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+  };
+  constexpr int SLOTS = FN * FM;
+  auto share = [&](int slot, int items, auto f) {
+#pragma unroll
+    for (int i = 0; i < items; ++i)
+      if (i * SLOTS / items == slot) f(i);
+  };
+  // A row of the weight's blocks is read once the same of the blocks before is used up.
+  auto read_share = [&](int slot, auto f) {
+#pragma unroll
+    for (int i = 0; i < READS; ++i)
+      if ((i < FN ? min(i * FM + FM - 1, SLOTS - 2) : (i - FN) * SLOTS / (4 * FM)) == slot) f(i);
   };
 
   Blocks c0, c1;
   Scales s0, s1;
-  // Step g, the h-th of pair `p`, out of `l`; the first instructions' blocks are in c0 and the scales in `s`.  Before the second
+  // Step g, the H-th of pair `p`, out of `l`; the first instructions' blocks are in c0 and the scales in `s`.  Before the second
   // ones the next step has arrived and this step's LDS has been read by all, so both the next first blocks and what
-  // comes two steps (or pairs) later come in under them.  No branch: beyond the last it is fetched again.
-  auto step = [&](Pair& p, Step& l, const Pair& next_p, const Step& next_l, auto which, const Scales& s, Scales& next_s, int g) {
+  // comes two steps later come in under them, with half of a pair: the second half of `other`, or, once `p` is read, the first
+  // half of what follows `other` in its place.  That half is the last to be on its way, and only the next step but one needs it.
+  // No branch: beyond the last it is fetched again.
+  auto step = [&](Pair& p, Step& l, Pair& other, const Step& next_l, auto which, const Scales& s, Scales& next_s, int g) {
     constexpr int H = decltype(which)::value;
-    read(p, l, H, 1, c1);
-    multiply(c0, s, Int<0>{});
-    __syncthreads();
-    read_scales(next_p, 1 - H, next_s);
-    read(next_p, next_l, 1 - H, 0, c0);
-    fetch_step(l, min(g + 2, groups - 1));
-    if constexpr (H == 1) fetch_pair(p, min(g + 3, (groups - 1) / 2 * 2));
-    multiply(c1, s, Int<1>{});
+    asm volatile("" : "+v"(from_w), "+v"(from_x));
+    multiply(c0, s, Int<0>{}, [&](int slot) { read_share(slot, [&](int i) { read(p, l, H, 1, i, c1); }); });
+    meet<H == 0 ? HALF : 0>();
+    const int gx = min(g + 2, groups - 1), gw = min(g + 2 + H, (groups - 1) / 2 * 2);
+    const uint32_t back = gw + 1 < groups ? 0 : (piece >= 4 ? 64 : 0), sback = gw + 1 < groups ? 0 : lane % 2 * 4;
+    const Pair& next_p = H ? other : p;
+    multiply(c1, s, Int<1>{}, [&](int slot) {
+      if (slot == 0) read_scales(next_p, 1 - H, next_s);
+      read_share(slot, [&](int i) { read(next_p, next_l, 1 - H, 0, i, c0); });
+      share(slot, LOADS_X + HALF, [&](int i) {
+        if (i < LOADS_X) fetch_x(l, gx, i);
+        else fetch_w(H ? p : other, gw, (H ? 0 : HALF) + i - LOADS_X, back, sback);
+      });
+    });
   };
-  fetch_pair(pair0, 0);
-  fetch_step(step0, 0);
-  __syncthreads();
-  fetch_pair(pair1, min(2, (groups - 1) / 2 * 2));
-  fetch_step(step1, min(1, groups - 1));
+  auto first = [&](Pair& l, int g, int begin, int end) {
+    const uint32_t back = g + 1 < groups ? 0 : (piece >= 4 ? 64 : 0), sback = g + 1 < groups ? 0 : lane % 2 * 4;
+#pragma unroll
+    for (int u = begin; u < end; ++u) fetch_w(l, g, u, back, sback);
+  };
+  first(pair0, 0, 0, 2 * HALF);
+#pragma unroll
+  for (int u = 0; u < LOADS_X; ++u) fetch_x(step0, 0, u);
+  meet<0>();
+#pragma unroll
+  for (int u = 0; u < LOADS_X; ++u) fetch_x(step1, min(1, groups - 1), u);
+  first(pair1, min(2, (groups - 1) / 2 * 2), 0, HALF);
   read_scales(pair0, 0, s0);
-  read(pair0, step0, 0, 0, c0);
+#pragma unroll
+  for (int i = 0; i < READS; ++i) read(pair0, step0, 0, 0, i, c0);
   int g = 0;
   for (; g + 4 <= groups; g += 4) {
-    step(pair0, step0, pair0, step1, Int<0>{}, s0, s1, g);
+    step(pair0, step0, pair1, step1, Int<0>{}, s0, s1, g);
     step(pair0, step1, pair1, step0, Int<1>{}, s1, s0, g + 1);
-    step(pair1, step0, pair1, step1, Int<0>{}, s0, s1, g + 2);
+    step(pair1, step0, pair0, step1, Int<0>{}, s0, s1, g + 2);
     step(pair1, step1, pair0, step0, Int<1>{}, s1, s0, g + 3);
   }
-  if (g < groups) step(pair0, step0, pair0, step1, Int<0>{}, s0, s1, g);
+  if (g < groups) step(pair0, step0, pair1, step1, Int<0>{}, s0, s1, g);
   if (g + 1 < groups) step(pair0, step1, pair1, step0, Int<1>{}, s1, s0, g + 1);
-  if (g + 2 < groups) step(pair1, step0, pair1, step1, Int<0>{}, s0, s1, g + 2);
+  if (g + 2 < groups) step(pair1, step0, pair0, step1, Int<0>{}, s0, s1, g + 2);
 
   // Results leave through LDS, whose last loads have to have come first.
-  __syncthreads();
+  meet<0>();
   static_assert(sizeof(Pair) >= W / 2 * turn_floats(2) * 4, "");
   float* part = (wave < W / 2 ? (float*)&pair0 : (float*)&pair1) + wave % (W / 2) * turn_floats(2);
   leave<FN, FM, GATED, O, (N * M >= 256 * 256)>(acc, part, i0 + wave_m, j0 + (GATED ? wave_n / 2 : wave_n), m, n, ep);
@@ -340,6 +425,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
 // the terms each, in LDS of their own, and their sums are added in order at the end; D steps are in LDS or on their way
 // at once.  The weight's rows come as half lines then, 64 bytes a step, at place piece ^ (row / 4 mod 4) of a row's four (a
 // row is a quarter of the banks).  Every wave has the same number of loads a step, and waits for those of the next step alone.
+// Bound by the loads' latency: 64 tokens by 4096 rows of 4096 terms in 9.1 us, 1001 by 2000 of 1333 in 7.1, of which starting,
+// filling LDS and leaving take five.
 template <int FN, int FM, int WN, int WM>
 struct Stage {
   static constexpr int kWaves = WN * WM, N = 32 * FN * WN, M = 32 * FM * WM;
@@ -347,27 +434,9 @@ struct Stage {
   uint8_t scales[N * 4 + M * 4];  // the weight's, the tokens'
 };
 
-// Waits until at most LATER of this wave's loads are on their way and all its reads of LDS are done, then for the other waves.
-template <int LATER>
-__device__ __forceinline__ void meet() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LATER) : "memory");
-}
-
-// Loads of 16 bytes a lane from base + at, and of 4 bytes from p, into LDS, lane after lane from `to` on.  Written out: the
-// compiler's own ones make it wait for all of them before LDS is read, in every turn of the loop.
-__device__ __forceinline__ uint32_t lds_place(const uint8_t* to) {
-  return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to);
-}
-__device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t at, const uint8_t* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
-}
-__device__ __forceinline__ void load_to_lds4(const uint8_t* p, const uint8_t* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_place(to)), "v"(p) : "memory");
-}
-
 template <int FN, int FM, int WN, int WM, int PARTS, int D, bool GATED, typename O>
-__global__ __launch_bounds__(64 * WN * WM * PARTS, WN * WM * PARTS == 8 ? 2 : 1) void deep_kernel(MxbMat x, MxMat w, int64_t m, int64_t n, int groups, int64_t tiles_n,
-                                                            Epilogue ep) {
+__global__ __launch_bounds__(64 * WN * WM * PARTS, WN * WM * PARTS == 8 ? 2 : 1) void deep_kernel(MxbMat x, MxMat w, int64_t m, int64_t n,
+                                                                                                 int groups, int64_t tiles_n, Epilogue ep) {
   typedef Stage<FN, FM, WN, WM> S;
   constexpr int N = S::N, M = S::M, W = S::kWaves, COLS = GATED ? N / 2 : N;
   __shared__ __attribute__((aligned(16))) S all_lds[PARTS][D];
@@ -490,14 +559,17 @@ __global__ __launch_bounds__(64 * WN * WM * PARTS, WN * WM * PARTS == 8 ? 2 : 1)
   if constexpr (PARTS > 1) {
     constexpr int SIZE = FN * FM * 16 * 64;  // floats of a wave's sums
     static_assert(sizeof(all_lds) >= (PARTS - 1) * W * SIZE * 4, "");
-    auto sums = [&](int p, int a, int b, int e) -> v4f& { return *(v4f*)(room + ((p - 1) * W + wave) * SIZE + (((a * FM + b) * 4 + e) * 64 + lane) * 4); };
+    auto sums = [&](int p, int a, int b, int e) -> v4f& {
+      return *(v4f*)(room + ((p - 1) * W + wave) * SIZE + (((a * FM + b) * 4 + e) * 64 + lane) * 4);
+    };
     if (part) {
 #pragma unroll
       for (int a = 0; a < FN; ++a)
 #pragma unroll
         for (int b = 0; b < FM; ++b)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sums(part, a, b, e) = v4f{acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2], acc[a][b][4 * e + 3]};
+          for (int e = 0; e < 4; ++e)
+            sums(part, a, b, e) = v4f{acc[a][b][4 * e], acc[a][b][4 * e + 1], acc[a][b][4 * e + 2], acc[a][b][4 * e + 3]};
     }
     __syncthreads();
     if (part) {
@@ -552,6 +624,9 @@ hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const E
 // side, of the weight all of block l / 16, of the activations 16 values of block l / 32 and 16 of block 2 + l / 32.  The j-th
 // instruction takes the j-th block of each of the four groups, so that a lane's four loads of the weight are 64 bytes in a
 // row; both sides' scales are those of block l / 16, a byte of one word.
+//
+// Bound by the weight's bytes and one latency each of loading, joining and storing: one token by 2 x 8192 gated rows of 4096 terms
+// (35.7 MB) in 8.9 us, by 8192 rows (17.8 MB) in 5.7.
 constexpr int kFewWaves = 8;
 
 template <int MT, int H, bool GATED, typename O>
