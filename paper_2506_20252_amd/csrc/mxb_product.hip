@@ -620,14 +620,23 @@ hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const E
 // ---- few tokens ----------------------------------------------------------------------------------------------
 //
 // A workgroup computes 16 * MT tokens by 16 * H columns (gated: 16 * 2 H rows of the weight); its waves take 512 terms (four
-// groups) in turn.  An instruction of 16 x 16 x 128 takes four blocks of 16 rows: lane l has row l mod 16 of either
-// side, of the weight all of block l / 16, of the activations 16 values of block l / 32 and 16 of block 2 + l / 32.  The j-th
-// instruction takes the j-th block of each of the four groups, so that a lane's four loads of the weight are 64 bytes in a
-// row; both sides' scales are those of block l / 16, a byte of one word.
+// groups) in turn, a group an instruction of 16 x 16 x 128: lane l has row l mod 16 of either side, of the weight all of
+// block l / 16, of the activations 16 values of block l / 32 and 16 of block 2 + l / 32, so that a load takes 64 bytes in a row of
+// each of 16 rows.  Scales come a group's word a lane, in one load for the four groups, and are turned round between the lanes.
 //
 // Bound by the weight's bytes and one latency each of loading, joining and storing: one token by 2 x 8192 gated rows of 4096 terms
-// (35.7 MB) in 8.9 us, by 8192 rows (17.8 MB) in 5.7.
+// (35.7 MB) in 8.8 us, by 8192 rows (17.8 MB) in 5.6; by 2 x 28672 of 8192 (250 MB) in 55, 4.6 TB/s.  A lane with 64 bytes in a row of
+// the weight instead: 8.9, 5.7 and 56.
 constexpr int kFewWaves = 8;
+
+// Of four words of lanes l, l + 16, l + 32 and l + 48 the byte l / 16 of each, in order.
+__device__ __forceinline__ int turn_bytes(int w) {
+  const int quarter = threadIdx.x % 64 / 16;
+  const auto a = __builtin_amdgcn_permlane16_swap(w, w, false, false);  // of quarters 0 and 2; of 1 and 3
+  const int v = __builtin_amdgcn_perm(a[1], a[0], quarter & 1 ? 0x07030501 : 0x06020400);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);  // of quarters 0 and 1; of 2 and 3
+  return __builtin_amdgcn_perm(b[1], b[0], quarter & 2 ? 0x07060302 : 0x05040100);
+}
 
 template <int MT, int H, bool GATED, typename O>
 __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, int64_t m, int64_t n, int groups, int64_t tiles_n,
@@ -642,13 +651,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
 #pragma unroll
   for (int y = 0; y < MT; ++y) {
     const int64_t i = min(i0 + 16 * y + lane % 16, m - 1);
-    px[y] = x.codes + i * 2 * pitch + lane / 16 % 2 * 16;
+    px[y] = x.codes + i * 2 * pitch + quarter * 16;
     qx[y] = x.scales + i * (pitch / 16);
   }
 #pragma unroll
   for (int z = 0; z < NT; ++z) {
     const int64_t j = min(j0 + 16 * (z % H) + lane % 16, n - 1) + (z < H ? 0 : n);
-    pw[z] = w.codes + j * pitch;
+    pw[z] = w.codes + j * pitch + quarter * 16;
     qw[z] = w.scales + j * (pitch / 16);
   }
 
@@ -666,15 +675,14 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
     v4i x[MT][J][2], w[NT][4];
     int sw[NT], sx[MT];
   };
-  auto load_x = [&](Turn& c, int g0, int j0) {
-    // What is beyond the last group is that one again, and counts as zeros.
-    const int lo = min(g0 + quarter / 2, groups - 1), hi = min(g0 + 2 + quarter / 2, groups - 1);
+  auto load_x = [&](Turn& c, int g0, int j0) {  // beyond the last group that one again, not multiplied
 #pragma unroll
     for (int y = 0; y < MT; ++y)
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        c.x[y][j][0] = ldg<v4i, false>((const char*)px[y] + (int64_t)lo * 128 + (j0 + j) * 32);
-        c.x[y][j][1] = ldg<v4i, false>((const char*)px[y] + (int64_t)hi * 128 + (j0 + j) * 32);
+        const char* p = (const char*)px[y] + (int64_t)min(g0 + j0 + j, groups - 1) * 128;
+        c.x[y][j][0] = ldg<v4i, false>(p);
+        c.x[y][j][1] = ldg<v4i, false>(p + 64);
       }
   };
   auto load = [&](Turn& c, int g0) {
@@ -687,26 +695,24 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
 #pragma unroll
     for (int z = 0; z < NT; ++z)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) c.w[z][j] = ldg<v4i, false>((const char*)pw[z] + (int64_t)g * 64 + j * 16);
+      for (int j = 0; j < 4; ++j) c.w[z][j] = ldg<v4i, false>((const char*)pw[z] + (int64_t)min(g0 + j, groups - 1) * 64);
     __builtin_amdgcn_sched_barrier(0);
   };
   auto multiply = [&](Turn& c, int g0) {
-    const bool in = g0 + quarter < groups, lo_in = g0 + quarter / 2 < groups, hi_in = g0 + 2 + quarter / 2 < groups;
 #pragma unroll
-    for (int z = 0; z < NT; ++z) c.sw[z] = in ? c.sw[z] : 0;
+    for (int z = 0; z < NT; ++z) c.sw[z] = turn_bytes(c.sw[z]);
 #pragma unroll
-    for (int y = 0; y < MT; ++y) c.sx[y] = in ? c.sx[y] : 0;
+    for (int y = 0; y < MT; ++y) c.sx[y] = turn_bytes(c.sx[y]);
     auto step = [&](auto which) {
       constexpr int I = decltype(which)::value;
       if constexpr (I == J) load_x(c, g0, J);
+      if (g0 + I >= groups) return;
 #pragma unroll
-      for (int y = 0; y < MT; ++y) {
-        const v4i none = {0, 0, 0, 0};
-        const v8i fx = frag(lo_in ? c.x[y][I % J][0] : none, hi_in ? c.x[y][I % J][1] : none);
+      for (int y = 0; y < MT; ++y)
 #pragma unroll
         for (int z = 0; z < NT; ++z)
-          acc[y][z] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(c.w[z][I]), fx, acc[y][z], 4, 0, I, c.sw[z], I, c.sx[y]);
-      }
+          acc[y][z] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(frag(c.w[z][I]), frag(c.x[y][I % J][0], c.x[y][I % J][1]), acc[y][z],
+                                                                      4, 0, I, c.sw[z], I, c.sx[y]);
     };
     step(Int<0>{});
     step(Int<1>{});
