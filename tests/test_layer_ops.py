@@ -610,7 +610,7 @@ def depth(cols):
 
 NORMS = [(1, 1), (3, 2), (2, 3), (5, 4), (3, 5), (1, 8), (300, 7), (70, 31), (9, 33), (4, 127), (65, 128), (7, 129), (2, 1000), (3, 2048),
          (1, 2049), (5, 4096), (3, 4100), (2, 8192), (1, 8200), (2, 16384), (2, 16385), (3, 32768), (1, 40001), (2049, 130), (2100, 4096), (2050, 1000),
-         (2048, 515), (5000, 16)]
+         (2048, 515), (5000, 16), (600, 2129), (513, 3000), (300, 9795), (270, 16383)]
 
 
 @gpu
@@ -714,6 +714,62 @@ def test_norm_in_place(cols, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("rows,cols", [(9000, 7), (5000, 333), (1500, 2129), (700, 16383), (600, 16391)])
+@pytest.mark.parametrize("dtype", [F32, B16])
+def test_norm_in_place_through_many_rows(rows, cols, dtype):
+    """More rows than go through at once, with ends that vectors are moved down from: the next row is read before this one is written."""
+    x, res, weight = values((rows, cols), 1, dtype), values((rows, cols), 2, dtype), values((cols,), 3)
+    want, total = ops.rms_norm(x, weight, 1e-5, res)
+    a, r = x.clone(), res.clone()
+    got, kept = ops.rms_norm(a, weight, 1e-5, r, total=a, out=r)
+    assert got is r and kept is a and torch.equal(got, want) and torch.equal(kept, total)
+    a = x.clone()
+    assert torch.equal(ops.rms_norm(a, weight, 1e-5, out=a), ops.rms_norm(x, weight, 1e-5))
+    dx, dw = ops.rms_norm_grad(res, x, weight, 1e-5, total)
+    for target in ("g", "more"):
+        g, more = res.clone(), total.clone()
+        got, dweight = ops.rms_norm_grad(g, x, weight, 1e-5, more, out=g if target == "g" else more)
+        assert torch.equal(got, dx) and torch.equal(dweight, dw)
+
+
+@gpu
+@pytest.mark.parametrize("cols", [33, 4096, 20001])
+def test_norm_of_one_tensor_in_two_places(cols):
+    """x its own residual, g the total's gradient too, a weight that starts inside another vector."""
+    x, g = values((70, cols), 1, B16), values((70, cols), 2, B16)
+    weight = values((cols + 1,), 3, B16)[1:]
+    out, total = ops.rms_norm(x, weight, 1e-5, x)
+    other = ops.rms_norm(x.clone(), weight.clone(), 1e-5, x.clone())
+    assert torch.equal(out, other[0]) and torch.equal(total, other[1])
+    both = x.clone()
+    out, total = ops.rms_norm(both, weight, 1e-5, both, total=both)
+    assert total is both and torch.equal(out, other[0]) and torch.equal(both, other[1])
+    want = ops.rms_norm_grad(g.clone(), x, weight.clone(), 1e-5, g.clone())
+    both = g.clone()
+    got = ops.rms_norm_grad(both, x, weight, 1e-5, both, out=both)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(5, 70, 300), (60, 140, 300), (300, 1500, 700), (1500, 1500, 300)])
+def test_rows_of_stored_matrices(m, n, k):
+    """Rows of a larger stored matrix are a stored matrix: as input, as weight and as output."""
+    x, w = ops.mxb_quantize(values((m + 7, k), 1)), ops.mx_quantize(values((2 * n + 5, k), 2))
+    part = ops.Mxb(x.codes[3:m + 3], x.scales[3:m + 3], k)
+    rows = ops.Mx(w.codes[5:], w.scales[5:], k)
+    own = ops.Mxb(part.codes.clone(), part.scales.clone(), k), ops.Mx(rows.codes.clone(), rows.scales.clone(), k)
+    assert torch.equal(ops.mxb_linear(part, rows), ops.mxb_linear(*own))
+    out = ops.Mxb(*(t.fill_(0x55) for t in ops.mxb_empty(m + 2, n)[:2]), n)
+    ops.gated(part, rows, "silu", ops.Mxb, out=ops.Mxb(out.codes[1:-1], out.scales[1:-1], n))
+    want = ops.gated(*own, "silu", ops.Mxb)
+    assert torch.equal(out.codes[1:-1], want.codes) and torch.equal(out.scales[1:-1], want.scales)
+    for t in out[:2]:
+        assert bool((t[0] == 0x55).all()) and bool((t[-1] == 0x55).all())
+    g = values((m, n), 3, B16)
+    assert torch.equal(ops.mxb_weight_grad(g, part), ops.mxb_weight_grad(g, own[0]))
+
+
+@gpu
 @pytest.mark.parametrize("cols", [40, 300, 20000])
 def test_norm_of_zero_rows_infinities_and_nan(cols):
     """A row of zeros gives zeros (NaN where eps is 0, as the formula does), what is not finite stays in its row, and blocks of
@@ -793,6 +849,27 @@ def test_graph_replays(name):
         assert all(torch.equal(a, b) for a, b in zip(flat(call()), want))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((junk == 0x77).all())
+
+
+@gpu
+def test_two_streams_at_once():
+    """Calls that run beside each other share nothing: each gives what it gives alone."""
+    calls = every_operator()
+    want = {name: [t.clone() for t in flat(call())] for name, call in calls.items()}
+    x, w = ops.mxb_quantize(values((1500, 1300), 1)), ops.mx_quantize(values((3000, 1300), 2))
+    calls["tiles"] = lambda s=None: ops.gated(x, w, "gelu", ops.Mxb, True, stream=s)
+    want["tiles"] = [t.clone() for t in flat(calls["tiles"]())]
+    torch.cuda.synchronize()
+    first, second = torch.cuda.Stream(), torch.cuda.Stream()
+    names = list(calls)
+    for shift in range(len(names)):
+        got = []
+        for i, name in enumerate(names):
+            other = names[(i + shift) % len(names)]
+            got += [(name, calls[name](first)), (other, calls[other](second))]
+        torch.cuda.synchronize()
+        for name, out in got:
+            assert all(torch.equal(a, b) for a, b in zip(flat(out), want[name])), (name, shift)
 
 
 @gpu
