@@ -29,6 +29,12 @@ __device__ __forceinline__ void cut(I cols, I last, I gap, F f) {
   else f(CutOf<kOne>{});
 }
 
+// Bytes from a row's start to its column `col`; without a sign where they fit, an address is a scalar and 32 bits.
+template <int BYTES>
+__device__ __forceinline__ uint32_t bytes_to(int col) { return (uint32_t)col * BYTES; }
+template <int BYTES>
+__device__ __forceinline__ int64_t bytes_to(int64_t col) { return col * BYTES; }
+
 // A lane's 8 columns from `col` of a row as they are in memory; nothing is done with what is loaded, so that a row's loads are
 // on their way together.  Columns behind the row's end are zero once they are widened.
 template <typename T>
@@ -39,7 +45,7 @@ template <typename T, bool SPLIT, Cut C, bool NT = false, typename I>
 __device__ __forceinline__ Raw<T> load_raw(const void* row, I col, I cols, I gap) {
   typedef typename T::vec4 V;
   const I n = cols - col;
-  const char* p = (const char*)row + col * T::kBytes;
+  const char* p = (const char*)row + bytes_to<T::kBytes>(col);
   if constexpr (C == kOne) {
     float v[8];
     load8<T, SPLIT, false, kFew>(p, n, gap, v);
@@ -85,7 +91,7 @@ __device__ __forceinline__ void widen(Elem e, const RawWeight& r, I col, I cols,
 }
 template <typename T, bool SPLIT, Cut C, bool NT = false, typename I>
 __device__ __forceinline__ void store_cols(void* row, I col, I cols, I gap, const float (&v)[8]) {
-  char* p = (char*)row + col * T::kBytes;
+  char* p = (char*)row + bytes_to<T::kBytes>(col);
   const I n = cols - col;
   if constexpr (C == kAll) store8<T, SPLIT, NT, kWhole>(p, n, gap, v);
   else if constexpr (C == kSome && !SPLIT) {
@@ -194,13 +200,15 @@ __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) 
   const int64_t step = (int64_t)gridDim.x * side;
   const Place<SPLIT, U> at(lanes);
   const int gap = at.gap();
+  // which of the rows beside each other; of lanes with several vectors a whole wave has one
+  const int mine = U > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / lanes) : threadIdx.x / lanes;
   const bool residual = a.residual.p != nullptr;
   auto all = [&](auto how) {
     constexpr Cut C = decltype(how)::value;
     Raw<X> x[U], r[U];
     RawWeight weight[U];
     auto fetch = [&](int64_t base) {
-      const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
+      const int64_t row = min(base + mine, a.rows - 1);
 #pragma unroll
       for (int u = 0; u < U; ++u) x[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), cols, gap);
       if (residual) {
@@ -214,8 +222,8 @@ __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) 
 #pragma unroll
     for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, a.weight, at(u), cols, gap);
     for (; base < a.rows; base += step, turn ^= 1) {
-      const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
-      const bool real = base + threadIdx.x / lanes < a.rows;
+      const int64_t row = min(base + mine, a.rows - 1);
+      const bool real = base + mine < a.rows;
       float t[U][8], sum[1] = {0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -274,20 +282,26 @@ __global__ __launch_bounds__(kNormMost) void norm_long_kernel(NormArgs a) {
 
 // With r = 1 / sqrt(mean(x^2) + eps):  out = total_grad + r (g w - x r^2 mean(g w x)),  dweight = the rows' sum of g x r.
 //
-// Bound by memory.  A row's loads are all on their way before its sums, and, where the registers suffice (up to 16 columns a
-// lane), the next row's before this row's results; the weight stays in registers then too.  Wider lanes load it, and the total's
-// gradient, where they use them.  8192 x 8192 bfloat16 with a total's gradient (537 MB) in 89 us with the parts' sum, 6.0 TB/s (97
-// without the total's gradient ahead), 16384 x 4096 in 97, 8192 x 2560 in 40, 10513 x 2129 in 59.
+// Bound by memory.  A row's loads are all on their way before its sums, and, where the registers suffice (AHEAD, up to 16
+// columns a lane), the next row's before this row's results; the weight stays in registers then too (KEEP).  Wider lanes load
+// it twice, the second time under the sums, and the total's gradient with the rest where that fits (EARLY: 4096 x 16384 in
+// 123 us, 147 with both after the sums, 175 with the next row's x and g before them).  8192 x 8192 bfloat16 with a total's
+// gradient (537 MB) in 89 us with the parts' sum, 6.0 TB/s (97 without that gradient ahead), 16384 x 4096 in 97, 8192 x 2560
+// in 40, 10513 x 2129 in 59.
 template <typename X, typename G, int U>
 __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= G::kBytes ? 3 : 2) void norm_grad_kernel(
     NormGradArgs a, int lanes, float* sums, int64_t pitch) {
-  constexpr bool SPLIT = Split<X, G>::value, AHEAD = X::kBytes + G::kBytes == 4 && U <= 2, KEEP = U <= 2;
+  constexpr bool SPLIT = Split<X, G>::value, AHEAD = X::kBytes + G::kBytes == 4 && U <= 2, KEEP = U <= 2,
+                 EARLY = KEEP || X::kBytes + G::kBytes == 4;
   __shared__ float part[2][2 * kNormGradMost / 64];
   __shared__ float joined[U == 1 ? 8 * kStripThreads : 1];
-  const int side = blockDim.x / lanes, cols = (int)a.cols;
+  const int side = blockDim.x / lanes;
+  int cols = (int)a.cols;
   const int64_t step = (int64_t)gridDim.x * side;
-  const Place<SPLIT, U> at(lanes);
+  Place<SPLIT, U> at(lanes);
   const int gap = at.gap();
+  // which of the rows beside each other; of lanes with several vectors a whole wave has one
+  const int mine = U > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / lanes) : threadIdx.x / lanes;
   float dw[U][8];
 #pragma unroll
   for (int u = 0; u < U; ++u)
@@ -304,13 +318,13 @@ __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= 
     Raw<X> x_raw[U];
     Raw<G> g_raw[U], t_raw[U];
     auto fetch = [&](int64_t base) {
-      const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
+      const int64_t row = min(base + mine, a.rows - 1);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         x_raw[u] = load_raw<X, SPLIT, C, true>(row_of<X>(a.x, row), at(u), cols, gap);
         g_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.g, row), at(u), cols, gap);
       }
-      if (KEEP && more) {
+      if (EARLY && more) {
 #pragma unroll
         for (int u = 0; u < U; ++u) t_raw[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), cols, gap);
       }
@@ -319,8 +333,10 @@ __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= 
     int64_t base = (int64_t)blockIdx.x * side;
     fetch(base);
     for (; base < a.rows; base += step, turn ^= 1) {
-      const int64_t row = min(base + threadIdx.x / lanes, a.rows - 1);
-      const bool real = base + threadIdx.x / lanes < a.rows;
+      // what follows from these is formed again in every turn, and not kept
+      if constexpr (U > 1 && !AHEAD) asm volatile("" : "+s"(cols), "+v"(at.lane));
+      const int64_t row = min(base + mine, a.rows - 1);
+      const bool real = base + mine < a.rows;
       float x[U][8], g[U][8], s[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -336,12 +352,16 @@ __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= 
 #pragma unroll
       for (int u = 0; u < U; ++u) t_now[u] = t_raw[u];
       if (AHEAD && base + step < a.rows) fetch(base + step);
+      if constexpr (!KEEP && EARLY) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), cols, gap);
+      }
       sum_of_row(s, lanes, part[turn]);
       const float n = (float)cols, r = rsqrtf(s[0] / n + a.eps), k = r * r * (s[1] / n);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float w[8], d[8];
-        if (!KEEP) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), cols, gap);
+        if (!EARLY) weight[u] = load_raw<SPLIT, C>(a.weight_dtype, again(a.weight), at(u), cols, gap);
         widen<SPLIT, C>(a.weight_dtype, weight[u], at(u), cols, gap, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -349,7 +369,7 @@ __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= 
           dw[u][i] += real ? g[u][i] * (x[u][i] * r) : 0.0f;
         }
         if (more) {
-          if (!KEEP) t_now[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), cols, gap);
+          if (!EARLY) t_now[u] = load_raw<G, SPLIT, C, true>(row_of<G>(a.total_grad, row), at(u), cols, gap);
           float t[8];
           widen<G, SPLIT, C>(t_now[u], at(u), cols, gap, t);
 #pragma unroll
