@@ -659,7 +659,7 @@ def gated(x, w, activation="silu", dtype=torch.bfloat16, checkpoint=False, out=N
     n, act = rows // 2, _activation(activation)
     out, address, stride, code, codes, scales, tensors = _result(out, m, n, dtype, x_codes, "gated", stream)
     saved = saved_codes = saved_scales = None
-    if checkpoint is not False:
+    if checkpoint is not False and checkpoint is not None:
         saved = _blocks_out(None if checkpoint is True else checkpoint, 2 * m, n, x_codes, "checkpoint", stream)
         saved_codes, saved_scales = saved.codes.data_ptr(), saved.scales.data_ptr()
         if checkpoint is not True:

@@ -74,6 +74,8 @@ static void check_plan(const NormPlan& p, int64_t rows, int64_t units, int most,
   CHECK(p.threads % p.lanes == 0 && p.threads % 64 == 0 && p.threads <= most, "%lld %lld: %d of %d", r, u, p.threads, p.lanes);
   CHECK(p.vectors == 0 ? units > (int64_t)most * vectors : (int64_t)p.lanes * p.vectors >= units && p.vectors <= vectors, "%lld %lld: %d x %d", r, u,
         p.lanes, p.vectors);
+  // a wave is of one row where lanes have several vectors
+  CHECK(p.vectors < 2 || p.lanes % 64 == 0, "%lld %lld: %d x %d", r, u, p.lanes, p.vectors);
   CHECK(p.wgs >= 1 && p.wgs * p.threads < kLanes, "%lld %lld: %lld", r, u, (long long)p.wgs);
 }
 

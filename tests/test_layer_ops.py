@@ -433,6 +433,15 @@ def test_gated(m, n, k, name):
 
 
 @gpu
+def test_gated_without_a_checkpoint():
+    q, m = ops.mxb_quantize(values((4, 40), 1)), ops.mx_quantize(values((6, 40), 2))
+    want, kept = ops.gated(q, m, checkpoint=True)
+    assert type(kept) is ops.Mxb
+    for none in (False, None):
+        assert torch.equal(ops.gated(q, m, checkpoint=none), want)
+
+
+@gpu
 @pytest.mark.parametrize("m,n", [(1500, 1501), (2900, 2899), (700, 300)])  # every size of tile
 @pytest.mark.parametrize("k", [1030, 1160, 1290, 1420, 2430])  # 9, 10, 11, 12 and 19 groups: every rest of the loop by four
 def test_products_through_many_columns_of_tiles(m, n, k):
