@@ -286,15 +286,15 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
   const uint8_t *codes_w = w.codes + jb * w_pitch, *scales_w = w.scales + jb * s_pitch;
   const uint8_t *codes_x = x.codes + i0 * x_pitch, *scales_x = x.scales + i0 * s_pitch;
 
-  // A step's loads in the order in which they are given out: the tokens' codes, then half of what the pair needs.
-  constexpr int HALF = LOADS_W / 2 + 1;
+  // A pair's loads: the weight's codes, both sides' scales.
+  constexpr int LOADS_P = LOADS_W + 2, THIRD = LOADS_P / 3;
+  static_assert(THIRD * 3 == LOADS_P, "");
   auto fetch_x = [&](Step& l, int g, int u) { load_to_lds16(codes_x + (int64_t)g * 128, at_x[u], l.codes + (u * W + wave) * 1024); };
   auto fetch_w = [&](Pair& l, int g, int u, uint32_t back, uint32_t sback) {
-    if (u % HALF < LOADS_W / 2) {
-      const int v = u / HALF * (LOADS_W / 2) + u % HALF;
-      const uint8_t* p = codes_w + (int64_t)g * 64 + (second((v * W + wave) * 8) ? n * w_pitch : 0);
-      load_to_lds16(p, at_w[v] - back, l.codes + (v * W + wave) * 1024);
-    } else if (u < HALF) {
+    if (u < LOADS_W) {
+      const uint8_t* p = codes_w + (int64_t)g * 64 + (second((u * W + wave) * 8) ? n * w_pitch : 0);
+      load_to_lds16(p, at_w[u] - back, l.codes + (u * W + wave) * 1024);
+    } else if (u == LOADS_W) {
       load_to_lds4(scales_w + (int64_t)g * 4 + (second(wave * 32) ? n * s_pitch : 0), sat_w - sback, l.w_scales + wave * 256);
     } else {
       load_to_lds4(scales_x + (int64_t)g * 4, sat_x - sback, l.x_scales + wave * 256);
@@ -366,23 +366,27 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
   Scales s0, s1;
   // Step g, the H-th of pair `p`, out of `l`; the first instructions' blocks are in c0 and the scales in `s`.  Before the second
   // ones the next step has arrived and this step's LDS has been read by all, so both the next first blocks and what
-  // comes two steps later come in under them, with half of a pair: the second half of `other`, or, once `p` is read, the first
-  // half of what follows `other` in its place.  That half is the last to be on its way, and only the next step but one needs it.
-  // No branch: beyond the last it is fetched again.
+  // comes two steps later come in under them, with a third of a pair.  A pair's thirds follow each other, the first in the place of
+  // `p` once that is read, two in that of `other` under the next step's first and second instructions: for 1500 tokens by 4096 rows of
+  // 4096 terms 30 us, 33 with halves under the second ones alone.  What came of the pair by the barrier after that is not
+  // waited for there.  No branch: beyond the last it is fetched again.
   auto step = [&](Pair& p, Step& l, Pair& other, const Step& next_l, auto which, const Scales& s, Scales& next_s, int g) {
     constexpr int H = decltype(which)::value;
     asm volatile("" : "+v"(from_w), "+v"(from_x));
-    multiply(c0, s, Int<0>{}, [&](int slot) { read_share(slot, [&](int i) { read(p, l, H, 1, i, c1); }); });
-    meet<H == 0 ? HALF : 0>();
     const int gx = min(g + 2, groups - 1), gw = min(g + 2 + H, (groups - 1) / 2 * 2);
     const uint32_t back = gw + 1 < groups ? 0 : (piece >= 4 ? 64 : 0), sback = gw + 1 < groups ? 0 : lane % 2 * 4;
+    multiply(c0, s, Int<0>{}, [&](int slot) {
+      read_share(slot, [&](int i) { read(p, l, H, 1, i, c1); });
+      if constexpr (H == 0) share(slot, THIRD, [&](int i) { fetch_w(other, gw, THIRD + i, back, sback); });
+    });
+    meet<H == 0 ? 2 * THIRD : 0>();
     const Pair& next_p = H ? other : p;
     multiply(c1, s, Int<1>{}, [&](int slot) {
       if (slot == 0) read_scales(next_p, 1 - H, next_s);
       read_share(slot, [&](int i) { read(next_p, next_l, 1 - H, 0, i, c0); });
-      share(slot, LOADS_X + HALF, [&](int i) {
+      share(slot, LOADS_X + THIRD, [&](int i) {
         if (i < LOADS_X) fetch_x(l, gx, i);
-        else fetch_w(H ? p : other, gw, (H ? 0 : HALF) + i - LOADS_X, back, sback);
+        else fetch_w(H ? p : other, gw, (H ? 0 : 2 * THIRD) + i - LOADS_X, back, sback);
       });
     });
   };
@@ -391,13 +395,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
 #pragma unroll
     for (int u = begin; u < end; ++u) fetch_w(l, g, u, back, sback);
   };
-  first(pair0, 0, 0, 2 * HALF);
+  first(pair0, 0, 0, LOADS_P);
 #pragma unroll
   for (int u = 0; u < LOADS_X; ++u) fetch_x(step0, 0, u);
   meet<0>();
 #pragma unroll
   for (int u = 0; u < LOADS_X; ++u) fetch_x(step1, min(1, groups - 1), u);
-  first(pair1, min(2, (groups - 1) / 2 * 2), 0, HALF);
+  first(pair1, min(2, (groups - 1) / 2 * 2), 0, THIRD);
   read_scales(pair0, 0, s0);
 #pragma unroll
   for (int i = 0; i < READS; ++i) read(pair0, step0, 0, 0, i, c0);
