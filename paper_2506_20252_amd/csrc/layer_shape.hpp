@@ -73,8 +73,9 @@ inline NormGradPlan norm_grad_plan(int64_t rows, int64_t cols) {
 // parts of the terms).
 //
 // The largest of the first two that gives more than half of the 256 CUs one; else 64 x 64 as long as each CU has at most one.
-// us with 64 x 64, 64 x 128, 128 x 128: 9.1, 11.1, 14.8 (64 tokens, 4096 rows and terms: 64, 32, 32 tiles), 13.4, 16.8, 20.5 (256 tokens: 256,
-// 128, 64), 21.6, 20.2, 21.9 (512: 512, 256, 128), 10.1, 7.1, 8.1 (1001 tokens, 2000 rows, 1333 terms: 512, 256, 128).
+// us with 64 x 64, 64 x 128, 128 x 128: 8.9, 10.8, 15.1 (64 tokens, 4096 rows and terms: 64, 32, 32 tiles), 13.1, 16.4, 21.9 (256
+// tokens: 256, 128, 64), 20.1, 19.2, 22.7 (512: 512, 256, 128), 34, 31, 24 (1024: 1024, 512, 256), 9.4, 6.6, 8.6 (1001 tokens, 2000 rows,
+// 1333 terms: 512, 256, 128).
 inline int64_t layer_tiles(int64_t m, int64_t n, int rows_x, int rows_w) { return (int64_t)(ceil_div(m, rows_x) * ceil_div(n, rows_w)); }
 inline int layer_tile(int64_t m, int64_t n) {
   if (layer_tiles(m, n, 256, 256) > 128) return 256;

@@ -429,7 +429,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(MxbMat x, MxMat w
 // the terms each, in LDS of their own, and their sums are added in order at the end; D steps are in LDS or on their way
 // at once.  The weight's rows come as half lines then, 64 bytes a step, at place piece ^ (row / 4 mod 4) of a row's four (a
 // row is a quarter of the banks).  Every wave has the same number of loads a step, and waits for those of the next step alone.
-// Bound by the loads' latency: 64 tokens by 4096 rows of 4096 terms in 9.1 us, 1001 by 2000 of 1333 in 7.1, of which starting,
+// Bound by the loads' latency: 64 tokens by 4096 rows of 4096 terms in 8.9 us, 1001 by 2000 of 1333 in 6.6, of which starting,
 // filling LDS and leaving take five.
 template <int FN, int FM, int WN, int WM>
 struct Stage {
