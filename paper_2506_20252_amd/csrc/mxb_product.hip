@@ -59,18 +59,19 @@ __device__ __forceinline__ void meet() {
 }
 
 // Loads of 16 bytes a lane from base + at, and of 4 bytes from p, into LDS, lane after lane from `to` on.  Written out: the
-// compiler's own ones make it wait for all of them before LDS is read, in every turn of the loop.
+// compiler's own ones make it wait for all of them before LDS is read, in every turn of the loop.  m0, which says where in LDS,
+// is an operand: the compiler writes it and knows that it did.
 __device__ __forceinline__ uint32_t lds_place(const uint8_t* to) {
   return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint8_t*)to);
 }
 __device__ __forceinline__ void load_to_lds16(const uint8_t* base, uint32_t at, const uint8_t* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(lds_place(to)), "v"(at), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(const uint8_t* base, uint32_t at, const uint8_t* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_place(to)), "v"(at), "s"(base) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(lds_place(to)), "v"(at), "s"(base) : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(const uint8_t* p, const uint8_t* to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_place(to)), "v"(p) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(lds_place(to)), "v"(p) : "memory");
 }
 
 // ---- tiles through LDS ---------------------------------------------------------------------------------------
