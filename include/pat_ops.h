@@ -176,9 +176,10 @@ pat_status_t pat_dropout(const void* x, int64_t x_stride, const void* residual, 
 /*
  * Quantises x[rows][cols] (PAT_FLOAT32 or PAT_BFLOAT16).  Per block: s = the least,
  * from 0, for which no magnitude is above 3.75 * 2^(s - 127); code = the nearest value
- * of x * 2^(127 - s), ties to the even code: half a step, 2^-4 of the value at most, down
- * to 2^-8 of the block's largest, and 2^-10 of the scale below.  A block that holds an
- * infinity or a NaN gets s = 255 and stands for NaN in whole.
+ * of x * 2^(127 - s), ties to the even code.  Off by half a step at most: 2^-4 of the value
+ * from 2^-6 * 2^(s - 127) on, which is, where s > 0, at least down to 1/120 of the block's
+ * largest magnitude, and 2^-10 * 2^(s - 127) below.  A block that holds an infinity or a
+ * NaN gets s = 255 and stands for NaN in whole.
  */
 pat_status_t pat_mxb_quantize(const void* x, int64_t x_stride, size_t rows, size_t cols, pat_dtype_t dtype, void* codes,
                               void* scales, hipStream_t stream);
@@ -246,7 +247,10 @@ pat_status_t pat_gated_grad(const void* g, int64_t g_stride, pat_dtype_t g_dtype
  * out[r][c] = t[r][c] * weight[c] / sqrt(mean over c of t[r][c]^2 + eps), eps >= 0.
  * x, residual and total: dtype; weight: cols elements of weight_dtype; the output:
  * `out` of out_dtype, or, where out is NULL, 8-bit blocks in out_codes and out_scales.
- * Squares are summed in float32 (values above 2^63 overflow).
+ * Squares are summed in float32, to its full precision in rows whose sum of squares is
+ * at most 2^127 and whose mean of squares plus eps is at least 2^-126.  Sums that
+ * overflow, from 2^128 on, give a row of zeros; squares that vanish, below 2^-149, count
+ * as zero, so that with eps = 0 a row of such values gives infinities or NaN.
  * In place: total or out == x, total or out == residual, with equal strides and types;
  * total and out are two buffers.
  */
@@ -260,8 +264,9 @@ pat_status_t pat_rms_norm(const void* x, int64_t x_stride, const void* residual,
  *   out[r][c] = r * (g * weight - x * r^2 * mean over c of g * weight * x) + total_grad[r][c],
  *   dweight[c] = sum over rows of g * x * r  (PAT_FLOAT32, cols elements, 4-byte aligned).
  * out is the gradient of x and of the residual alike; total_grad (NULL: none) is what
- * reaches the total from elsewhere.  g, total_grad and out: dtype; x: x_dtype.  With no
- * rows dweight is zero.  In place: out == g or out == total_grad with equal strides.
+ * reaches the total from elsewhere.  g, total_grad and out: dtype; x: x_dtype.  Sums are
+ * float32's, as the norm's: beside x^2, the magnitudes of g * weight * x sum to 2^127 at
+ * most in a row.  With no rows dweight is zero.  In place: out == g or out == total_grad with equal strides.
  * Fewer than 2^28 rows, 2^26 columns (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_rms_norm_grad(const void* g, int64_t g_stride, pat_dtype_t dtype, const void* x, int64_t x_stride,
