@@ -94,6 +94,62 @@ def test_oracle_rounding_is_what_the_header_says():
     assert abs(got[0, 1] / row[0, 1] - 1) > 0.11  # 2^-8 of the largest is below where 2^-4 of a value holds
 
 
+def source_of(name, function):
+    with open(os.path.join(B.CSRC, name)) as f:
+        return re.search(rf"\n[^\n]*\b{function}\(.*?\n}}\n", f.read(), re.S)[0]
+
+
+def comment_of(name, function):
+    with open(os.path.join(B.CSRC, name)) as f:
+        return re.search(rf"((?://[^\n]*\n)+)[^\n]*\b{function}\(", f.read())[1].replace("\n// ", " ")
+
+
+def normal_below(a, rcp_off=0, exp_off=0):
+    """The kernels' P(a) = (1 + erf(a / sqrt 2)) / 2 in float32 step by step, with the source's coefficients; 1 / x and 2^x right or
+    a unit off.  Fused multiply-adds through float64, whose own rounding is 2^-29 of float32's."""
+    f = np.float32
+    text = source_of("layer_device.hpp", "normal_below")
+    slope = f(re.search(r"1\.0f \+ ([\d.]+)f \* fabsf", text)[1])
+    c = [f(v) for v in [re.search(r"float p = (-?[\d.]+)f;", text)[1], *re.findall(r"fmaf\(p, t, (-?[\d.]+)f\)", text)]]
+    assert len(c) == 7
+
+    def unit(v, off):
+        return np.nextafter(v, f(np.inf) * off) if off else v
+
+    t = unit((1 / (1 + slope.astype(np.float64) * np.abs(a)).astype(f).astype(np.float64)).astype(f), rcp_off)
+    p = np.full_like(t, c[0])
+    for v in c[1:]:
+        p = (p.astype(np.float64) * t + np.float64(v)).astype(f)
+    log2e = f(1.44269504088896341)
+    bell = unit(np.exp2((f(-0.5) * log2e * a * a).astype(np.float64)).astype(f), exp_off)
+    q = f(0.5) * (p * t) * bell
+    assert q.dtype == f
+    return np.where(a >= 0, f(1) - q, q)
+
+
+def normal(a):
+    return 0.5 * torch.erfc(torch.from_numpy(-a / np.sqrt(2))).numpy()
+
+
+def normal_grid():
+    near = np.exp(np.linspace(np.log(1e-9), 0, 200001))
+    a = np.concatenate((near, np.linspace(0, 13, 1000001))).astype(np.float32)
+    return np.concatenate((a, -a))
+
+
+def test_the_normal_distribution_is_as_close_as_its_comment_says():
+    text = comment_of("layer_device.hpp", "normal_below")
+    exact, off = (float(re.search(p, text)[1]) for p in (r"by ([\d.]+) \* 2\^-24 with float32's", r"([\d.]+) \* 2\^-24 where the"))
+    near, tail = (float(re.search(rf"([\d.e-]+) down to -{e}\b", text)[1]) for e in (5, 13))
+    a = normal_grid()
+    want = normal(a.astype(np.float64))
+    for r in (-1, 0, 1):
+        for e in (-1, 0, 1):
+            error = np.abs(normal_below(a, r, e) - want)
+            assert error.max() <= (off if r or e else exact) * U
+            assert np.all(error[a < 0] <= (tail * want)[a < 0]) and np.all(error[(a < 0) & (a >= -5)] <= (near * want)[(a < 0) & (a >= -5)])
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
@@ -152,3 +208,38 @@ def test_norm_beyond_its_range(cols):
     small = f64(ops.rms_norm(x, one, 2.0**-20)[1])
     want = L.rms_norm(f64(x), 1.0, 2.0**-20)[1]
     assert np.all(np.abs(small - want) <= 8 * U * want)
+
+
+@gpu
+@pytest.mark.parametrize("m", [8, 40])  # few tokens; tiles
+@pytest.mark.parametrize("low,high", [(112, 115), (115, 119), (119, 122)])
+def test_gelu_is_as_close_as_its_distribution(m, low, high):
+    """Projections that are exact (products are multiples of 2^-10 of the scales, and fewer than 2^24 of these in a sum) and b = 1, so
+    that the output is a P(a) alone, rounded once.  P is off by 6.6 u at most: t by 2 u (its denominator's rounding and 1 / x), of
+    which 1.57 times; the polynomial by 2.5 u (u, u/2, u/2, u/4, u/4, u/32) and p t, the bell, the two products by u each at
+    most, of which half; 1 - q by u/2; the fit by 0.15 u.  Below -1 it is also off by 1.1e-4 of itself at most, down to -13."""
+    n, k = 3000, 128
+    g = np.random.default_rng(low)
+    x, w = np.zeros((m, k)), np.zeros((2 * n, k))
+    x[:, :96] = L.CODES[g.integers(0, 0x48, size=(m, 96))] * g.choice([-1, 1], size=(m, 96))
+    x[:, [0, 32, 64]] = 3.75  # every block's scale is one
+    x[:, 96] = 1.0
+    size = np.exp2(g.integers(low, high, size=(n, 1)) - 122.0)
+    w[:n, :96] = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])[g.integers(0, 8, size=(n, 96))] * g.choice([-1, 1], size=(n, 96)) * size
+    w[n:, 96] = 1.0
+    x8, w4 = (f(torch.from_numpy(v).float().cuda()) for f, v in ((ops.mxb_quantize, x), (ops.mx_quantize, w)))
+    assert np.array_equal(f64(ops.mxb_dequantize(x8, F32)), x) and np.array_equal(f64(ops.mx_dequantize(w4, F32)), w)
+    a = x @ w[:n].T
+    h = f64(ops.gated(x8, w4, "gelu", F32))
+    p = normal(a)
+    off = np.abs(h - a * p)
+    assert np.all(off <= np.abs(a) * (6.6 + 1) * U + 2.0**-149)
+    tail = (a > -13) & (a < -1)
+    assert np.all(off[tail] <= 1.1e-4 * np.abs(a * p)[tail] + 2.0**-149)
+    assert low < 119 or np.count_nonzero(tail & (a < -5)) > 1000
+    silu = f64(ops.gated(x8, w4, "silu", F32))
+    want = a / (1 + np.exp(-a))  # the oracle's tanh has no relative exactness far out
+    # e^-a: its argument a log2 e is off by 0.23 u for the constant and u for the product, relatively, so e^-a by 1.23 |a| u; 2^x,
+    # 1 + e, 1 / x and a s by 8 u together.  From e^-a = 2^126 on, a = -87.4, its reciprocal is no normal number, and zero from
+    # 2^128 on: off by 87.4 * 2^-126 < 2^-119 at most.
+    assert np.all(np.abs(silu - want) <= U * (1.23 * np.abs(a) + 8) * np.abs(want) + 2.0**-119)
