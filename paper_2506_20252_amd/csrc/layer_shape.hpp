@@ -67,6 +67,20 @@ inline NormGradPlan norm_grad_plan(int64_t rows, int64_t cols) {
   return p;
 }
 
+// Their workspace: the parts, where there are several or rows are long, as floats from its start, then two floats a row where
+// rows are long.
+struct NormGradSpace {
+  int64_t parts, rows_at;  // floats; the rows' first
+  size_t bytes;
+};
+inline NormGradSpace norm_grad_space(const NormGradPlan& p, int64_t rows) {
+  NormGradSpace s;
+  s.parts = p.wgs > 1 || p.vectors == 0 ? p.wgs * p.pitch : 0;
+  s.rows_at = s.parts;
+  s.bytes = (size_t)(s.parts + (p.vectors ? 0 : 2 * rows)) * 4;
+  return s;
+}
+
 // ---- products of 8-bit with 4-bit blocks ------------------------------------------------------------------------
 
 // Tiles of m tokens by n rows of the weight: 256 (256 x 256), 128 (128 x 128), 64 (64 tokens by 128 rows), or 32 (64 x 64, in two
@@ -91,6 +105,39 @@ constexpr int kFewLinear = 48, kFewGated = 32;
 inline int few_columns_sixteens(int64_t n) { return n <= 16 * 256 ? 1 : n <= 32 * 256 ? 2 : 4; }
 inline int64_t few_band(int64_t m, int64_t tiles_n, int64_t tokens) {
   return std::min(m, std::max<int64_t>(1, (((int64_t)1 << 22) - 1) / tiles_n) * tokens);
+}
+
+// A tile's tokens, its rows of the weight, its workgroup's lanes.
+constexpr int tile_tokens(int tile) { return tile < 128 ? 64 : tile; }
+constexpr int tile_rows(int tile) { return tile == 32 ? 64 : tile == 64 ? 128 : tile; }
+constexpr int tile_threads(int tile) { return tile == 256 ? 512 : 256; }
+constexpr int kFewWaves = 8;
+
+// How x w^T is launched, for n columns of the output (`gated`: 2 n rows of the weight).  tile == 0: few_kernel, 16 * `tokens` by
+// 16 * `columns` values of the output a workgroup.  `blocks`: something leaves in 8-bit blocks, which are filled up to 128
+// columns.  `tiles_n` workgroups beside each other, `band` tokens a launch, `wgs` workgroups in the largest one.
+struct ProductPlan {
+  int tile, tokens, columns, threads;
+  int64_t tiles_n, band, wgs;
+};
+inline ProductPlan product_plan(int64_t m, int64_t n, int64_t k, bool gated, bool blocks) {
+  ProductPlan p{};
+  const int64_t width = blocks ? groups_of(n) * 128 : n;
+  if (k > 0 && m > (gated ? kFewGated : kFewLinear)) {
+    p.tile = layer_tile(m, gated ? 2 * n : n);
+    p.threads = tile_threads(p.tile);
+    p.tiles_n = (int64_t)ceil_div(width, gated ? tile_rows(p.tile) / 2 : tile_rows(p.tile));
+    p.band = m;
+    p.wgs = (int64_t)ceil_div(ceil_div(m, tile_tokens(p.tile)) * p.tiles_n, 8) * 8;  // the same for each XCD
+    return p;
+  }
+  p.tokens = m <= 16 ? 1 : m <= 32 || gated ? 2 : 3;
+  p.columns = gated ? 2 : few_columns_sixteens(n);
+  p.threads = 64 * kFewWaves;
+  p.tiles_n = (int64_t)ceil_div(width, 16 * p.columns);
+  p.band = few_band(m, p.tiles_n, 16 * p.tokens);
+  p.wgs = (int64_t)ceil_div(p.band, 16 * p.tokens) * p.tiles_n;
+  return p;
 }
 
 }  // namespace pat

@@ -601,24 +601,22 @@ __global__ __launch_bounds__(64 * WN * WM * PARTS, WN * WM * PARTS == 8 ? 2 : 1)
 
 typedef void (*Product)(MxbMat, MxMat, int64_t, int64_t, int, int64_t, Epilogue);
 
-// `kernel` has tiles of M tokens by N rows of the weight, a workgroup of `threads` each.
-template <bool GATED, typename O>
-hipError_t run_tiles(Product kernel, int M, int N, int threads, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e,
+// `kernel` with the tiles of a plan, its shape S, in PARTS groups of waves.
+template <int TILE, typename S, int PARTS>
+hipError_t run_tiles(Product kernel, const ProductPlan& p, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e,
                      hipStream_t stream) {
-  const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);
-  const int64_t tiles_n = (int64_t)ceil_div(blocks ? groups_of(n) * 128 : n, GATED ? N / 2 : N);
-  const int64_t wgs = (int64_t)ceil_div(ceil_div(m, M) * tiles_n, 8) * 8;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, stream, x, w, m, n, (int)groups_of(k), tiles_n, e);
+  static_assert(S::M == tile_tokens(TILE) && S::N == tile_rows(TILE) && 64 * S::kWaves * PARTS == tile_threads(TILE), "");
+  hipLaunchKernelGGL(kernel, dim3((unsigned)p.wgs), dim3(p.threads), 0, stream, x, w, m, n, (int)groups_of(k), p.tiles_n, e);
   return hipGetLastError();
 }
 
 template <bool GATED, typename O>
-hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  switch (layer_tile(m, GATED ? 2 * n : n)) {
-    case 256: return run_tiles<GATED, O>(tile_kernel<4, 2, 2, 4, GATED, O>, 256, 256, 512, x, w, m, n, k, e, stream);
-    case 128: return run_tiles<GATED, O>(tile_kernel<2, 2, 2, 2, GATED, O>, 128, 128, 256, x, w, m, n, k, e, stream);
-    case 64: return run_tiles<GATED, O>(deep_kernel<2, 1, 2, 2, 1, 3, GATED, O>, 64, 128, 256, x, w, m, n, k, e, stream);
-    default: return run_tiles<GATED, O>(deep_kernel<2, 1, 1, 2, 2, 3, GATED, O>, 64, 64, 256, x, w, m, n, k, e, stream);
+hipError_t pick_tile(const ProductPlan& p, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  switch (p.tile) {
+    case 256: return run_tiles<256, Tile<4, 2, 2, 4>, 1>(tile_kernel<4, 2, 2, 4, GATED, O>, p, x, w, m, n, k, e, stream);
+    case 128: return run_tiles<128, Tile<2, 2, 2, 2>, 1>(tile_kernel<2, 2, 2, 2, GATED, O>, p, x, w, m, n, k, e, stream);
+    case 64: return run_tiles<64, Stage<2, 1, 2, 2>, 1>(deep_kernel<2, 1, 2, 2, 1, 3, GATED, O>, p, x, w, m, n, k, e, stream);
+    default: return run_tiles<32, Stage<2, 1, 1, 2>, 2>(deep_kernel<2, 1, 1, 2, 2, 3, GATED, O>, p, x, w, m, n, k, e, stream);
   }
 }
 
@@ -632,8 +630,6 @@ hipError_t pick_tile(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const E
 // Bound by the weight's bytes and one latency each of loading, joining and storing: one token by 2 x 8192 gated rows of 4096 terms
 // (35.7 MB) in 8.8 us, by 8192 rows (17.8 MB) in 5.6; by 2 x 28672 of 8192 (250 MB) in 55, 4.6 TB/s.  A lane with 64 bytes in a row of
 // the weight instead: 8.9, 5.7 and 56.
-constexpr int kFewWaves = 8;
-
 // Of four words of lanes l, l + 16, l + 32 and l + 48 the byte l / 16 of each, in order.
 __device__ __forceinline__ int turn_bytes(int w) {
   const int quarter = threadIdx.x % 64 / 16;
@@ -774,15 +770,12 @@ __global__ __launch_bounds__(64 * kFewWaves) void few_kernel(MxbMat x, MxMat w, 
 }
 
 template <int MT, int H, bool GATED, typename O>
-hipError_t run_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, Epilogue e, hipStream_t stream) {
-  const bool blocks = GATED && (O::kBytes == 1 || e.saved_a.codes);  // filled up to 128 columns
-  const int64_t groups = groups_of(k), out_groups = groups_of(n);
-  const int64_t tiles_n = (int64_t)ceil_div(blocks ? out_groups * 128 : n, 16 * H);
-  const int64_t band = few_band(m, tiles_n, 16 * MT);
+hipError_t run_few(const ProductPlan& p, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, Epilogue e, hipStream_t stream) {
+  const int64_t groups = groups_of(k), out_groups = groups_of(n), band = p.band;
   for (int64_t i = 0; i < m; i += band) {  // as many rows as a launch holds
     const int64_t here = std::min(band, m - i);
-    hipLaunchKernelGGL((few_kernel<MT, H, GATED, O>), dim3((unsigned)(ceil_div(here, 16 * MT) * tiles_n)), dim3(64 * kFewWaves),
-                       (size_t)kFewWaves * MT * H * (GATED ? 2 : 1) * 1024, stream, x, w, here, n, (int)groups, tiles_n, e);
+    hipLaunchKernelGGL((few_kernel<MT, H, GATED, O>), dim3((unsigned)(ceil_div(here, 16 * MT) * p.tiles_n)), dim3(p.threads),
+                       (size_t)kFewWaves * MT * H * (GATED ? 2 : 1) * 1024, stream, x, w, here, n, (int)groups, p.tiles_n, e);
     x.codes += band * groups * 128, x.scales += band * groups * 4;
     for (MxbOut* q : {&e.blocks, &e.saved_a, &e.saved_b})
       if (q->codes) q->codes += band * out_groups * 128, q->scales += band * out_groups * 4;
@@ -793,27 +786,29 @@ hipError_t run_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, Epilogue 
 }
 
 template <int MT, typename O>
-hipError_t pick_few(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  switch (few_columns_sixteens(n)) {
-    case 1: return run_few<MT, 1, false, O>(x, w, m, n, k, e, stream);
-    case 2: return run_few<MT, 2, false, O>(x, w, m, n, k, e, stream);
-    default: return run_few<MT, 4, false, O>(x, w, m, n, k, e, stream);
+hipError_t pick_few(const ProductPlan& p, MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
+  switch (p.columns) {
+    case 1: return run_few<MT, 1, false, O>(p, x, w, m, n, k, e, stream);
+    case 2: return run_few<MT, 2, false, O>(p, x, w, m, n, k, e, stream);
+    default: return run_few<MT, 4, false, O>(p, x, w, m, n, k, e, stream);
   }
 }
 
 template <typename O>
 hipError_t linear(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  if (m > kFewLinear && k > 0) return pick_tile<false, O>(x, w, m, n, k, e, stream);
-  if (m <= 16) return pick_few<1, O>(x, w, m, n, k, e, stream);
-  if (m <= 32) return pick_few<2, O>(x, w, m, n, k, e, stream);
-  return pick_few<3, O>(x, w, m, n, k, e, stream);
+  const ProductPlan p = product_plan(m, n, k, false, false);
+  if (p.tile) return pick_tile<false, O>(p, x, w, m, n, k, e, stream);
+  if (p.tokens == 1) return pick_few<1, O>(p, x, w, m, n, k, e, stream);
+  if (p.tokens == 2) return pick_few<2, O>(p, x, w, m, n, k, e, stream);
+  return pick_few<3, O>(p, x, w, m, n, k, e, stream);
 }
 
 template <typename O>
 hipError_t gated(MxbMat x, MxMat w, int64_t m, int64_t n, int64_t k, const Epilogue& e, hipStream_t stream) {
-  if (m > kFewGated && k > 0) return pick_tile<true, O>(x, w, m, n, k, e, stream);
-  if (m <= 16) return run_few<1, 2, true, O>(x, w, m, n, k, e, stream);
-  return run_few<2, 2, true, O>(x, w, m, n, k, e, stream);
+  const ProductPlan p = product_plan(m, n, k, true, O::kBytes == 1 || e.saved_a.codes);
+  if (p.tile) return pick_tile<true, O>(p, x, w, m, n, k, e, stream);
+  if (p.tokens == 1) return run_few<1, 2, true, O>(p, x, w, m, n, k, e, stream);
+  return run_few<2, 2, true, O>(p, x, w, m, n, k, e, stream);
 }
 
 }  // namespace

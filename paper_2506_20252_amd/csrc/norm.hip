@@ -523,7 +523,7 @@ hipError_t run_norm_grad(const NormGradArgs& a, void* workspace, hipStream_t str
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.wgs), dim3(p.threads), 0, stream, a, p.lanes, p.wgs > 1 ? parts : a.dweight,
                        p.pitch);
   } else {
-    v2f* rows = (v2f*)(parts + p.wgs * p.pitch);
+    v2f* rows = (v2f*)(parts + norm_grad_space(p, a.rows).rows_at);
     hipLaunchKernelGGL((norm_sums_kernel<X, G>), dim3((unsigned)std::min<int64_t>(a.rows, 1 << 20)), dim3(kStripThreads), 0, stream,
                        a, rows);
     hipLaunchKernelGGL((norm_strip_kernel<X, G>), dim3((unsigned)p.strips, (unsigned)p.wgs), dim3(kStripThreads), 0, stream, a, rows,
@@ -548,12 +548,7 @@ hipError_t launch_rms_norm(const NormArgs& a, hipStream_t stream) {
   return blocks ? run_norm<B16, Q8>(a, stream) : f32 ? run_norm<B16, F32>(a, stream) : run_norm<B16, B16>(a, stream);
 }
 
-// The parts' sums, then two floats a row where rows are long.
-size_t rms_norm_grad_workspace(int64_t rows, int64_t cols) {
-  const NormGradPlan p = norm_grad_plan(rows, cols);
-  if (p.vectors) return p.wgs > 1 ? (size_t)(p.wgs * p.pitch) * 4 : 0;
-  return (size_t)(p.wgs * p.pitch) * 4 + (size_t)rows * 8;
-}
+size_t rms_norm_grad_workspace(int64_t rows, int64_t cols) { return norm_grad_space(norm_grad_plan(rows, cols), rows).bytes; }
 
 hipError_t launch_rms_norm_grad(const NormGradArgs& a, void* workspace, hipStream_t stream) {
   if (a.rows == 0) {

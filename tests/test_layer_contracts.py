@@ -5,6 +5,8 @@ rules of how the kernels' sources are written.  Tolerances as in tests/test_laye
 import glob
 import os
 import re
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -12,12 +14,13 @@ import torch
 
 from oracle import layer as L
 from paper_2506_20252_amd import build as B
-from paper_2506_20252_amd import ops
+from paper_2506_20252_amd import ops, pat
 from test_layer_ops import blocks_within, depth
 from test_ops import E, F32, B16, U, f64, values, within
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 gpu = pytest.mark.gpu
+NAME = {F32: "float32", B16: "bfloat16"}
 
 
 def header():
@@ -150,6 +153,31 @@ def test_the_normal_distribution_is_as_close_as_its_comment_says():
             assert np.all(error[a < 0] <= (tail * want)[a < 0]) and np.all(error[(a < 0) & (a >= -5)] <= (near * want)[(a < 0) & (a >= -5)])
 
 
+@pytest.mark.skipif(shutil.which("g++") is None or not os.path.isdir("/opt/rocm/include/hip"),
+                    reason="no g++ or no HIP headers")
+def test_launches_and_workspaces_under_asan_ubsan(tmp_path):
+    """By the functions that the launches use."""
+    exe = tmp_path / "layer_plan_check"
+    cmd = ["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+           "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I", B.CSRC,
+           os.path.join(ROOT, "tests", "host", "layer_plan_check.cpp"), "-o", str(exe)]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    res = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, (res.stdout[-2000:], res.stderr[-2000:])
+    assert " 0 failures" in res.stdout
+
+
+def test_launches_take_their_sizes_from_what_is_checked():
+    """The kernels' sources cut nothing themselves: products are launched by product_plan, workspaces laid out by norm_grad_space."""
+    with open(os.path.join(B.CSRC, "mxb_product.hip")) as f:
+        product = f.read()
+    assert product.count("product_plan(m, n, k,") == 2 and product.count("hipLaunchKernelGGL") == 2
+    assert not re.search(r"\b(layer_tile|few_band|few_columns_sixteens|kFewGated|kFewLinear)\b", product)
+    with open(os.path.join(B.CSRC, "norm.hip")) as f:
+        norm = f.read()
+    assert norm.count("norm_grad_space(") == 2
+
+
 # ---------------------------------------------------------------------------
 # On the GPU
 # ---------------------------------------------------------------------------
@@ -243,3 +271,48 @@ def test_gelu_is_as_close_as_its_distribution(m, low, high):
     # 1 + e, 1 / x and a s by 8 u together.  From e^-a = 2^126 on, a = -87.4, its reciprocal is no normal number, and zero from
     # 2^128 on: off by 87.4 * 2^-126 < 2^-119 at most.
     assert np.all(np.abs(silu - want) <= U * (1.23 * np.abs(a) + 8) * np.abs(want) + 2.0**-119)
+
+
+def guarded_workspace(nbytes, value):
+    """`nbytes` inside a buffer of one value, and a check that nothing around them was written."""
+    room = torch.full((nbytes + 8192,), value, dtype=torch.uint8, device="cuda")
+    assert room.data_ptr() % 16 == 0
+
+    def untouched():
+        return bool((room[:4096] == value).all() and (room[4096 + nbytes:] == value).all())
+
+    return room.data_ptr() + 4096, untouched
+
+
+@gpu
+@pytest.mark.parametrize("rows,cols", [(2, 3), (9, 5), (300, 7), (257, 129), (513, 1000), (1001, 1333), (70, 4097), (300, 8200), (270, 16383),
+                                       (1, 16385), (2, 16391), (7, 20001), (300, 17000), (1030, 40001)])
+@pytest.mark.parametrize("dtype,x_dtype", [(F32, F32), (B16, B16)])
+def test_norm_gradients_in_a_workspace_of_exactly_their_bytes(rows, cols, dtype, x_dtype):
+    """Nothing is written beside it and nothing read that was not written: whatever it held before, the result is the same."""
+    x, g, weight = values((rows, cols), 1, x_dtype), values((rows, cols), 2, dtype), 1 + values((cols,), 3)
+    want, want_weight = ops.rms_norm_grad(g, x, weight, 1e-5)
+    nbytes = ops.pat_rms_norm_grad_workspace(rows, cols)
+    for value in (0xFF, 0x7B):
+        work, untouched = guarded_workspace(nbytes, value)
+        out, dweight = torch.empty_like(g), torch.empty(cols, device="cuda")
+        status = ops.pat_rms_norm_grad(g, cols, NAME[dtype], x, cols, NAME[x_dtype], weight, "float32", None, 0, rows, cols, 1e-5, out, cols, dweight, work,
+                                       nbytes, torch.cuda.current_stream())
+        assert status == pat.PAT_OK and untouched()
+        assert torch.equal(out, want) and torch.equal(dweight, want_weight)
+
+
+@gpu
+@pytest.mark.parametrize("rows,inner,cols", [(40, 8449, 200), (64, 5761, 33), (100, 4096, 90), (33, 9000, 129), (512, 8200, 512), (8, 30001, 1000)])
+def test_weight_gradients_in_a_workspace_of_exactly_their_bytes(rows, inner, cols):
+    g, x = values((inner, rows), 1, B16), ops.mxb_quantize(values((inner, cols), 2))
+    nbytes = ops.pat_mxb_weight_grad_workspace(rows, inner, cols)
+    assert nbytes > 0  # sums in slices
+    for dtype in (F32, B16):
+        want = ops.mxb_weight_grad(g, x, dtype)
+        for value in (0xFF, 0x7B):
+            work, untouched = guarded_workspace(nbytes, value)
+            out = torch.empty((rows, cols), dtype=dtype, device="cuda")
+            status = ops.pat_mxb_weight_grad(g, rows, x.codes, x.scales, rows, inner, cols, out, cols, NAME[dtype], work, nbytes,
+                                             torch.cuda.current_stream())
+            assert status == pat.PAT_OK and untouched() and torch.equal(out, want)
