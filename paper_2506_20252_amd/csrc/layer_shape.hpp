@@ -97,9 +97,21 @@ inline int layer_tile(int64_t m, int64_t n) {
   return layer_tiles(m, n, 64, 64) > 256 ? 64 : 32;
 }
 
-// few_kernel: up to so many tokens.  us, and by tiles: 7.8 and 8.5, gated 12.5 and 11.8 (32 tokens, 4096 columns and terms), 10.3 and
-// 11.4, 14.9 and 14.7 (33, 8192, 4096), 18.1 and 19.6, 25.3 and 22.3 (48, 4096, 8192), gated 11.0 and 10.8 (17, 4096, 4096).
+// few_kernel: up to so many tokens.  us, and by tiles: 7.8 and 8.5 (32 tokens, 4096 columns and terms), 10.3 and 11.4 (33, 8192,
+// 4096), 18.1 and 19.6 (48, 4096, 8192).  Gated, 33 tokens: 14.9 and 14.7 (8192, 4096), 48: 25.3 and 22.3 (4096, 8192).
+//
+// Gated products of 17 to 32 tokens go by tiles already where columns are few and terms are many (each of few_kernel's
+// workgroups reads all tokens, as many bytes as its 32 rows of the weight or more).  With 17 and with 32 tokens: 4.1 and 4.9,
+// 4.3 and 4.9 (2048 columns, 512 terms), 4.9 and 5.8, 5.4 and 5.9 (2048, 1333), 6.6 and 6.3, 7.4 and 6.4 (2048, 2000), 9.9 and
+// 8.1, 11.4 and 8.3 (1024, 4096), 16.8 and 11.8, 19.9 and 12.3 (512, 8192), 17.4 and 17.5, 20.3 and 18.6 (2048, 8192); at 4096
+// columns either way, 10.4 and 10.3, 11.9 and 11.4 (4096), 17.4 and 18.7, 20.3 and 20.2 (8192); 10.6 and 11.9, 12.1 and 13.6
+// (8192, 4096).
 constexpr int kFewLinear = 48, kFewGated = 32;
+inline bool few_product(int64_t m, int64_t n, int64_t k, bool gated) {
+  if (k == 0) return true;
+  if (!gated) return m <= kFewLinear;
+  return m <= 16 || (m <= kFewGated && (n > 2048 || k <= 1536));
+}
 // Its columns of the output, in sixteens (two where gated, each two rows of the weight): as many as leave a workgroup for each of
 // the 256 CUs, since every workgroup reads the tokens.  And the tokens that go into one launch of fewer than 2^22 workgroups.
 inline int few_columns_sixteens(int64_t n) { return n <= 16 * 256 ? 1 : n <= 32 * 256 ? 2 : 4; }
@@ -123,7 +135,7 @@ struct ProductPlan {
 inline ProductPlan product_plan(int64_t m, int64_t n, int64_t k, bool gated, bool blocks) {
   ProductPlan p{};
   const int64_t width = blocks ? groups_of(n) * 128 : n;
-  if (k > 0 && m > (gated ? kFewGated : kFewLinear)) {
+  if (!few_product(m, n, k, gated)) {
     p.tile = layer_tile(m, gated ? 2 * n : n);
     p.threads = tile_threads(p.tile);
     p.tiles_n = (int64_t)ceil_div(width, gated ? tile_rows(p.tile) / 2 : tile_rows(p.tile));

@@ -2,6 +2,7 @@
 // of a product gets workgroups for all of its output and fewer than 2^32 lanes a launch, and the workspace of the norm's
 // gradients holds everything that the kernels put there, each part in its own place.
 #include <cstdio>
+#include <utility>
 
 #include "layer_shape.hpp"
 
@@ -78,6 +79,13 @@ int main() {
     for (int f = 0; f <= 26; ++f)
       for (int d = -17; d <= 17; ++d) products(((int64_t)1 << e) + d, ((int64_t)1 << f) + d);
   for (int i = 0; i < 100000; ++i) products(rnd((1 << 26) + 100), rnd((1 << 26) + 100));
+  // Gated products of 17 to 32 tokens: the faster kernel of each side of the rule, as measured.
+  for (int64_t m : {17, 24, 32}) {
+    for (const auto& s : {std::pair{512, 2000}, {2048, 2000}, {1024, 4096}, {512, 8192}, {1024, 8192}, {512, 16384}})
+      CHECK(product_plan(m, s.first, s.second, true, false).tile != 0, "%lld %d %d", (long long)m, s.first, s.second);
+    for (const auto& s : {std::pair{512, 512}, {2048, 1333}, {8192, 1333}, {8192, 4096}, {16384, 4096}, {8192, 8192}})
+      CHECK(product_plan(m, s.first, s.second, true, false).tile == 0, "%lld %d %d", (long long)m, s.first, s.second);
+  }
   for (int64_t cols = 1; cols < 40000; ++cols)
     for (int64_t rows : {1, 2, 7, 255, 256, 257, 513, 2048, 100000}) check_space(rows, cols);
   for (int i = 0; i < 200000; ++i) check_space(rnd(1 << 28), rnd(1 << 26));

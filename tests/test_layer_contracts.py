@@ -15,8 +15,8 @@ import torch
 from oracle import layer as L
 from paper_2506_20252_amd import build as B
 from paper_2506_20252_amd import ops, pat
-from test_layer_ops import blocks_within, depth
-from test_ops import E, F32, B16, U, f64, values, within
+from test_layer_ops import blocks_within, depth, gated_error, random_mxb
+from test_ops import E, F32, B16, U, f64, guarded, random_mx, values, within
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 gpu = pytest.mark.gpu
@@ -172,7 +172,7 @@ def test_launches_take_their_sizes_from_what_is_checked():
     with open(os.path.join(B.CSRC, "mxb_product.hip")) as f:
         product = f.read()
     assert product.count("product_plan(m, n, k,") == 2 and product.count("hipLaunchKernelGGL") == 2
-    assert not re.search(r"\b(layer_tile|few_band|few_columns_sixteens|kFewGated|kFewLinear)\b", product)
+    assert not re.search(r"\b(layer_tile|few_band|few_columns_sixteens|few_product|kFewGated|kFewLinear)\b", product)
     with open(os.path.join(B.CSRC, "norm.hip")) as f:
         norm = f.read()
     assert norm.count("norm_grad_space(") == 2
@@ -316,3 +316,25 @@ def test_weight_gradients_in_a_workspace_of_exactly_their_bytes(rows, inner, col
             status = ops.pat_mxb_weight_grad(g, rows, x.codes, x.scales, rows, inner, cols, out, cols, NAME[dtype], work, nbytes,
                                              torch.cuda.current_stream())
             assert status == pat.PAT_OK and untouched() and torch.equal(out, want)
+
+
+@gpu
+@pytest.mark.parametrize("m,n,k", [(16, 60, 1700), (17, 60, 1537), (24, 100, 2000), (32, 33, 4100), (32, 2048, 1664), (32, 2049, 1664),
+                                   (17, 2048, 1536), (33, 40, 1700)])
+@pytest.mark.parametrize("name", ["silu", "gelu"])
+def test_gated_products_on_either_side_of_the_kernels_rule(m, n, k, name):
+    x, vx = random_mxb(m, k, m + n, 118, 124)
+    w, vw = random_mx(2 * n, k, n + k, 113, 122)
+    h, a, b, eh, ea, eb = gated_error(vx, vw, n, k, name)
+    for dtype in (F32, B16):
+        out, untouched = guarded((m, n), dtype, pad=n % 3, shift=1)
+        ops.gated(x, w, name, dtype, out=out)
+        assert untouched()
+        assert np.all(np.abs(f64(out) - h) <= eh + (E if dtype == B16 else 2 * U) * np.abs(h) + 1e-300)
+    plain = out
+    other, saved = ops.gated(x, w, name, B16, True)
+    q = ops.gated(x, w, name, ops.Mxb)
+    assert torch.equal(other, plain)
+    blocks_within(q, h, eh)
+    blocks_within(ops.Mxb(saved.codes[:m], saved.scales[:m], n), a, ea)
+    blocks_within(ops.Mxb(saved.codes[m:], saved.scales[m:], n), b, eb)
