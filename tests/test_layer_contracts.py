@@ -15,7 +15,7 @@ import torch
 from oracle import layer as L
 from paper_2506_20252_amd import build as B
 from paper_2506_20252_amd import ops, pat
-from test_layer_ops import blocks_within, depth, gated_error, random_mxb
+from test_layer_ops import EVERY, blocks_within, depth, every_operator, flat, gated_error, random_mxb
 from test_ops import E, F32, B16, U, f64, guarded, random_mx, values, within
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -338,3 +338,58 @@ def test_gated_products_on_either_side_of_the_kernels_rule(m, n, k, name):
     blocks_within(q, h, eh)
     blocks_within(ops.Mxb(saved.codes[:m], saved.scales[:m], n), a, ea)
     blocks_within(ops.Mxb(saved.codes[m:], saved.scales[m:], n), b, eb)
+
+
+# ---------------------------------------------------------------------------
+# New tensors
+# ---------------------------------------------------------------------------
+
+
+@gpu
+@pytest.mark.parametrize("shape", [(3, 5), (1, 1), (7, 0), (0, 7), (0, 0), (9,), (0,)])
+@pytest.mark.parametrize("dtype", [F32, B16, torch.uint8])
+def test_new_tensors_are_as_torch_makes_them(shape, dtype, monkeypatch):
+    """By torch's own short way, where it has one, or by the public call: the same kind of tensor."""
+    like = torch.empty(1, device="cuda")
+    made = [ops._empty(shape, dtype, like, None)]
+    monkeypatch.setattr(ops, "_strided", None)
+    made.append(ops._empty(shape, dtype, like, None))
+    want = like.new_empty(shape, dtype=dtype)
+    for t in made:
+        assert type(t) is torch.Tensor and not t.requires_grad and t.is_contiguous()
+        assert (t.shape, t.stride(), t.dtype, t.device) == (want.shape, want.stride(), want.dtype, want.device)
+
+
+@gpu
+@pytest.mark.parametrize("name", EVERY)
+def test_without_torchs_short_ways(name, monkeypatch):
+    """Where this torch has no private functions for streams and new tensors: the same results, on the current stream."""
+    call = every_operator()[name]
+    want = [t.clone() for t in flat(call())]
+    monkeypatch.setattr(ops, "_strided", None)
+    monkeypatch.setattr(ops, "_raw_stream", None)
+    monkeypatch.setattr(ops, "_current_device", torch.cuda.current_device)
+    assert all(torch.equal(a, b) for a, b in zip(flat(call()), want))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = flat(call())
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@gpu
+@pytest.mark.parametrize("name", EVERY)
+def test_every_element_of_a_result_is_written(name, monkeypatch):
+    """Whatever new memory holds: results and workspaces are filled before the call here, as torch does it to new tensors in its
+    deterministic mode."""
+    call, empty = every_operator()[name], ops._empty
+    want = [t.clone() for t in flat(call())]
+    for value in (0xFF, 0x5A):
+        def filled(shape, dtype, like, stream):
+            t = empty(shape, dtype, like, stream)
+            t.view(torch.uint8).fill_(value)
+            return t
+
+        monkeypatch.setattr(ops, "_empty", filled)
+        assert all(torch.equal(a, b) for a, b in zip(flat(call()), want))
