@@ -15,7 +15,7 @@ import torch
 from oracle import layer as L
 from paper_2506_20252_amd import build as B
 from paper_2506_20252_amd import ops, pat
-from test_layer_ops import EVERY, blocks_within, depth, every_operator, flat, gated_error, random_mxb
+from test_layer_ops import EVERY, act_error, blocks_within, depth, every_operator, flat, gated_error, random_mxb
 from test_ops import E, F32, B16, U, f64, guarded, random_mx, values, within
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -393,3 +393,67 @@ def test_every_element_of_a_result_is_written(name, monkeypatch):
 
         monkeypatch.setattr(ops, "_empty", filled)
         assert all(torch.equal(a, b) for a, b in zip(flat(call()), want))
+
+
+# ---------------------------------------------------------------------------
+# Stored matrices beyond 4 GiB
+# ---------------------------------------------------------------------------
+
+
+def repeated(q, parts, rows):
+    """The rows of a stored matrix again and again, `rows` of them."""
+    return type(q)(*(t.repeat(parts, 1)[:rows].contiguous() for t in q[:2]), q.cols)
+
+
+def parts_agree(t, each):
+    """Rows `each` apart hold the same."""
+    return all(torch.equal(part, t[:len(part)]) for part in t.split(each))
+
+
+@gpu
+@pytest.mark.parametrize("n", [40, 300])
+def test_products_of_more_than_4_gib_of_tokens(n):
+    """Every part of the result is that of the same tokens elsewhere, and the first is right."""
+    each, k = 4096, 8200
+    m = 128 * each + 77
+    some, v = random_mxb(each, k, 1, 118, 124)
+    w, vw = random_mx(2 * n, k, 2, 112, 118)
+    x = repeated(some, 129, m)
+    assert x.codes.numel() > 1 << 32
+    out = ops.mxb_linear(x, w, F32)
+    assert parts_agree(out, each)
+    within(out[:300], v[:300] @ vw.T, np.abs(v[:300]) @ np.abs(vw).T, k, F32)
+    h, saved = ops.gated(x, w, "silu", ops.Mxb, True)
+    _, a, b, _, ea, eb = gated_error(v[:300], vw, n, k, "silu")
+    for codes, scales in ((saved.codes[:m], saved.scales[:m]), (saved.codes[m:], saved.scales[m:]), h[:2]):
+        assert parts_agree(codes, each) and parts_agree(scales, each)
+    blocks_within(ops.Mxb(saved.codes[:300], saved.scales[:300], n), a, ea)
+    blocks_within(ops.Mxb(saved.codes[m:m + 300], saved.scales[m:m + 300], n), b, eb)
+    # each row counts as often as it is there
+    g = values((each, n), 3, B16)
+    dw = ops.mxb_weight_grad(g.repeat(129, 1)[:m], x, F32)
+    times = np.where(np.arange(each) < 77, 129.0, 128.0)[:, None]
+    vg = f64(g) * times
+    within(dw, vg.T @ v, np.abs(vg).T @ np.abs(v), m, F32)
+
+
+@gpu
+@pytest.mark.parametrize("m", [1, 33, 70])
+def test_products_of_more_than_4_gib_of_weights(m):
+    each, k = 4096, 8200
+    n = 128 * each + 77
+    x, vx = random_mxb(m, k, 1, 118, 124)
+    some, v = random_mx(each, k, 2, 112, 118)
+    half = repeated(some, 129, n)
+    w = ops.Mx(torch.cat((half.codes, half.codes)), torch.cat((half.scales, half.scales)), k)
+    assert half.codes.numel() > 1 << 31 and w.codes.numel() > 1 << 32
+    a, size = vx @ v.T, np.abs(vx) @ np.abs(v).T
+    out = ops.mxb_linear(x, w, F32)
+    assert parts_agree(out[:, :n].t(), each) and torch.equal(out[:, :n], out[:, n:])
+    within(out[:, :each], a, size, k, F32)
+    h = ops.gated(x, w, "silu", F32)
+    assert parts_agree(h.t(), each)
+    err = 2 * (k + 2) * U * size
+    want = L.act(a, "silu")[0]
+    off = np.abs(f64(h[:, :each]) - want * a)
+    assert np.all(off <= 1.01 * (act_error(a, "silu", err) * np.abs(a) + (np.abs(want) + err) * err + 4 * U * np.abs(want * a)))
