@@ -457,3 +457,30 @@ def test_products_of_more_than_4_gib_of_weights(m):
     want = L.act(a, "silu")[0]
     off = np.abs(f64(h[:, :each]) - want * a)
     assert np.all(off <= 1.01 * (act_error(a, "silu", err) * np.abs(a) + (np.abs(want) + err) * err + 4 * U * np.abs(want * a)))
+
+
+@gpu
+def test_products_of_the_most_terms():
+    """2^24 - 1 terms in the largest tiles, whose rows lie up to 2^32 bytes apart: values of 0 and 1, so that every sum is a whole
+    number below 2^24 and exact."""
+    m, n, k, part = 2900, 2898, (1 << 24) - 1, 8192
+    g = torch.Generator(device="cuda").manual_seed(1)
+    bits_x, bits_w = (torch.randint(0, 2, (rows, part), device="cuda", generator=g, dtype=torch.uint8) for rows in (m, n))
+    want = torch.mm(bits_x.double(), bits_w.double().t().contiguous()) * 2048
+    want -= torch.outer(bits_x[:, -1].double(), bits_w[:, -1].double())
+    assert float(want.max()) < 1 << 24
+    codes = (bits_x * 0x38).repeat(1, 2048)
+    codes[:, -1] = 0
+    x = ops.Mxb(codes, torch.full((m, 1 << 19), 127, dtype=torch.uint8, device="cuda"), k)
+    codes = (2 * bits_w[:, 0::2] + 32 * bits_w[:, 1::2]).repeat(1, 2048)
+    codes[:, -1] &= 15
+    w = ops.Mx(codes, torch.full((n, 1 << 19), 127, dtype=torch.uint8, device="cuda"), k)
+    del codes
+    assert torch.equal(ops.mxb_linear(x, w, F32).double(), want)
+    a, b = want[:, :n // 2], want[:, n // 2:]
+    h = ops.gated(x, w, "silu", F32).double()
+    assert bool(((h - a * b).abs() <= 8 * U * a * b).all())  # e^-a is 0 against 1; a quotient and two products
+    assert torch.equal(ops.mxb_linear(ops.Mxb(x.codes[:70], x.scales[:70], k), w, F32).double(), want[:70])
+    assert torch.equal(ops.mxb_linear(ops.Mxb(x.codes[:5], x.scales[:5], k), w, F32).double(), want[:5])
+    del x, w
+    torch.cuda.empty_cache()
