@@ -5,7 +5,8 @@ namespace pat {
 namespace {
 
 // A lane takes 8 columns of a row, 16 lanes a group of 128, as the casts do.  Bound by memory: 8192 x 8192 bfloat16 (541 MB) in
-// 82.5 us, 6.6 TB/s, by nontemporal loads (95 with cached ones, 87 with nontemporal stores too); two groups a lane at once: 97.
+// 81 us, 6.7 TB/s, by nontemporal loads (95 with cached ones, 87 with nontemporal stores too); two groups a lane at once: 97.
+// From a float32 gradient (675 MB) 105, 6.4.
 template <typename G>
 __global__ __launch_bounds__(256) void gated_grad_kernel(Mat g, MxbMat a, MxbMat b, uint32_t total, int64_t n, Divisor groups, Act act,
                                                          MatOut out) {

@@ -415,7 +415,8 @@ hipError_t launch_mx_grad(Mat g, bool transposed, MxMat q, int64_t rows, int64_t
                     : pick_grad<Fours, false>(g, q, rows, inner, cols, out, dtype, workspace, stream);
 }
 
-// 8192 x 4096 from 8192 rows, float32 out: 460 us, 1195 TFLOP/s, as the 4-bit form is bound, by LDS's traffic.
+// 8192 x 4096 from 8192 rows, float32 out: 470 us, 1170 TFLOP/s (460 to 483 from card to card), bfloat16 458; as the 4-bit form is
+// bound, by LDS's traffic.
 hipError_t launch_mxb_weight_grad(Mat g, MxbMat x, int64_t rows, int64_t inner, int64_t cols, MatOut out, Elem dtype,
                                   void* workspace, hipStream_t stream) {
   return pick_grad<Eights, true>(g, {x.codes, x.scales}, rows, inner, cols, out, dtype, workspace, stream);

@@ -90,11 +90,12 @@ __device__ __forceinline__ void load_to_lds4(const uint8_t* p, const uint8_t* to
 // are two neighbouring bytes, of which the instruction picks the J-th.
 //
 // Bound by the matrix instructions' rate, of which the loads into LDS take a part.  8192 tokens, 2 x 8192 rows, 4096 terms in
-// 381 us, 2.9 PFLOP/s, 8192^3 with a residual in 406, 2.7: the instructions out of registers alone give 4.5 at the clock
-// of short runs.  Measured for the former (418 us then): a wave of higher priority 540, scales packed 458, three steps on their way, the
-// weight by half lines, 455, bands of 3, 4 or 8 tiles of tokens no faster, no loads at all 340.  Each instruction followed by
-// its share of the reads and loads, and the loads' waits counted, gave the last 8 %: issued together after the barrier they
-// kept the instructions behind them waiting.  Two workgroups of 128 tokens a CU, the weight by half lines: 532.
+// 404 us, 2.7 PFLOP/s, 8192^3 with a residual in 419, 2.6 (medians of one card; 381 to 406 and 406 to 420 from card to card): the
+// instructions out of registers alone give 4.5 at the clock of short runs.  In 8 bits the former takes 418, with a
+// checkpoint 474, in float32 462.  Measured for the former (418 us then): a wave of higher priority 540, scales packed 458,
+// three steps on their way, the weight by half lines, 455, bands of 3, 4 or 8 tiles of tokens no faster, no loads at all 340.
+// Each instruction followed by its share of the reads and loads, and the loads' waits counted, gave the last 8 %: issued together
+// after the barrier they kept the instructions behind them waiting.  Two workgroups of 128 tokens a CU, the weight by half lines: 532.
 template <int FN, int FM, int WN, int WM>
 struct Tile {
   static constexpr int kWaves = WN * WM, N = 32 * FN * WN, M = 32 * FM * WM;

@@ -190,8 +190,8 @@ __device__ __forceinline__ void total_of(const Raw<X>& x, const Raw<X>& r, bool 
 }
 
 // Workgroups go through rows gridDim.x apart; a row's values stay in registers, the weight too, and the next row's loads are on
-// their way before this row's sum.  Bound by memory: 8192 x 8192 bfloat16 with a residual (537 MB) in 81 us, 6.6 TB/s (94 with
-// a workgroup for every row); loads and the total's stores are nontemporal, the output's, which are read next, are not.
+// their way before this row's sum.  Bound by memory: 8192 x 8192 bfloat16 with a residual (537 MB) in 80 us, 6.7 TB/s (94 with
+// a workgroup for every row), float32 (1.07 GB) in 155, 6.9, float32 to 8 bits (874 MB) in 160, 5.5; loads and the total's stores are nontemporal, the output's, which are read next, are not.
 template <typename X, typename O, int U>
 __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) {
   constexpr bool SPLIT = O::kBytes > 1 && Split<X, O>::value;
@@ -285,9 +285,9 @@ __global__ __launch_bounds__(kNormMost) void norm_long_kernel(NormArgs a) {
 // Bound by memory.  A row's loads are all on their way before its sums, and, where the registers suffice (AHEAD, up to 16
 // columns a lane), the next row's before this row's results; the weight stays in registers then too (KEEP).  Wider lanes load
 // it twice, the second time under the sums, and the total's gradient with the rest where that fits (EARLY: 4096 x 16384 in
-// 123 us, 147 with both after the sums, 175 with the next row's x and g before them).  8192 x 8192 bfloat16 with a total's
-// gradient (537 MB) in 89 us with the parts' sum, 6.0 TB/s (97 without that gradient ahead), 16384 x 4096 in 97, 8192 x 2560
-// in 40, 10513 x 2129 in 59.
+// 122 us, 147 with both after the sums, 175 with the next row's x and g before them).  8192 x 8192 bfloat16 with a total's
+// gradient (537 MB) in 88 us with the parts' sum, 6.1 TB/s (97 without that gradient ahead), 16384 x 4096 in 95, 8192 x 2560
+// in 40, 10513 x 2129 in 59; without the next row ahead float32 (1.07 GB) in 184, 5.8 TB/s, x alone float32 (671 MB) in 129, 5.2.
 template <typename X, typename G, int U>
 __global__ __launch_bounds__(kNormGradMost, U == 1 ? 4 : U == 2 && X::kBytes >= G::kBytes ? 3 : 2) void norm_grad_kernel(
     NormGradArgs a, int lanes, float* sums, int64_t pitch) {
@@ -435,8 +435,8 @@ __global__ __launch_bounds__(kStripThreads) void norm_sums_kernel(NormGradArgs a
   }
 }
 
-// Then a strip of columns a workgroup, every gridDim.y-th row.  Both: 2048 x 20000 bfloat16 with a total's gradient in 95 us (328 MB, and g and x
-// once more).
+// Then a strip of columns a workgroup, every gridDim.y-th row.  Both: 2048 x 20000 bfloat16 with a total's gradient in 95 to 100 us (328 MB,
+// and g and x once more).
 template <typename X, typename G>
 __global__ __launch_bounds__(kStripThreads) void norm_strip_kernel(NormGradArgs a, const v2f* rows, float* sums, int64_t pitch) {
   constexpr bool SPLIT = Split<X, G>::value;
