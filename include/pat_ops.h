@@ -265,8 +265,9 @@ pat_status_t pat_rms_norm(const void* x, int64_t x_stride, const void* residual,
  *   dweight[c] = sum over rows of g * x * r  (PAT_FLOAT32, cols elements, 4-byte aligned).
  * out is the gradient of x and of the residual alike; total_grad (NULL: none) is what
  * reaches the total from elsewhere.  g, total_grad and out: dtype; x: x_dtype.  Sums are
- * float32's, as the norm's: beside x^2, the magnitudes of g * weight * x sum to 2^127 at
- * most in a row.  With no rows dweight is zero.  In place: out == g or out == total_grad with equal strides.
+ * float32's, in the norm's range; the magnitudes of g * weight * x, too, may sum to 2^127
+ * at most in a row.  With no rows dweight is zero.
+ * In place: out == g or out == total_grad with equal strides.
  * Fewer than 2^28 rows, 2^26 columns (else PAT_ERR_UNSUPPORTED).
  */
 pat_status_t pat_rms_norm_grad(const void* g, int64_t g_stride, pat_dtype_t dtype, const void* x, int64_t x_stride,

@@ -631,6 +631,7 @@ hipError_t pick_tile(const ProductPlan& p, MxbMat x, MxMat w, int64_t m, int64_t
 // Bound by the weight's bytes and one latency each of loading, joining and storing: one token by 2 x 8192 gated rows of 4096 terms
 // (35.7 MB) in 8.8 us, by 8192 rows (17.8 MB) in 5.6; by 2 x 28672 of 8192 (250 MB) in 55, 4.6 TB/s.  A lane with 64 bytes in a row of
 // the weight instead: 8.9, 5.7 and 56.
+
 // Of four words of lanes l, l + 16, l + 32 and l + 48 the byte l / 16 of each, in order.
 __device__ __forceinline__ int turn_bytes(int w) {
   const int quarter = threadIdx.x % 64 / 16;

@@ -191,7 +191,8 @@ __device__ __forceinline__ void total_of(const Raw<X>& x, const Raw<X>& r, bool 
 
 // Workgroups go through rows gridDim.x apart; a row's values stay in registers, the weight too, and the next row's loads are on
 // their way before this row's sum.  Bound by memory: 8192 x 8192 bfloat16 with a residual (537 MB) in 80 us, 6.7 TB/s (94 with
-// a workgroup for every row), float32 (1.07 GB) in 155, 6.9, float32 to 8 bits (874 MB) in 160, 5.5; loads and the total's stores are nontemporal, the output's, which are read next, are not.
+// a workgroup for every row), float32 (1.07 GB) in 155, 6.9, float32 to 8 bits (874 MB) in 160, 5.5; loads and the total's
+// stores are nontemporal, the output's, which are read next, are not.
 template <typename X, typename O, int U>
 __global__ __launch_bounds__(kNormMost) void norm_kernel(NormArgs a, int lanes) {
   constexpr bool SPLIT = O::kBytes > 1 && Split<X, O>::value;
@@ -435,8 +436,8 @@ __global__ __launch_bounds__(kStripThreads) void norm_sums_kernel(NormGradArgs a
   }
 }
 
-// Then a strip of columns a workgroup, every gridDim.y-th row.  Both: 2048 x 20000 bfloat16 with a total's gradient in 95 to 100 us (328 MB,
-// and g and x once more).
+// Then a strip of columns a workgroup, every gridDim.y-th row.  Both: 2048 x 20000 bfloat16 with a total's gradient in 95 to
+// 100 us (328 MB, and g and x once more).
 template <typename X, typename G>
 __global__ __launch_bounds__(kStripThreads) void norm_strip_kernel(NormGradArgs a, const v2f* rows, float* sums, int64_t pitch) {
   constexpr bool SPLIT = Split<X, G>::value;

@@ -589,7 +589,7 @@ def mxb_quantize(x, out=None, stream=None):
 
 
 def mxb_dequantize(q, dtype=torch.bfloat16, out=None, stream=None):
-    """The matrix that an Mxb stands for, in `dtype` (exact but for bfloat16 below 2^-126)."""
+    """The matrix that an Mxb stands for, in `dtype` (exact but for bfloat16 below 2^-126; values of 2^128 are infinite)."""
     codes, scales, rows, cols = _blocks(q, "q")
     code = _float(dtype, "dtype")
     if out is None:
@@ -702,7 +702,8 @@ def _vector(t, n, what):
 def rms_norm(x, weight, eps, residual=None, dtype=None, total=None, out=None, stream=None):
     """t * weight / sqrt(mean(t^2) + eps) of every row, t = x; `dtype` is x's by default and may be Mxb, for a next product.
     With a `residual`, t = x + residual rounded to x's type, and the result is (out, t); `total` is where t goes, new by
-    default.  `total` or `out` may be x or the residual."""
+    default.  `total` or `out` may be x or the residual.  Sums of squares are float32's: full precision up to 2^127 a row, and
+    zeros from 2^128 on."""
     rows, cols, x_stride, x_code = _matrix(x, "x")
     weight_code = _vector(weight, cols, "weight")
     out, address, stride, code, codes, scales, tensors = _result(out, rows, cols, x.dtype if dtype is None else dtype, x, "rms_norm",
